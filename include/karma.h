@@ -590,6 +590,116 @@ int karma_k_attention_bwd_bf16(const void* qkv_dev, const void* ctx_dev, const v
                                float* delta_ws_dev, void* dqkv_dev, uint32_t batch, uint32_t seq, uint32_t heads,
                                uint32_t d, void* stream);
 
+/* ---- gated linear recurrence, a sequence layer whose memory does not grow with the sequence --------
+ * h_t = h_{t-1} + b_t (x_t - h_{t-1}),  b_t = 1 / (1 + e^gate_t), per channel; b is one minus the gate's sigmoid: a large
+ * gate keeps the state, a small one takes the input.  The tokens of `sequences` sequences lie one behind the other in
+ * tensors [tokens][ld] (channels <= ld side by side; a stride of 0 stands for channels; gate and x may be halves of one
+ * projection).  starts_dev int32 [sequences + 1], ascending from 0: sequence j has tokens starts[j] .. starts[j+1] - 1, none
+ * if they are equal; rows from starts[sequences] on are neither used nor written.  starts_dev NULL: all sequences have
+ * tokens / sequences tokens.
+ * h0_dev fp32 [sequences][channels], the states to start from (NULL: zeros); h_last_dev, the same shape, receives the states
+ * behind the last tokens (h0 for a sequence without tokens; may be NULL, may be h0_dev).  marks_dev (NULL where no backward
+ * pass follows) fp32 [ceil(tokens / KARMA_SCAN_MARK)][channels] receives the state before every KARMA_SCAN_MARK-th row, all
+ * that the backward pass needs beside gate and x (undefined where that row starts a sequence or belongs to none).
+ * h_dev may be gate_dev or x_dev where the strides are equal; no other overlap.
+ * ws_dev: karma_k_gated_scan_ws_bytes(shape) bytes (0 for a wrong shape), 16-byte aligned, for one call at a time: calls that may run at the same
+ * time (graphs replayed on two streams among them) need a workspace each.  The call clears what it needs cleared.
+ * Errors: KARMA_E_INVAL, KARMA_E_OOM (ws_bytes too small). */
+#define KARMA_SCAN_MARK 256u
+typedef struct {
+  uint64_t tokens;              /* rows of the tensors, < 2^31 */
+  uint32_t channels, sequences; /* at least one of each */
+  uint64_t ld_gate, ld_x, ld_h, ld_dgate, ld_dx; /* elements; ld_h: of h and of dh */
+} karma_scan_shape;
+uint64_t karma_k_gated_scan_ws_bytes(const karma_scan_shape* shape);
+int karma_k_gated_scan_fwd_bf16(const void* gate_dev, const void* x_dev, const float* h0_dev, const int32_t* starts_dev, void* h_dev,
+                                float* h_last_dev, float* marks_dev, const karma_scan_shape* shape, void* ws_dev, uint64_t ws_bytes,
+                                void* stream);
+int karma_k_gated_scan_fwd_f32(const float* gate_dev, const float* x_dev, const float* h0_dev, const int32_t* starts_dev, float* h_dev,
+                               float* h_last_dev, float* marks_dev, const karma_scan_shape* shape, void* ws_dev, uint64_t ws_bytes,
+                               void* stream);
+/* Its backward: dgate and dx from dh (the gradient of every h_t) and dh_last_dev fp32 [sequences][channels] (of the last
+ * states; NULL: zeros); dh0_dev (may be NULL), the gradient of h0 (dh_last for a sequence without tokens).  The states
+ * are computed again from marks_dev; h itself is not needed.  dgate_dev and dx_dev may be gate_dev, x_dev or dh_dev (each
+ * another one) where the strides are equal; dh0_dev overlaps nothing. */
+int karma_k_gated_scan_bwd_bf16(const void* gate_dev, const void* x_dev, const float* h0_dev, const int32_t* starts_dev,
+                                const float* marks_dev, const void* dh_dev, const float* dh_last_dev, void* dgate_dev, void* dx_dev,
+                                float* dh0_dev, const karma_scan_shape* shape, void* ws_dev, uint64_t ws_bytes, void* stream);
+int karma_k_gated_scan_bwd_f32(const float* gate_dev, const float* x_dev, const float* h0_dev, const int32_t* starts_dev,
+                               const float* marks_dev, const float* dh_dev, const float* dh_last_dev, float* dgate_dev, float* dx_dev,
+                               float* dh0_dev, const karma_scan_shape* shape, void* ws_dev, uint64_t ws_bytes, void* stream);
+
+/* ---- log probabilities of given tokens, entropies and best alternatives of rows of logits ---------
+ * logits_dev [rows][ld], cols <= ld used (ld 0: cols); q_j = scale z_j - ln sum_i e^(scale z_i), scale > 0 (one over the
+ * temperature).  Outputs, each NULL where it is not wanted (not all of them):
+ *   logprob_dev fp32 [rows]     q of tokens_dev[row]; 0 where the token is none of the columns (-1: padding)
+ *   entropy_dev fp32 [rows]     -sum_j e^q_j q_j
+ *   stats_dev fp32 [rows][2]    the largest z and ln sum_j e^(scale (z_j - largest)), for the backward pass
+ *   top_logprob_dev fp32, top_id_dev int32 [rows][top]: the `top` largest (at most KARMA_TOP_MAX and cols), in descending
+ *                               order, equal ones by ascending index
+ * A logit of -inf is not allowed: its probability is 0.  A row of nothing else has q = -inf, entropy 0 and gradient 0.  +inf
+ * or NaN in a row makes its results NaN (NaN is no alternative; where too few are left the index is -1).
+ * ws_dev: karma_k_token_logprob_ws_bytes(rows, cols, top) bytes, 16-byte aligned, for one call at a time (0 bytes: may be NULL).
+ * Errors: KARMA_E_INVAL, KARMA_E_OOM. */
+#define KARMA_TOP_MAX 64u
+uint64_t karma_k_token_logprob_ws_bytes(uint32_t rows, uint32_t cols, uint32_t top);
+int karma_k_token_logprob_fwd_bf16(const void* logits_dev, uint64_t ld, const int32_t* tokens_dev, float* logprob_dev, float* entropy_dev,
+                                   float* stats_dev, float* top_logprob_dev, int32_t* top_id_dev, uint32_t rows, uint32_t cols,
+                                   uint32_t top, float scale, void* ws_dev, uint64_t ws_bytes, void* stream);
+int karma_k_token_logprob_fwd_f32(const float* logits_dev, uint64_t ld, const int32_t* tokens_dev, float* logprob_dev, float* entropy_dev,
+                                  float* stats_dev, float* top_logprob_dev, int32_t* top_id_dev, uint32_t rows, uint32_t cols,
+                                  uint32_t top, float scale, void* ws_dev, uint64_t ws_bytes, void* stream);
+/* Gradient with respect to the logits, dlogits_dev [rows][ld_d] (ld_d 0: cols), from those of logprob and entropy (fp32
+ * [rows], one may be NULL) and the forward's stats and entropy (entropy_dev only with dentropy_dev).  dlogits_dev may be
+ * logits_dev where the strides are equal.  Columns from cols on are not touched. */
+int karma_k_token_logprob_bwd_bf16(const void* logits_dev, uint64_t ld, const int32_t* tokens_dev, const float* stats_dev,
+                                   const float* entropy_dev, const float* dlogprob_dev, const float* dentropy_dev, void* dlogits_dev,
+                                   uint64_t ld_d, uint32_t rows, uint32_t cols, float scale, void* stream);
+int karma_k_token_logprob_bwd_f32(const float* logits_dev, uint64_t ld, const int32_t* tokens_dev, const float* stats_dev,
+                                  const float* entropy_dev, const float* dlogprob_dev, const float* dentropy_dev, float* dlogits_dev,
+                                  uint64_t ld_d, uint32_t rows, uint32_t cols, float scale, void* stream);
+
+/* ---- AdamW over many tensors at once ----------------------------------------------------------------
+ * Per tensor of n values: w fp32, grad bf16 or fp32, out (may be NULL) bf16 or fp32, the moments m and v.  With g = grad_scale * grad:
+ *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
+ *   w -= lr weight_decay w + lr m / (1 - beta1^step) / (sqrt(v / (1 - beta2^step)) + eps),  out = w.
+ * KARMA_ADAMW_STATES_8BIT: m is int8 [n], v uint8 [n], and every KARMA_ADAMW_BLOCK values share an element of m_scale and
+ * v_scale, fp32 [ceil(n / KARMA_ADAMW_BLOCK)]: m = code * m_scale, v = code^2 * v_scale (all zeros: states at the beginning).
+ * The step is computed from the moments before they are rounded; each then becomes one of the two codes around it at random, its
+ * expectation kept (v > 0 becomes at least code 1).  The random bits follow from `seed`, the tensor's place in the list and the element's:
+ * give every step another seed.  A gradient that is not finite makes the scales, and with them the moments, of its block NaN.
+ * Without the flag m and v are fp32 [n].  Tensors overlap nothing, other tensors of the list included; n may be 0.
+ * tensors is a host array, read during the call.  live_dev (may be NULL): lr, grad_scale, step and seed are read from there when
+ * the kernels run, not from `now`: for a captured graph, which is replayed with other values (a step of 0 counts as 1).
+ * Errors: KARMA_E_INVAL (step 0 and betas outside [0, 1) among them). */
+#define KARMA_ADAMW_GRAD_BF16 1u
+#define KARMA_ADAMW_OUT_BF16 2u
+#define KARMA_ADAMW_STATES_8BIT 4u
+#define KARMA_ADAMW_BLOCK 64u
+typedef struct {
+  float* w;
+  void* m; void* v;
+  float* m_scale; float* v_scale; /* NULL with fp32 states */
+  const void* grad;
+  void* out;
+  uint64_t n;
+  float weight_decay;
+  uint32_t flags;
+} karma_adamw_tensor;
+typedef struct {
+  float lr, beta1, beta2, eps, grad_scale;
+  uint32_t seed;
+  uint64_t step; /* counts from 1 */
+} karma_adamw_step;
+typedef struct {
+  float lr, grad_scale;
+  uint32_t step, seed;
+} karma_adamw_live;
+int karma_k_adamw(const karma_adamw_tensor* tensors, uint32_t n, const karma_adamw_step* now, const karma_adamw_live* live_dev, void* stream);
+/* The moments that 8-bit states stand for, in fp32 (checkpoints, inspection, a change to fp32 states): m_out and v_out are host
+ * arrays of n device pointers, to as many values as the tensor has.  All tensors need the flag; w, grad and out are not looked at. */
+int karma_k_adamw_states(const karma_adamw_tensor* tensors, uint32_t n, float* const* m_out, float* const* v_out, void* stream);
+
 /* ---- convolutional workload (Sec. III-C: convolution, batch normalisation, ReLU and
  * pooling layers).  Tensors are NHWC bf16, convolution weights [c_out][r][s][c_in]; c_in and
  * c_out must be multiples of 8 (an image with 3 channels is stored with 8, the rest zero).

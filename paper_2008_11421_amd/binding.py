@@ -21,6 +21,8 @@ GEMM_A_STRIDED, GEMM_B_STRIDED, GEMM_OUT_F32, GEMM_ACCUMULATE = 1, 2, 4, 8
 GEMM_GELU_FWD, GEMM_GELU_BWD = 1, 2
 PRODUCT_STAGED_SMALL, PRODUCT_STAGED_LARGE, PRODUCT_SMALL, PRODUCT_LARGE, PRODUCT_NARROW = range(5)
 PRODUCT_SLICES, PRODUCT_BROAD, PRODUCT_FLAT, PLAN_TILES = 5, 6, 7, 1 << 31
+SCAN_MARK, TOP_MAX = 256, 64
+ADAMW_GRAD_BF16, ADAMW_OUT_BF16, ADAMW_STATES_8BIT, ADAMW_BLOCK = 1, 2, 4, 64
 CONV_FWD, CONV_DGRAD, CONV_WGRAD, CONV_KEEP_SUMS = 0, 1, 2, 4
 
 
@@ -66,6 +68,21 @@ class ConvShape(C.Structure):
                 ("r", C.c_uint32), ("s", C.c_uint32), ("stride", C.c_uint32), ("pad", C.c_uint32)]
 
 
+class ScanShape(C.Structure):
+    _fields_ = [("tokens", C.c_uint64), ("channels", C.c_uint32), ("sequences", C.c_uint32), ("ld_gate", C.c_uint64), ("ld_x", C.c_uint64),
+                ("ld_h", C.c_uint64), ("ld_dgate", C.c_uint64), ("ld_dx", C.c_uint64)]
+
+
+class AdamwTensor(C.Structure):
+    _fields_ = [("w", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p), ("m_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("grad", C.c_void_p), ("out", C.c_void_p), ("n", C.c_uint64), ("weight_decay", C.c_float), ("flags", C.c_uint32)]
+
+
+class AdamwStep(C.Structure):
+    _fields_ = [("lr", C.c_float), ("beta1", C.c_float), ("beta2", C.c_float), ("eps", C.c_float), ("grad_scale", C.c_float),
+                ("seed", C.c_uint32), ("step", C.c_uint64)]
+
+
 class ProductPart(C.Structure):
     _fields_ = [("kernel", C.c_uint32), ("m", C.c_uint32), ("n", C.c_uint32), ("splits", C.c_uint32)]
 
@@ -108,6 +125,8 @@ def lib():
         _lib.karma_last_error.argtypes = [C.c_void_p]
         _lib.karma_destroy.restype = None
         _lib.karma_destroy.argtypes = [C.c_void_p]
+        _lib.karma_k_gated_scan_ws_bytes.restype = C.c_uint64
+        _lib.karma_k_token_logprob_ws_bytes.restype = C.c_uint64
     return _lib
 
 
@@ -134,6 +153,14 @@ def linear_bwd_together(rows, n, k, gelu=False, flags=0, ws_bytes=0):
     out = C.c_uint32()
     _check(lib().karma_k_linear_bwd_plan(rows, n, k, int(gelu), flags, C.c_uint64(ws_bytes), C.byref(out)), "karma_k_linear_bwd_plan")
     return bool(out.value)
+
+
+def gated_scan_ws_bytes(shape):
+    return lib().karma_k_gated_scan_ws_bytes(C.byref(shape))
+
+
+def token_logprob_ws_bytes(rows, cols, top=0):
+    return lib().karma_k_token_logprob_ws_bytes(rows, cols, top)
 
 
 def _layers_array(layers):

@@ -167,6 +167,47 @@ struct OptimTensor {
 constexpr int OPTIM_TENSORS = 16;
 int optim_update_dev(int kind, const OptimTensor* tensors, int n, float lr, float beta1, float beta2, float eps, uint64_t step, hipStream_t s);
 
+// ---- gated linear recurrence (gated_scan.hip); the strides of 0 in s become the number of channels
+struct ScanFwd {
+  const void* gate; const void* x;
+  const float* h0; const int* starts;        // may be null: zeros; sequences of one length
+  void* h; float* h_last; float* marks;      // h_last and marks may be null
+  karma_scan_shape s;
+  void* ws; size_t ws_bytes;
+};
+struct ScanBwd {
+  const void* gate; const void* x;
+  const float* h0; const int* starts; const float* marks;
+  const void* dh; const float* dh_last;      // dh_last may be null: zeros
+  void* dgate; void* dx; float* dh0;         // dh0 may be null
+  karma_scan_shape s;
+  void* ws; size_t ws_bytes;
+};
+size_t gated_scan_ws_bytes(const karma_scan_shape& s);
+int gated_scan_fwd(ScanFwd a, bool bf16, hipStream_t s);
+int gated_scan_bwd(ScanBwd a, bool bf16, hipStream_t s);
+
+// ---- log probabilities of tokens (token_logprob.hip); strides of 0 become cols
+struct LogprobFwd {
+  const void* logits; uint64_t ld; const int* tokens;
+  float* logprob; float* entropy; float* stats; float* top_logprob; int* top_id;
+  uint32_t rows, cols, top; float scale;
+  void* ws; size_t ws_bytes;
+};
+struct LogprobBwd {
+  const void* logits; uint64_t ld; const int* tokens;
+  const float* stats; const float* entropy; const float* dlogprob; const float* dentropy;
+  void* dlogits; uint64_t ld_d;
+  uint32_t rows, cols; float scale;
+};
+size_t token_logprob_ws_bytes(uint32_t rows, uint32_t cols, uint32_t top);
+int token_logprob_fwd(LogprobFwd a, bool bf16, hipStream_t s);
+int token_logprob_bwd(LogprobBwd a, bool bf16, hipStream_t s);
+
+// ---- AdamW over many tensors (adamw.hip)
+int adamw(const karma_adamw_tensor* tensors, uint32_t n, const karma_adamw_step& now, const karma_adamw_live* live, hipStream_t s);
+int adamw_states(const karma_adamw_tensor* tensors, uint32_t n, float* const* m_out, float* const* v_out, hipStream_t s);
+
 // ---- fused causal attention (attention.hip); seq multiple of 128, d in {64, 128, 152}
 int attention_fwd(const bf16_t* qkv, bf16_t* ctx, float* lse, int batch, int seq, int heads, int d, hipStream_t s);
 int attention_bwd(const bf16_t* qkv, const bf16_t* ctx, const bf16_t* dctx, const float* lse, float* delta,

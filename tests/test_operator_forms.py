@@ -1,0 +1,165 @@
+"""The plain forms of the recurrence, the log probabilities and the AdamW step: gradients against central differences, closed
+forms, and what the entry points refuse (no GPU is needed for a refusal)."""
+import ctypes as C
+
+import numpy as np
+import pytest
+
+import operator_forms as F
+import paper_2008_11421_amd as K
+
+
+def test_scan_gradients_against_differences():
+    rng = np.random.default_rng(1)
+    starts = [0, 3, 3, 9]
+    f, x, dh = (rng.standard_normal((9, 2)) for _ in range(3))
+    h0, dl = rng.standard_normal((3, 2)), rng.standard_normal((3, 2))
+
+    def loss(f, x, h0):
+        h, _, last = F.scan_forward(f, x, starts, h0)
+        return (h * dh).sum() + (last * dl).sum()
+
+    dgate, dx, dh0, _ = F.scan_backward(f, x, starts, dh, h0, dl)
+    for k, (a, got) in enumerate(((f, dgate), (x, dx), (h0, dh0))):
+        want = np.zeros_like(a)
+        for i in np.ndindex(a.shape):
+            args = [f.copy(), x.copy(), h0.copy()]
+            args[k][i] += 1e-5
+            up = loss(*args)
+            args[k][i] -= 2e-5
+            want[i] = (up - loss(*args)) / 2e-5
+        # the differences are off by h^2 / 6 times the third derivative (about 1) and 1e-16 / h
+        assert np.abs(got - want).max() < 1e-8, k
+    assert np.array_equal(dh0[1], dl[1])        # a sequence without tokens hands its gradient on
+
+
+def test_scan_closed_forms():
+    x = np.full((200, 1), 3.0)
+    f = np.full((200, 1), 2.0)
+    h, _, _ = F.scan_forward(f, x, [0, 200])
+    a = 1 / (1 + np.exp(-2.0))
+    assert np.allclose(h[:, 0], 3.0 * (1 - a ** np.arange(1, 201)), rtol=0, atol=1e-13)
+
+
+def test_logprob_gradients_against_differences():
+    rng = np.random.default_rng(2)
+    z, tokens = rng.standard_normal((4, 7)), np.array([3, -1, 0, 6])
+    z[2, 5] = -np.inf
+    dl, de = rng.standard_normal(4), rng.standard_normal(4)
+    loss = lambda z: (lambda r: (r["logprob"] * dl).sum() + (r["entropy"] * de).sum())(F.logprob_forward(z, tokens, 1.3))
+    got = F.logprob_backward(z, tokens, 1.3, dl, de)
+    for i in np.ndindex(z.shape):
+        if z[i] > -np.inf:
+            up, dn = z.copy(), z.copy()
+            up[i] += 1e-5
+            dn[i] -= 1e-5
+            assert abs(got[i] - (loss(up) - loss(dn)) / 2e-5) < 1e-8, i
+        else:
+            assert got[i] == 0
+
+
+def test_logprob_closed_forms():
+    r = F.logprob_forward(np.zeros((1, 8)), np.array([2]), 0.5, 3)
+    assert np.allclose(r["logprob"], -np.log(8)) and np.allclose(r["entropy"], np.log(8)) and r["top_id"].tolist() == [[0, 1, 2]]
+    r = F.logprob_forward(np.full((1, 4), -np.inf), np.array([2]), 1.0, 2)
+    assert r["logprob"][0] == -np.inf and r["entropy"][0] == 0 and r["top_id"].tolist() == [[0, 1]]
+
+
+def test_adamw_first_step_is_the_sign():
+    w, m, v = F.adamw(np.ones(3), np.zeros(3), np.zeros(3), np.array([2.0, -0.5, 0.0]), 0.1, 0.01, 0.9, 0.95, 1e-12, 1.0, 1)
+    assert np.allclose(w, 1 - F.f32(0.01) * F.f32(0.1) - F.f32(0.01) * np.array([1, -1, 0]), atol=1e-10)
+
+
+def test_codes_keep_the_expectation():
+    """Over 512 seeds the mean of the values that the codes stand for is the value, within six deviations of the mean."""
+    rng = np.random.default_rng(3)
+    m, v = rng.standard_normal(256) * 1e-3, rng.standard_normal(256) ** 2 * 1e-6
+    ms, vs = [], []
+    for seed in range(512):
+        cm, sm, cv, sv = F.quantised(m, v, 5, seed)
+        ms.append(cm * F.by_block(sm, 256))
+        vs.append(cv.astype(float) ** 2 * F.by_block(sv, 256))
+    ms, vs = np.array(ms), np.array(vs)
+    assert (np.abs(ms.mean(0) - m) <= 6 * F.by_block(sm, 256) * 0.5 / np.sqrt(512)).all()
+    step = (2 * np.sqrt(v / F.by_block(sv, 256)) + 1) * F.by_block(sv, 256)
+    far = v >= F.by_block(sv, 256)      # below one code a value is held up on purpose
+    assert far.sum() > 200 and (np.abs(vs.mean(0) - v)[far] <= 6 * (step * 0.5 / np.sqrt(512))[far]).all()
+    assert (vs > 0).all()
+
+
+# ------------------------------------------------------------------------------------------------- refusals
+P = C.c_void_p(4096)        # a pointer that no call here may follow
+
+
+def scan_fwd(shape, gate=P, x=P, h=P, starts=None, ws=P, ws_bytes=1 << 40, fn=None):
+    return (fn or K.lib().karma_k_gated_scan_fwd_bf16)(gate, x, None, starts, h, None, None, C.byref(shape) if shape else None, ws, C.c_uint64(ws_bytes), None)
+
+
+def test_scan_refusals():
+    good = dict(tokens=512, channels=8, sequences=2)
+    S = lambda **k: K.ScanShape(**{**good, **k})
+    assert scan_fwd(None) == K.E_INVAL
+    for bad in (dict(channels=0), dict(sequences=0), dict(tokens=511), dict(tokens=1 << 31), dict(ld_gate=7), dict(ld_x=4), dict(ld_h=1),
+                dict(ld_dx=7), dict(channels=1 << 31), dict(ld_gate=1 << 62)):
+        assert scan_fwd(S(**bad)) == K.E_INVAL, bad
+        assert K.gated_scan_ws_bytes(S(**bad)) == 0 or bad == dict(tokens=511), bad
+    for missing in ("gate", "x", "h"):
+        assert scan_fwd(S(), **{missing: None}) == K.E_INVAL, missing
+        assert scan_fwd(S(), **{missing: C.c_void_p(4097)}) == K.E_INVAL, missing
+        assert scan_fwd(S(), fn=K.lib().karma_k_gated_scan_fwd_f32, **{missing: C.c_void_p(4098)}) == K.E_INVAL, missing
+    args = dict(gate=P, x=P, marks=P, dh=P, dgate=P, dx=P)
+    for missing in args:
+        a = dict(args, **{missing: None})
+        assert K.lib().karma_k_gated_scan_bwd_bf16(a["gate"], a["x"], None, None, a["marks"], a["dh"], None, a["dgate"], a["dx"], None,
+                                                   C.byref(S()), P, C.c_uint64(1 << 40), None) == K.E_INVAL, missing
+
+
+def logprob_fwd(rows=4, cols=100, ld=0, top=0, scale=1.0, logits=P, tokens=P, logprob=P, entropy=None, stats=None, top_lp=None, top_id=None,
+                fn="bf16", ws=P, ws_bytes=1 << 40):
+    return getattr(K.lib(), "karma_k_token_logprob_fwd_" + fn)(logits, C.c_uint64(ld), tokens, logprob, entropy, stats, top_lp, top_id, C.c_uint32(rows),
+                                                               C.c_uint32(cols), C.c_uint32(top), C.c_float(scale), ws, C.c_uint64(ws_bytes), None)
+
+
+def logprob_bwd(rows=4, cols=100, ld=0, ld_d=0, scale=1.0, logits=P, tokens=P, stats=P, entropy=P, dl=P, de=P, out=P, fn="bf16"):
+    return getattr(K.lib(), "karma_k_token_logprob_bwd_" + fn)(logits, C.c_uint64(ld), tokens, stats, entropy, dl, de, out, C.c_uint64(ld_d),
+                                                               C.c_uint32(rows), C.c_uint32(cols), C.c_float(scale), None)
+
+
+def test_logprob_refusals():
+    for bad in (dict(cols=0), dict(ld=99), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(tokens=None),
+                dict(logprob=None), dict(top=2), dict(top=2, top_lp=P), dict(top=65, top_lp=P, top_id=P), dict(cols=3, top=4, top_lp=P, top_id=P),
+                dict(logits=None), dict(logits=C.c_void_p(4097)), dict(logits=C.c_void_p(4098), fn="f32"), dict(rows=1 << 31), dict(ld=1 << 62),
+                dict(cols=1 << 31)):
+        assert logprob_fwd(**bad) == K.E_INVAL, bad
+    for bad in (dict(cols=0), dict(ld=99), dict(ld_d=99), dict(scale=0.0), dict(tokens=None), dict(entropy=None), dict(dl=None, de=None), dict(stats=None),
+                dict(out=None), dict(out=C.c_void_p(4097)), dict(out=C.c_void_p(4098), fn="f32"), dict(logits=None)):
+        assert logprob_bwd(**bad) == K.E_INVAL, bad
+    assert logprob_fwd(rows=0, logits=None) == K.OK and logprob_bwd(rows=0, logits=None, out=None, stats=None) == K.OK
+
+
+def test_adamw_refusals():
+    now = dict(lr=1e-3, beta1=0.9, beta2=0.95, eps=1e-8, grad_scale=1.0, seed=1, step=1)
+    tensor = dict(w=4096, m=4096, v=4096, grad=4096, n=10, flags=0)
+
+    def call(now_change=None, live=None, **change):
+        t = (K.AdamwTensor * 1)(K.AdamwTensor(**{**tensor, **change}))
+        return K.lib().karma_k_adamw(t, 1, C.byref(K.AdamwStep(**{**now, **(now_change or {})})), live, None)
+
+    lib = K.lib()
+    assert lib.karma_k_adamw(None, 0, None, None, None) == K.E_INVAL
+    assert lib.karma_k_adamw(None, 1, C.byref(K.AdamwStep(**now)), None, None) == K.E_INVAL
+    assert lib.karma_k_adamw(None, 0, C.byref(K.AdamwStep(**now)), None, None) == K.OK
+    for bad in (dict(step=0), dict(beta1=1.0), dict(beta2=-0.1), dict(beta1=float("nan")), dict(eps=-1.0)):
+        assert call(bad) == K.E_INVAL, bad
+    for bad in (dict(w=None), dict(m=None), dict(v=None), dict(grad=None), dict(w=4098), dict(grad=4098), dict(grad=4097, flags=1), dict(out=4098),
+                dict(out=4097, flags=2), dict(flags=4), dict(flags=4, m_scale=4096), dict(flags=8), dict(m=4098), dict(n=1 << 50),
+                dict(flags=4, m_scale=4096, v_scale=4098)):
+        assert call(**bad) == K.E_INVAL, bad
+    assert call(live=C.c_void_p(4098)) == K.E_INVAL
+    assert call(n=0, w=None, m=None, v=None, grad=None) == K.OK
+    ptrs = (C.c_void_p * 1)(4096)
+    t = (K.AdamwTensor * 1)(K.AdamwTensor(**tensor))
+    assert lib.karma_k_adamw_states(t, 1, ptrs, ptrs, None) == K.E_INVAL            # fp32 states
+    t = (K.AdamwTensor * 1)(K.AdamwTensor(**dict(tensor, flags=4, m_scale=4096, v_scale=4096)))
+    assert lib.karma_k_adamw_states(t, 1, (C.c_void_p * 1)(None), ptrs, None) == K.E_INVAL
+    assert lib.karma_k_adamw_states(t, 1, None, ptrs, None) == K.E_INVAL
