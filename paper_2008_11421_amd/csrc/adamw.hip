@@ -20,7 +20,6 @@ namespace karma {
 namespace {
 
 constexpr int ADAMW_TENSORS = 44;       // of one launch: their descriptors travel as kernel arguments (4 KB)
-constexpr unsigned ADAMW_SPAN = 256;    // values of a workgroup
 
 struct AdamwSet {
   karma_adamw_tensor t[ADAMW_TENSORS];
@@ -30,8 +29,8 @@ struct AdamwSet {
 };
 struct AdamwNow {
   float lr, beta1, beta2, eps, grad_scale;
+  float c1, k2;                         // not with live
   unsigned seed;
-  unsigned long long step;
   const karma_adamw_live* live;
 };
 static_assert(sizeof(AdamwSet) + sizeof(AdamwNow) <= 4096, "kernel arguments");
@@ -43,6 +42,10 @@ __host__ __device__ inline double one_minus_power(float beta, unsigned long long
     if (step & 1) p *= b;
   return 1.0 - p;
 }
+__host__ __device__ inline void corrections(AdamwNow& a, unsigned long long step) {
+  a.c1 = (float)(1.0 / one_minus_power(a.beta1, step));
+  a.k2 = (float)(1.0 / sqrt(one_minus_power(a.beta2, step)));
+}
 
 __device__ __forceinline__ unsigned random_bits(unsigned long long i, unsigned key) {
   unsigned x = (unsigned)i + key;
@@ -51,62 +54,171 @@ __device__ __forceinline__ unsigned random_bits(unsigned long long i, unsigned k
   return x ^ (x >> 16);
 }
 
-__device__ __forceinline__ float max64(float v) {
-  for (int k = 32; k > 0; k >>= 1) {
-    const float o = __shfl_xor(v, k);
-    v = v != v ? v : (o != o ? o : fmaxf(v, o));    // NaN wins
-  }
-  return v;
+// The largest of 16 lanes' values, none of which is negative: as whole numbers they have the same order, and NaN is the largest.
+__device__ __forceinline__ float max16(float v) {
+  unsigned x = __float_as_uint(v);
+#define KARMA_MAX_STEP(CTRL) x = max(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, false))
+  KARMA_MAX_STEP(0xB1);     // quad_perm [1,0,3,2]
+  KARMA_MAX_STEP(0x4E);     // quad_perm [2,3,0,1]
+  KARMA_MAX_STEP(0x141);    // row_half_mirror
+  KARMA_MAX_STEP(0x140);    // row_mirror
+#undef KARMA_MAX_STEP
+  return __uint_as_float(x);
 }
 
-__global__ __launch_bounds__(ADAMW_SPAN) void adamw_kernel(AdamwSet u, AdamwNow a) {
-  int k = 0;
-  while (k + 1 < u.n && blockIdx.x >= u.first[k + 1]) ++k;
-  const karma_adamw_tensor& p = u.t[k];
-  if (a.live) { a.lr = a.live->lr; a.grad_scale = a.live->grad_scale; a.step = a.live->step ? a.live->step : 1; a.seed = a.live->seed; }
-  const float c1 = (float)(1.0 / one_minus_power(a.beta1, a.step)), k2 = (float)(1.0 / sqrt(one_minus_power(a.beta2, a.step)));
-  const size_t i = (size_t)(blockIdx.x - u.first[k]) * ADAMW_SPAN + threadIdx.x;
-  const bool live = i < p.n, eight = p.flags & KARMA_ADAMW_STATES_8BIT;
-  if (!live && !eight) return;
-  const float g = !live ? 0.f : (p.flags & KARMA_ADAMW_GRAD_BF16) ? bf2f(((const bf16_t*)p.grad)[i]) : ((const float*)p.grad)[i];
-  float m, v;
-  if (!eight) {
-    const float gs = g * a.grad_scale;
-    m = a.beta1 * ((float*)p.m)[i] + (float)(1.0 - (double)a.beta1) * gs;
-    v = a.beta2 * ((float*)p.v)[i] + (float)(1.0 - (double)a.beta2) * gs * gs;
-    ((float*)p.m)[i] = m;
-    ((float*)p.v)[i] = v;
-  } else {
-#pragma clang fp contract(off)
-    const size_t block = i / 64;
-    const bool some = block * 64 < p.n;     // the wavefront has a block: block's scales exist
-    const int qm = live ? ((const int8_t*)p.m)[i] : 0, qv = live ? ((const uint8_t*)p.v)[i] : 0;
-    const double gs = (double)g * (double)a.grad_scale;
-    const double md = a.beta1 * (qm * (double)(some ? p.m_scale[block] : 0.f)) + (1.0 - (double)a.beta1) * gs;
-    const double vd = a.beta2 * ((double)(qv * qv) * (some ? p.v_scale[block] : 0.f)) + (1.0 - (double)a.beta2) * gs * gs;
-    m = (float)md;
-    v = (float)vd;
-    float sm = max64(live ? fabsf(m) : 0.f) * (float)(1.0 / 127), sv = max64(live ? v : 0.f) * (float)(1.0 / 65025);
-    if (!(sm <= 3.4e38f) || !(sv <= 3.4e38f)) sm = sv = NAN;    // a gradient that is not finite: the block's states are lost, and say so
-    int cm = 0, cv = 0;
-    const unsigned x = random_bits(i, u.key[k] + a.seed * 0x9e3779b1u);
-    if (sm > 0.f) cm = min(127, max(-127, (int)floor(md / sm + ((x & 0xffff) + 0.5) / 65536)));
-    if (sv > 0.f) {
-      const double z = vd / sv, q = fmin(255.0, floor(sqrt(z)));
-      cv = min(255, (int)q + (z - q * q > ((x >> 16) + 0.5) / 65536 * (2 * q + 1)));
-      if (cv == 0 && z > 0) cv = 1;
-    }
-    if (some && threadIdx.x % 64 == 0) { p.m_scale[block] = sm; p.v_scale[block] = sv; }
-    if (!live) return;
-    ((int8_t*)p.m)[i] = (int8_t)cm;
-    ((uint8_t*)p.v)[i] = (uint8_t)cv;
+// Four consecutive values of a buffer: at once where `whole` (all four exist and the buffer is aligned), else one by one.
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+__device__ __forceinline__ f32x4 load4(const float* p, size_t i, size_t n, bool whole) {
+  if (whole) return *(const f32x4*)(p + i);
+  f32x4 r;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) r[e] = i + e < n ? p[i + e] : 0.f;
+  return r;
+}
+__device__ __forceinline__ f32x4 load4(const bf16_t* p, size_t i, size_t n, bool whole) {
+  f32x4 r;
+  if (whole) {
+    const u32x2 v = *(const u32x2*)(p + i);
+    return f32x4{__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u), __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u)};
   }
-  float w = p.w[i];
-  w = w - a.lr * p.weight_decay * w - a.lr * (c1 * m / (sqrtf(v) * k2 + a.eps));
-  p.w[i] = w;
-  if (p.out) {
-    if (p.flags & KARMA_ADAMW_OUT_BF16) ((bf16_t*)p.out)[i] = f2bf(w);
-    else ((float*)p.out)[i] = w;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) r[e] = i + e < n ? bf2f(p[i + e]) : 0.f;
+  return r;
+}
+__device__ __forceinline__ unsigned load4(const uint8_t* p, size_t i, size_t n, bool whole) {
+  if (whole) return *(const unsigned*)(p + i);
+  unsigned r = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) r |= i + e < n ? (unsigned)p[i + e] << (8 * e) : 0u;
+  return r;
+}
+__device__ __forceinline__ void store4(float* p, size_t i, size_t n, bool whole, const f32x4& v) {
+  if (whole) { *(f32x4*)(p + i) = v; return; }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) if (i + e < n) p[i + e] = v[e];
+}
+__device__ __forceinline__ void store4(bf16_t* p, size_t i, size_t n, bool whole, const f32x4& v) {
+  if (whole) { *(u32x2*)(p + i) = u32x2{pack2(v[0], v[1]), pack2(v[2], v[3])}; return; }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) if (i + e < n) p[i + e] = f2bf(v[e]);
+}
+__device__ __forceinline__ void store4(uint8_t* p, size_t i, size_t n, bool whole, unsigned v) {
+  if (whole) { *(unsigned*)(p + i) = v; return; }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) if (i + e < n) p[i + e] = (uint8_t)(v >> (8 * e));
+}
+
+// Four values' moments in 8 bits: old codes and scales in, new ones out; mo and vo, the moments in fp32 before they are rounded.
+// In 64 bits: which of two codes a value gets does not hang on the order of the operations.  Sixteen lanes have a block.
+struct Codes { unsigned m, v; float sm, sv; };
+__device__ __forceinline__ Codes quantised_step(const Codes& c, const f32x4& g, const AdamwNow& a, unsigned key, size_t i, f32x4& mo, f32x4& vo) {
+  const double b1 = (double)a.beta1 * c.sm, b2 = (double)a.beta2 * c.sv, d1 = 1.0 - (double)a.beta1, d2 = 1.0 - (double)a.beta2;
+  double m[4], v[4];
+  float tm = 0.f, tv = 0.f;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int qm = (int)(c.m << (24 - 8 * e)) >> 24, qv = (c.v >> (8 * e)) & 0xff;
+    const double gs = (double)g[e] * (double)a.grad_scale;
+    m[e] = fma((double)qm, b1, d1 * gs);
+    v[e] = fma((double)(qv * qv), b2, d2 * gs * gs);
+    mo[e] = (float)m[e];
+    vo[e] = (float)v[e];
+    // (as whole numbers: NaN is kept)
+    tm = __uint_as_float(max(__float_as_uint(tm), __float_as_uint(fabsf(mo[e]))));
+    tv = __uint_as_float(max(__float_as_uint(tv), __float_as_uint(vo[e])));
+  }
+  Codes r;
+  r.sm = max16(tm) * (float)(1.0 / 127);
+  r.sv = max16(tv) * (float)(1.0 / 65025);
+  // a gradient that is not finite: the block's moments are lost, and say so
+  if (!(r.sm < INFINITY) || !(r.sv < INFINITY)) r.sm = r.sv = NAN;
+  const double im = r.sm > 0.f ? 1.0 / (double)r.sm : 0.0, iv = r.sv > 0.f ? 1.0 / (double)r.sv : 0.0;    // NaN: codes 0
+  r.m = r.v = 0;
+  if (r.sm != r.sm) return r;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const unsigned x = random_bits(i + e, key);
+    const float um = ((x & 0xffff) + 0.5f) * (1.f / 65536), uv = ((x >> 16) + 0.5f) * (1.f / 65536);    // exact
+    const int cm = min(127, max(-127, (int)floor(m[e] * im + um)));
+    const double z = v[e] * iv;
+    float q = floorf(sqrtf((float)z));
+    double rest = z - (double)(q * q);
+    // the root of z rounded to 32 bits may be a border too far, or one short of it
+    if (rest < 0.0) { q -= 1.f; rest += 2.f * q + 1.f; }
+    else if (rest >= 2.f * q + 1.f) { rest -= 2.f * q + 1.f; q += 1.f; }
+    int cv = (int)q + (rest > (double)uv * (2.f * q + 1.f) ? 1 : 0);
+    cv = min(255, z > 0.0 ? max(1, cv) : cv);
+    r.m |= (unsigned)(cm & 0xff) << (8 * e);
+    r.v |= (unsigned)cv << (8 * e);
+  }
+  return r;
+}
+
+// A workgroup has ITER * 1024 consecutive values, a lane four of each 1024: 16-byte accesses of the fp32 buffers.  Reads and
+// writes 28 bytes a value (bf16 gradient and weight), 16.25 with 8-bit moments: bound by memory.
+template <bool EIGHT, int ITER>
+__global__ __launch_bounds__(256) void adamw_kernel(AdamwSet u, AdamwNow a) {
+  int lo = 0, hi = u.n - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) / 2;
+    if (blockIdx.x >= u.first[mid]) lo = mid;
+    else hi = mid - 1;
+  }
+  const karma_adamw_tensor p = u.t[lo];
+  if (a.live) {
+    a.lr = a.live->lr; a.grad_scale = a.live->grad_scale; a.seed = a.live->seed;
+    corrections(a, a.live->step ? a.live->step : 1);
+  }
+  const unsigned key = u.key[lo] + a.seed * 0x9e3779b1u;
+  const bool gbf = p.flags & KARMA_ADAMW_GRAD_BF16, obf = p.flags & KARMA_ADAMW_OUT_BF16;
+  const uintptr_t odd = (uintptr_t)p.w | (EIGHT ? ((uintptr_t)p.m | (uintptr_t)p.v) * 4 : (uintptr_t)p.m | (uintptr_t)p.v) |
+                        (uintptr_t)p.grad * (gbf ? 2 : 1) | (uintptr_t)p.out * (obf ? 2 : 1);
+  const bool vec = odd % 16 == 0;
+  const size_t at = (size_t)(blockIdx.x - u.first[lo]) * (ITER * 1024) + threadIdx.x * 4;
+  f32x4 g[ITER], w[ITER], m[ITER], v[ITER];
+  Codes c[ITER];
+#pragma unroll
+  for (int k = 0; k < ITER; ++k) {
+    const size_t i = at + k * 1024;
+    const bool whole = vec && i + 4 <= p.n;
+    g[k] = gbf ? load4((const bf16_t*)p.grad, i, p.n, whole) : load4((const float*)p.grad, i, p.n, whole);
+    w[k] = load4(p.w, i, p.n, whole);
+    if (EIGHT) {
+      const bool some = i / 64 * 64 < p.n;
+      c[k] = Codes{load4((const uint8_t*)p.m, i, p.n, whole), load4((const uint8_t*)p.v, i, p.n, whole), some ? p.m_scale[i / 64] : 0.f,
+                   some ? p.v_scale[i / 64] : 0.f};
+    } else {
+      m[k] = load4((const float*)p.m, i, p.n, whole);
+      v[k] = load4((const float*)p.v, i, p.n, whole);
+    }
+  }
+  const float d1 = (float)(1.0 - (double)a.beta1), d2 = (float)(1.0 - (double)a.beta2), keep = 1.f - a.lr * p.weight_decay;
+#pragma unroll
+  for (int k = 0; k < ITER; ++k) {
+    const size_t i = at + k * 1024;
+    const bool whole = vec && i + 4 <= p.n;
+    if (EIGHT) {
+      const Codes r = quantised_step(c[k], g[k], a, key, i, m[k], v[k]);
+      store4((uint8_t*)p.m, i, p.n, whole, r.m);
+      store4((uint8_t*)p.v, i, p.n, whole, r.v);
+      if (threadIdx.x % 16 == 0 && i < p.n) { p.m_scale[i / 64] = r.sm; p.v_scale[i / 64] = r.sv; }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float gs = g[k][e] * a.grad_scale;
+        m[k][e] = a.beta1 * m[k][e] + d1 * gs;
+        v[k][e] = a.beta2 * v[k][e] + d2 * gs * gs;
+      }
+      store4((float*)p.m, i, p.n, whole, m[k]);
+      store4((float*)p.v, i, p.n, whole, v[k]);
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[k][e] = keep * w[k][e] - a.lr * (a.c1 * m[k][e] / (sqrtf(v[k][e]) * a.k2 + a.eps));
+    store4(p.w, i, p.n, whole, w[k]);
+    if (p.out) {
+      if (obf) store4((bf16_t*)p.out, i, p.n, whole, w[k]);
+      else store4((float*)p.out, i, p.n, whole, w[k]);
+    }
   }
 }
 
@@ -120,14 +232,34 @@ struct StatesSet {
   int n;
 };
 static_assert(sizeof(StatesSet) <= 4096, "kernel arguments");
-__global__ __launch_bounds__(ADAMW_SPAN) void adamw_states_kernel(StatesSet u) {
-  int k = 0;
-  while (k + 1 < u.n && blockIdx.x >= u.first[k + 1]) ++k;
-  const size_t i = (size_t)(blockIdx.x - u.first[k]) * ADAMW_SPAN + threadIdx.x;
-  if (i >= u.size[k]) return;
-  const float q = u.v[k][i];
-  u.m_out[k][i] = u.m[k][i] * u.m_scale[k][i / 64];
-  u.v_out[k][i] = q * q * u.v_scale[k][i / 64];
+constexpr unsigned STATES_SPAN = 4096;
+// four values a lane; 2.1 bytes in, 8 out
+__global__ __launch_bounds__(256) void adamw_states_kernel(StatesSet u) {
+  int lo = 0, hi = u.n - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) / 2;
+    if (blockIdx.x >= u.first[mid]) lo = mid;
+    else hi = mid - 1;
+  }
+  const size_t n = u.size[lo];
+  const uintptr_t odd = ((uintptr_t)u.m[lo] | (uintptr_t)u.v[lo]) * 4 | (uintptr_t)u.m_out[lo] | (uintptr_t)u.v_out[lo];
+#pragma unroll
+  for (int k = 0; k < STATES_SPAN / 1024; ++k) {
+    const size_t i = (size_t)(blockIdx.x - u.first[lo]) * STATES_SPAN + k * 1024 + threadIdx.x * 4;
+    if (i >= n) return;
+    const bool whole = odd % 16 == 0 && i + 4 <= n;
+    const unsigned cm = load4((const uint8_t*)u.m[lo], i, n, whole), cv = load4(u.v[lo], i, n, whole);
+    const float sm = u.m_scale[lo][i / 64], sv = u.v_scale[lo][i / 64];
+    f32x4 m, v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int q = (cv >> (8 * e)) & 0xff;
+      m[e] = (float)((int)(cm << (24 - 8 * e)) >> 24) * sm;
+      v[e] = (float)(q * q) * sv;
+    }
+    store4(u.m_out[lo], i, n, whole, m);
+    store4(u.v_out[lo], i, n, whole, v);
+  }
 }
 
 bool aligned_to(const void* p, size_t n) { return (uintptr_t)p % n == 0; }
@@ -151,26 +283,33 @@ int adamw(const karma_adamw_tensor* tensors, uint32_t n, const karma_adamw_step&
     if (t.n && (!t.w || !t.grad || !aligned_to(t.w, 4) || !aligned_to(t.grad, t.flags & KARMA_ADAMW_GRAD_BF16 ? 2 : 4) ||
                 !aligned_to(t.out, t.flags & KARMA_ADAMW_OUT_BF16 ? 2 : 4))) return KARMA_E_INVAL;
   }
+  AdamwNow a{now.lr, now.beta1, now.beta2, now.eps, now.grad_scale, 0.f, 0.f, now.seed, live};
+  if (!live) corrections(a, now.step);
+  uint64_t total = 0;
+  for (uint32_t k = 0; k < n; ++k) total += tensors[k].n;
+  // four groups of 1024 values a workgroup, one where the chip would not be full of those
+  const unsigned span = total >= (uint64_t)compute_units() * 4 * 4096 ? 4096 : 1024;
   bool launched = false;
-  const AdamwNow a{now.lr, now.beta1, now.beta2, now.eps, now.grad_scale, now.seed, now.step, live};
-  for (uint32_t k = 0; k < n;) {
-    AdamwSet u;
-    u.n = 0;
-    u.first[0] = 0;
-    uint64_t blocks = 0;
-    for (; k < n && u.n < ADAMW_TENSORS; ++k) {
-      if (!tensors[k].n) continue;
-      const uint64_t more = (tensors[k].n + ADAMW_SPAN - 1) / ADAMW_SPAN;
-      if (more > INT32_MAX) return KARMA_E_INVAL;
-      if (blocks + more > INT32_MAX) break;
-      blocks += more;
-      u.t[u.n] = tensors[k];
-      u.key[u.n] = (k + 1) * 0x7f4a7c15u;
-      u.first[++u.n] = (unsigned)blocks;
+  for (int eight = 0; eight < 2; ++eight) {
+    for (uint32_t k = 0; k < n;) {
+      AdamwSet u;
+      u.n = 0;
+      u.first[0] = 0;
+      uint64_t blocks = 0;
+      for (; k < n && u.n < ADAMW_TENSORS; ++k) {
+        if (!tensors[k].n || eight_bits(tensors[k]) != (eight != 0)) continue;
+        const uint64_t more = (tensors[k].n + span - 1) / span;
+        if (blocks + more > INT32_MAX) break;
+        blocks += more;
+        u.t[u.n] = tensors[k];
+        u.key[u.n] = (k + 1) * 0x7f4a7c15u;
+        u.first[++u.n] = (unsigned)blocks;
+      }
+      if (!u.n) continue;
+      auto* kernel = eight ? (span == 4096 ? adamw_kernel<true, 4> : adamw_kernel<true, 1>) : (span == 4096 ? adamw_kernel<false, 4> : adamw_kernel<false, 1>);
+      hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, s, u, a);
+      launched = true;
     }
-    if (!u.n) continue;
-    hipLaunchKernelGGL(adamw_kernel, dim3((unsigned)blocks), dim3(ADAMW_SPAN), 0, s, u, a);
-    launched = true;
   }
   return !launched || hipGetLastError() == hipSuccess ? KARMA_OK : KARMA_E_HIP;
 }
@@ -190,8 +329,7 @@ int adamw_states(const karma_adamw_tensor* tensors, uint32_t n, float* const* m_
     for (; k < n && u.n < ADAMW_TENSORS; ++k) {
       const karma_adamw_tensor& t = tensors[k];
       if (!t.n) continue;
-      const uint64_t more = (t.n + ADAMW_SPAN - 1) / ADAMW_SPAN;
-      if (more > INT32_MAX) return KARMA_E_INVAL;
+      const uint64_t more = (t.n + STATES_SPAN - 1) / STATES_SPAN;
       if (blocks + more > INT32_MAX) break;
       blocks += more;
       u.m[u.n] = (const int8_t*)t.m; u.v[u.n] = (const uint8_t*)t.v; u.m_scale[u.n] = t.m_scale; u.v_scale[u.n] = t.v_scale;
@@ -199,7 +337,7 @@ int adamw_states(const karma_adamw_tensor* tensors, uint32_t n, float* const* m_
       u.first[++u.n] = (unsigned)blocks;
     }
     if (!u.n) continue;
-    hipLaunchKernelGGL(adamw_states_kernel, dim3((unsigned)blocks), dim3(ADAMW_SPAN), 0, s, u);
+    hipLaunchKernelGGL(adamw_states_kernel, dim3((unsigned)blocks), dim3(256), 0, s, u);
     launched = true;
   }
   return !launched || hipGetLastError() == hipSuccess ? KARMA_OK : KARMA_E_HIP;

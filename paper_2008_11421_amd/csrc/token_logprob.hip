@@ -6,6 +6,7 @@
 // good as any other, where c z would overflow.  All sums are fp32.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "device_utils.h"
@@ -15,119 +16,348 @@
 namespace karma {
 namespace {
 
-constexpr int LP_THREADS = 256;
-
+// ---- rows in 16-byte vectors --------------------------------------------------------------------------------
 template <typename T>
-__device__ __forceinline__ float load1(const T* p);
+struct Vec;
 template <>
-__device__ __forceinline__ float load1<bf16_t>(const bf16_t* p) { return bf2f(*p); }
+struct Vec<bf16_t> {
+  static constexpr int N = 8;
+  static __device__ __forceinline__ void store(bf16_t* p, const float* f) { *(u32x4*)p = pack8(f); }
+  static __device__ __forceinline__ float one(const bf16_t* p) { return bf2f(*p); }
+  static __device__ __forceinline__ void put(bf16_t* p, float v) { *p = f2bf(v); }
+  static __device__ __forceinline__ void unpack(const u32x4& v, float* f) { unpack8(v, f); }
+};
 template <>
-__device__ __forceinline__ float load1<float>(const float* p) { return *p; }
-__device__ __forceinline__ void store1(bf16_t* p, float v) { *p = f2bf(v); }
-__device__ __forceinline__ void store1(float* p, float v) { *p = v; }
+struct Vec<float> {
+  static constexpr int N = 4;
+  static __device__ __forceinline__ void store(float* p, const float* f) {
+    *(u32x4*)p = u32x4{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])};
+  }
+  static __device__ __forceinline__ float one(const float* p) { return *p; }
+  static __device__ __forceinline__ void put(float* p, float v) { *p = v; }
+  static __device__ __forceinline__ void unpack(const u32x4& v, float* f) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f[e] = __uint_as_float(v[e]);
+  }
+};
+// Rows may begin anywhere (a vocabulary of odd size): `head` elements before the first 16-byte boundary and `tail` behind the
+// last are taken one by one.
+template <typename T>
+struct Row {
+  const T* at;
+  unsigned head, vectors, tail;
+  __device__ __forceinline__ Row(const T* z, unsigned cols) : at(z) {
+    head = min((unsigned)((16 - (uintptr_t)z % 16) % 16 / sizeof(T)), cols);
+    vectors = (cols - head) / Vec<T>::N;
+    tail = cols - head - vectors * Vec<T>::N;
+  }
+};
 
-// largest, sum and first moment of a part of a row; empty: {-inf, 0, 0}
-struct RowPart { float m, s, t; };
-__device__ __forceinline__ RowPart join(const RowPart& a, const RowPart& b, float scale) {
-  RowPart r;
-  r.m = fmaxf(a.m, b.m);
-  if (r.m == -INFINITY) return RowPart{r.m, a.s + b.s, a.t + b.t};   // nothing allowed so far (or NaN alone, which the sums carry)
-  // a part whose largest is -inf has sums of zero; its difference must not make -inf * 0
-  const float da = fmaxf(a.m - r.m, -1e30f), db = fmaxf(b.m - r.m, -1e30f);
-  const float ea = expf(da * scale), eb = expf(db * scale);
-  r.s = a.s * ea + b.s * eb;
-  r.t = (a.t + (ea ? da * a.s : 0.f)) * ea + (b.t + (eb ? db * b.s : 0.f)) * eb;
+// ---- maximum, sum and first moment of what has been seen --------------------------------------------------------
+// m: the largest; s = sum of 2^(c2 (z - m)), t = sum of (z - m) 2^(c2 (z - m)).  Nothing seen: m the lowest finite value and s = 0,
+// which no logit that is allowed leaves (the largest adds 1).  NaN comes through the exponential into s.
+struct Running { float m, s, t; };
+__device__ __forceinline__ Running nothing_seen() { return Running{-3.402823466e38f, 0.f, 0.f}; }
+__device__ __forceinline__ void raise(Running& r, float m, float c2) {
+  const float d = fmaxf(r.m - m, -1e30f), k = __builtin_amdgcn_exp2f(d * c2);   // (bounded: -inf times an s of 0)
+  r.t = (r.t + d * r.s) * k;
+  r.s *= k;
+  r.m = m;
+}
+template <int N>
+__device__ __forceinline__ float max_of(const float (&f)[N]) {
+  float m = f[0];
+#pragma unroll
+  for (int e = 1; e < N; ++e) m = fmaxf(m, f[e]);
+  return m;
+}
+template <int N>
+__device__ __forceinline__ void take(Running& r, const float (&f)[N], float most, float c2) {
+  if (most > r.m) raise(r, most, c2);
+#pragma unroll
+  for (int e = 0; e < N; ++e) {
+    const float d = f[e] - r.m, x = __builtin_amdgcn_exp2f(d * c2);
+    r.s += x;
+    r.t = fmaf(x, fmaxf(d, -1e30f), r.t);   // (bounded: -inf times a probability of 0)
+  }
+}
+__device__ __forceinline__ Running join(Running a, Running b, float c2) {
+  const float m = fmaxf(a.m, b.m);
+  raise(a, m, c2);
+  raise(b, m, c2);
+  return Running{m, a.s + b.s, a.t + b.t};
+}
+__device__ __forceinline__ Running wave_join(Running r, float c2) {
+#pragma unroll
+  for (int k = 32; k > 0; k >>= 1) r = join(r, Running{__shfl_xor(r.m, k), __shfl_xor(r.s, k), __shfl_xor(r.t, k)}, c2);
   return r;
 }
 
-template <typename T>
-__global__ __launch_bounds__(LP_THREADS) void logprob_fwd_kernel(LogprobFwd a) {
-  __shared__ RowPart part[LP_THREADS];
-  __shared__ float best_v[LP_THREADS];
-  __shared__ int best_i[LP_THREADS];
-  const int tid = threadIdx.x;
-  const size_t r = blockIdx.x;
-  const T* z = (const T*)a.logits + r * a.ld;
-  RowPart p{-INFINITY, 0.f, 0.f};
-  for (unsigned j = tid; j < a.cols; j += LP_THREADS) {
-    const float v = load1(z + j);
-    if (v > p.m) {
-      const float d = fmaxf(p.m - v, -1e30f), e = expf(d * a.scale);
-      p.t = (p.t + (e ? d * p.s : 0.f)) * e;
-      p.s *= e;
-      p.m = v;
+// ---- the best alternatives -------------------------------------------------------------------------------------
+// A wavefront keeps the best so far in order, lane i the i-th, as 64-bit keys: the value's bits in an order of whole numbers, then
+// the inverted index, so that equal values are in ascending order.  0: none.  Most elements fall to one comparison of a vector's
+// largest with the last one's value; one that does not is inserted: its place is the number of lanes that are better, and the
+// lanes behind that move up by one.
+__device__ __forceinline__ uint64_t order_key(float v, unsigned i) {
+  unsigned u = __float_as_uint(v);
+  if (u == 0x80000000u) u = 0;      // -0 equals 0
+  u = u & 0x80000000u ? ~u : u | 0x80000000u;
+  return (uint64_t)u << 32 | (0xffffffffu - i);
+}
+__device__ __forceinline__ float key_value(uint64_t k) {
+  const unsigned u = (unsigned)(k >> 32);
+  return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u);
+}
+__device__ __forceinline__ int key_index(uint64_t k) { return (int)(0xffffffffu - (unsigned)k); }
+__device__ __forceinline__ uint64_t lane_key(uint64_t k, int lane) {
+  return (uint64_t)(unsigned)__builtin_amdgcn_readlane((int)(k >> 32), lane) << 32 | (unsigned)__builtin_amdgcn_readlane((int)k, lane);
+}
+
+struct Best {
+  uint64_t key;       // this lane's
+  uint64_t last;      // of lane top - 1 (the same in all lanes, as the following)
+  float floor;        // values below it need not be looked at
+  int top;
+  __device__ __forceinline__ explicit Best(int top_) : key(0), last(0), floor(-INFINITY), top(top_) {}
+  __device__ __forceinline__ void insert(uint64_t k) {      // k: the same in all lanes, not 0
+    if (k <= last) return;
+    const int place = __popcll(__ballot(key > k));
+    const int hi = __builtin_amdgcn_update_dpp(0, (int)(key >> 32), 0x138, 0xf, 0xf, false);   // wave_shr:1
+    const int lo = __builtin_amdgcn_update_dpp(0, (int)key, 0x138, 0xf, 0xf, false);
+    const int lane = threadIdx.x & 63;
+    if (lane > place) key = (uint64_t)(unsigned)hi << 32 | (unsigned)lo;
+    if (lane == place) key = k;
+    last = lane_key(key, top - 1);
+    if (last) floor = fmaxf(floor, key_value(last));
+  }
+  // the elements of a vector, the e-th of lane l being column base + e
+  template <int N>
+  __device__ __forceinline__ void look(const float (&f)[N], float most, unsigned base) {
+    if (!__ballot(most >= floor)) return;
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      uint64_t mask = __ballot(f[e] >= floor);      // NaN is none
+      while (mask) {
+        const int l = __builtin_ctzll(mask);
+        mask &= mask - 1;
+        const float v = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f[e]), l));
+        insert(order_key(v, (unsigned)__builtin_amdgcn_readlane((int)base, l) + e));
+      }
     }
-    const float d = v == -INFINITY ? -INFINITY : v - p.m, e = expf(d * a.scale);
-    p.s += e;
-    p.t += e == 0.f ? 0.f : d * e;
   }
-  part[tid] = p;
-  __syncthreads();
-  for (int k = LP_THREADS / 2; k > 0; k >>= 1) {
-    if (tid < k) part[tid] = join(part[tid], part[tid + k], a.scale);
-    __syncthreads();
+  // A floor to begin with: the largest of each lane's first elements are 64 different elements, so `top` of them are not below the
+  // top-th largest.  Found to 16 bits, from below.
+  __device__ __forceinline__ void begin(float most) {
+    unsigned u = __float_as_uint(most);
+    u = most != most ? 0u : u & 0x80000000u ? ~u : u | 0x80000000u;
+    unsigned at = 0;
+#pragma unroll
+    for (unsigned bit = 0x80000000u; bit >= 0x10000u; bit >>= 1)
+      if (__popcll(__ballot(u >= (at | bit))) >= top) at |= bit;
+    // (at may lie among the patterns below -inf, of NaN: then there is no floor)
+    const float v = __uint_as_float(at & 0x80000000u ? at & 0x7fffffffu : ~at);
+    floor = v == v ? v : -INFINITY;
   }
-  p = part[0];
-  const float ls = p.m == -INFINITY && p.s == 0.f ? 0.f : logf(p.s);
-  auto log_p = [&](float v) { return v == -INFINITY && p.s == p.s ? v : (v - p.m) * a.scale - ls; };
-  if (tid == 0) {
-    if (a.stats) { a.stats[2 * r] = p.m; a.stats[2 * r + 1] = ls; }
-    if (a.entropy) a.entropy[r] = p.m == -INFINITY && p.s == 0.f ? 0.f : ls - a.scale * p.t / p.s;
+  __device__ __forceinline__ void add(uint64_t others) {       // another list of `top` keys in order, lane i the i-th
+    for (int i = 0; i < top; ++i) {
+      const uint64_t k = lane_key(others, i);
+      if (k <= last) break;
+      insert(k);
+    }
+  }
+};
+
+// ---- forward -------------------------------------------------------------------------------------------------
+constexpr int LP_THREADS = 256, LP_WAVES = LP_THREADS / 64;
+constexpr int LP_BATCH = 4;     // vectors a lane has under way
+
+struct LogprobPart { float m, s, t, unused; };
+
+template <typename T>
+__device__ __forceinline__ void finish_row(const LogprobFwd& a, size_t r, Running w, const Best& best) {
+  const int lane = threadIdx.x & 63;
+  const bool empty = w.s == 0.f;
+  if (empty) { w.m = -INFINITY; w.s = 1.f; w.t = 0.f; }
+  const float ls = logf(w.s);
+  auto log_p = [&](float v) { return empty ? -INFINITY : (v - w.m) * a.scale - ls; };
+  if (lane == 0) {
+    if (a.stats) { a.stats[2 * r] = w.m; a.stats[2 * r + 1] = ls; }
+    if (a.entropy) a.entropy[r] = ls - a.scale * w.t / w.s;
     if (a.logprob) {
       const int t = a.tokens[r];
-      a.logprob[r] = t >= 0 && (unsigned)t < a.cols ? log_p(load1(z + t)) : 0.f;
+      a.logprob[r] = t >= 0 && (unsigned)t < a.cols ? log_p(Vec<T>::one((const T*)a.logits + r * a.ld + t)) : 0.f;
     }
   }
-  // the k best, one after the other: the best among those behind the last one taken
-  float lv = INFINITY;
-  int li = -1;
-  for (unsigned k = 0; k < a.top; ++k) {
-    float bv = -INFINITY;
-    int bi = INT32_MAX;
-    for (unsigned j = tid; j < a.cols; j += LP_THREADS) {
-      const float v = load1(z + j);
-      if ((v < lv || (v == lv && (int)j > li)) && (v > bv || (v == bv && (int)j < bi))) { bv = v; bi = (int)j; }
-    }
-    best_v[tid] = bv;
-    best_i[tid] = bi;
-    __syncthreads();
-    for (int n = LP_THREADS / 2; n > 0; n >>= 1) {
-      if (tid < n && (best_v[tid + n] > best_v[tid] || (best_v[tid + n] == best_v[tid] && best_i[tid + n] < best_i[tid]))) {
-        best_v[tid] = best_v[tid + n];
-        best_i[tid] = best_i[tid + n];
+  if (lane < (int)a.top) {
+    a.top_id[r * a.top + lane] = best.key ? key_index(best.key) : -1;
+    a.top_logprob[r * a.top + lane] = best.key ? log_p(key_value(best.key)) : NAN;
+  }
+}
+
+// W wavefronts share a part of a row (`parts` parts a row, W = 1: the whole row), lanes side by side on vectors.  One pass: every
+// vector goes into the running sums and past the list of alternatives.
+template <typename T, int W, bool TOP>
+__global__ __launch_bounds__(LP_THREADS) void logprob_fwd_kernel(LogprobFwd a, unsigned parts, LogprobPart* sums, uint64_t* lists) {
+  constexpr int N = Vec<T>::N;
+  __shared__ Running wave_sums[LP_WAVES];
+  __shared__ uint64_t wave_best[TOP ? LP_WAVES : 1][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const unsigned unit = blockIdx.x * (LP_WAVES / W) + wave / W;    // a row's part
+  const unsigned r = unit / parts, part = unit % parts, w = wave % W;
+  const float c2 = a.scale * 1.44269504f;
+  Running run = nothing_seen();
+  Best best(TOP ? (int)a.top : 1);
+  if (r < a.rows) {
+    const Row<T> row((const T*)a.logits + (size_t)r * a.ld, a.cols);
+    const unsigned per = (row.vectors + parts - 1) / parts, v0 = min(row.vectors, part * per), v1 = min(row.vectors, v0 + per);
+    const T* body = row.at + row.head;
+    bool first = true;
+    for (unsigned v = v0 + w * 64; v < v1; v += LP_BATCH * W * 64) {
+      u32x4 raw[LP_BATCH];
+      float f[N], most[LP_BATCH];
+#pragma unroll
+      for (int k = 0; k < LP_BATCH; ++k) {
+        const unsigned i = v + k * W * 64 + lane;
+        if (i < v1) raw[k] = *(const u32x4*)(body + (size_t)i * N);
       }
-      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < LP_BATCH; ++k) {
+        most[k] = -INFINITY;
+        if (v + k * W * 64 + lane < v1) {
+          Vec<T>::unpack(raw[k], f);
+          most[k] = max_of(f);
+          take(run, f, most[k], c2);
+        }
+      }
+      if (TOP) {
+        if (first) best.begin(fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])));
+        first = false;
+#pragma unroll
+        for (int k = 0; k < LP_BATCH; ++k) {
+          const unsigned i = v + k * W * 64 + lane;
+          if (i < v1) Vec<T>::unpack(raw[k], f);
+          else
+#pragma unroll
+            for (int e = 0; e < N; ++e) f[e] = NAN;
+          best.look(f, most[k], row.head + i * N);
+        }
+      }
     }
-    lv = best_v[0];
-    li = best_i[0];
+    // what lies before the first boundary and behind the last, with the first and the last part
+    if (w == 0) {
+      const unsigned ends = (part == 0 ? row.head : 0) + (part == parts - 1 ? row.tail : 0);
+      if (ends) {
+        const unsigned i = part == 0 && (unsigned)lane < row.head ? lane : a.cols - row.tail + (lane - (part == 0 ? row.head : 0));
+        float f[1] = {NAN};
+        if ((unsigned)lane < ends) {
+          f[0] = Vec<T>::one(row.at + i);
+          take(run, f, f[0], c2);
+        }
+        if (TOP) best.look(f, f[0], i);
+      }
+    }
+  }
+  run = wave_join(run, c2);
+  if (W > 1) {
+    if (lane == 0) wave_sums[wave] = run;
+    if (TOP && lane < (int)a.top) wave_best[wave][lane] = best.key;
     __syncthreads();
-    if (tid == 0) {
-      const bool any = li != INT32_MAX;
-      a.top_id[r * a.top + k] = any ? li : -1;
-      a.top_logprob[r * a.top + k] = any ? log_p(lv) : NAN;
+    if (w) return;
+#pragma unroll
+    for (int k = 1; k < W; ++k) {
+      run = join(run, wave_sums[wave + k], c2);
+      if (TOP) best.add(lane < (int)a.top ? wave_best[wave + k][lane] : 0);
+    }
+  }
+  if (r >= a.rows) return;
+  if (parts == 1) { finish_row<T>(a, r, run, best); return; }
+  if (lane == 0) sums[unit] = LogprobPart{run.m, run.s, run.t, 0.f};
+  if (TOP && lane < (int)a.top) lists[(size_t)unit * a.top + lane] = best.key;
+}
+
+// A wavefront joins a row's parts.
+template <typename T>
+__global__ __launch_bounds__(64) void logprob_join_kernel(LogprobFwd a, unsigned parts, const LogprobPart* sums, const uint64_t* lists) {
+  const int lane = threadIdx.x;
+  const size_t r = blockIdx.x;
+  const float c2 = a.scale * 1.44269504f;
+  Running run = nothing_seen();
+  for (unsigned k = lane; k < parts; k += 64) {
+    const LogprobPart p = sums[r * parts + k];
+    run = join(run, Running{p.m, p.s, p.t}, c2);
+  }
+  run = wave_join(run, c2);
+  Best best(a.top ? (int)a.top : 1);
+  if (a.top)
+    for (unsigned k = 0; k < parts; ++k) best.add(lane < (int)a.top ? lists[(r * parts + k) * a.top + lane] : 0);
+  finish_row<T>(a, r, run, best);
+}
+
+// ---- backward ------------------------------------------------------------------------------------------------
+// A wavefront has LP_BATCH vectors of each lane of one row; `units` wavefronts a row.
+template <typename T>
+__global__ __launch_bounds__(LP_THREADS) void logprob_bwd_kernel(LogprobBwd a, unsigned units) {
+  constexpr int N = Vec<T>::N, SPAN = 64 * LP_BATCH;
+  const int lane = threadIdx.x & 63;
+  const unsigned unit = blockIdx.x * LP_WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), part = unit % units;
+  const size_t r = unit / units;
+  if (r >= a.rows) return;
+  const Row<T> row((const T*)a.logits + r * a.ld, a.cols);
+  T* d = (T*)a.dlogits + r * a.ld_d;
+  const float m = a.stats[2 * r], ls = a.stats[2 * r + 1];
+  const int token = a.tokens ? a.tokens[r] : -1;
+  const float dl = a.dlogprob && token >= 0 && (unsigned)token < a.cols ? a.dlogprob[r] * a.scale : 0.f;
+  const float de = a.dentropy ? a.dentropy[r] * a.scale : 0.f, ent = a.dentropy ? a.entropy[r] : 0.f;
+  const bool empty = m == -INFINITY && ls == 0.f;
+  const float c2 = a.scale * 1.44269504f, ls2 = ls * 1.44269504f;
+  auto grad = [&](float z, unsigned j) {
+    const float q2 = fmaf(z - m, c2, -ls2), p = __builtin_amdgcn_exp2f(q2);
+    float v = -p * dl - p * (de * fmaf(fmaxf(q2, -1e30f), 0.693147181f, ent));    // (bounded: -inf times a p of 0)
+    if ((int)j == token) v += dl;
+    return empty ? 0.f : v;
+  };
+  const bool same = ((uintptr_t)row.at - (uintptr_t)d) % 16 == 0;      // both come in vectors at the same places
+  const T* zb = row.at + row.head;
+  T* db = d + row.head;
+  const unsigned v0 = part * SPAN;
+  u32x4 raw[LP_BATCH];
+#pragma unroll
+  for (int k = 0; k < LP_BATCH; ++k) {
+    const unsigned i = v0 + k * 64 + lane;
+    if (i < row.vectors) raw[k] = *(const u32x4*)(zb + (size_t)i * N);
+  }
+#pragma unroll
+  for (int k = 0; k < LP_BATCH; ++k) {
+    const unsigned i = v0 + k * 64 + lane;
+    if (i >= row.vectors) break;
+    float f[N];
+    Vec<T>::unpack(raw[k], f);
+#pragma unroll
+    for (int e = 0; e < N; ++e) f[e] = grad(f[e], row.head + i * N + e);
+    if (same) Vec<T>::store(db + (size_t)i * N, f);
+    else
+#pragma unroll
+      for (int e = 0; e < N; ++e) Vec<T>::put(db + (size_t)i * N + e, f[e]);
+  }
+  if (part == 0) {
+    const unsigned ends = row.head + row.tail;
+    if ((unsigned)lane < ends) {
+      const unsigned j = (unsigned)lane < row.head ? lane : a.cols - ends + lane;
+      Vec<T>::put(d + j, grad(Vec<T>::one(row.at + j), j));
     }
   }
 }
 
-template <typename T>
-__global__ __launch_bounds__(LP_THREADS) void logprob_bwd_kernel(LogprobBwd a) {
-  const size_t r = blockIdx.x;
-  const T* z = (const T*)a.logits + r * a.ld;
-  T* d = (T*)a.dlogits + r * a.ld_d;
-  const float m = a.stats[2 * r], ls = a.stats[2 * r + 1];
-  const int token = a.tokens ? a.tokens[r] : -1;
-  const float dl = a.dlogprob && token >= 0 && (unsigned)token < a.cols ? a.dlogprob[r] : 0.f;
-  const float de = a.dentropy ? a.dentropy[r] : 0.f, ent = a.dentropy ? a.entropy[r] : 0.f;
-  for (unsigned j = threadIdx.x; j < a.cols; j += LP_THREADS) {
-    float v = 0.f;
-    if (m != -INFINITY || ls != 0.f) {
-      const float q = (load1(z + j) - m) * a.scale - ls, p = expf(q);
-      v = -dl * p - (p == 0.f ? 0.f : de * p * (q + ent));
-      if ((int)j == token) v += dl;
-    }
-    store1(d + j, v * a.scale);
-  }
+// Wavefronts for a row: one where four would not have a vector for every lane.  Parts of a row: enough for 2048 workgroups (eight on
+// each of 256 compute units), none smaller than one vector a lane.
+struct LogprobCut { unsigned waves, parts; };
+LogprobCut cut_rows(uint32_t rows, uint32_t cols, bool bf16) {
+  const uint32_t vectors = cols / (bf16 ? 8 : 4);
+  const uint64_t parts = std::min<uint64_t>((2048 + rows - 1) / std::max(rows, 1u), vectors / LP_THREADS);
+  if (parts <= 1) return LogprobCut{vectors <= LP_THREADS ? 1u : (unsigned)LP_WAVES, 1};
+  return LogprobCut{(unsigned)LP_WAVES, (unsigned)parts};
 }
+size_t up16(size_t b) { return (b + 15) / 16 * 16; }
 
 bool aligned_to(const void* p, size_t n) { return (uintptr_t)p % n == 0; }
 bool good_rows(uint32_t rows, uint32_t cols, uint64_t ld) {
@@ -136,7 +366,11 @@ bool good_rows(uint32_t rows, uint32_t cols, uint64_t ld) {
 
 }  // namespace
 
-size_t token_logprob_ws_bytes(uint32_t, uint32_t, uint32_t) { return 0; }
+// (the larger of the two types': fp32 rows have twice the vectors)
+size_t token_logprob_ws_bytes(uint32_t rows, uint32_t cols, uint32_t top) {
+  const uint64_t parts = cut_rows(rows, cols, false).parts;
+  return parts > 1 ? up16(rows * parts * sizeof(LogprobPart)) + rows * parts * top * sizeof(uint64_t) : 0;
+}
 
 int token_logprob_fwd(LogprobFwd a, bool bf16, hipStream_t s) {
   if (!a.ld) a.ld = a.cols;
@@ -146,8 +380,22 @@ int token_logprob_fwd(LogprobFwd a, bool bf16, hipStream_t s) {
   if (!a.rows) return KARMA_OK;
   if (!a.logits || !aligned_to(a.logits, bf16 ? 2 : 4)) return KARMA_E_INVAL;
   if (a.ws_bytes < token_logprob_ws_bytes(a.rows, a.cols, a.top)) return KARMA_E_OOM;
-  if (bf16) hipLaunchKernelGGL(logprob_fwd_kernel<bf16_t>, dim3(a.rows), dim3(LP_THREADS), 0, s, a);
-  else hipLaunchKernelGGL(logprob_fwd_kernel<float>, dim3(a.rows), dim3(LP_THREADS), 0, s, a);
+  if (!aligned_to(a.ws, 16)) return KARMA_E_INVAL;
+  const LogprobCut cut = cut_rows(a.rows, a.cols, bf16);
+  LogprobPart* sums = (LogprobPart*)a.ws;
+  uint64_t* lists = (uint64_t*)((char*)a.ws + up16((size_t)a.rows * cut.parts * sizeof(LogprobPart)));
+  const unsigned grid = (unsigned)(((uint64_t)a.rows * cut.parts + LP_WAVES / cut.waves - 1) / (LP_WAVES / cut.waves));
+#define KARMA_LOGPROB_LAUNCH(T, W, TOP) hipLaunchKernelGGL((logprob_fwd_kernel<T, W, TOP>), dim3(grid), dim3(LP_THREADS), 0, s, a, cut.parts, sums, lists)
+  if (bf16) {
+    if (cut.waves == 1) { if (a.top) KARMA_LOGPROB_LAUNCH(bf16_t, 1, true); else KARMA_LOGPROB_LAUNCH(bf16_t, 1, false); }
+    else { if (a.top) KARMA_LOGPROB_LAUNCH(bf16_t, LP_WAVES, true); else KARMA_LOGPROB_LAUNCH(bf16_t, LP_WAVES, false); }
+    if (cut.parts > 1) hipLaunchKernelGGL(logprob_join_kernel<bf16_t>, dim3(a.rows), dim3(64), 0, s, a, cut.parts, sums, lists);
+  } else {
+    if (cut.waves == 1) { if (a.top) KARMA_LOGPROB_LAUNCH(float, 1, true); else KARMA_LOGPROB_LAUNCH(float, 1, false); }
+    else { if (a.top) KARMA_LOGPROB_LAUNCH(float, LP_WAVES, true); else KARMA_LOGPROB_LAUNCH(float, LP_WAVES, false); }
+    if (cut.parts > 1) hipLaunchKernelGGL(logprob_join_kernel<float>, dim3(a.rows), dim3(64), 0, s, a, cut.parts, sums, lists);
+  }
+#undef KARMA_LOGPROB_LAUNCH
   return hipGetLastError() == hipSuccess ? KARMA_OK : KARMA_E_HIP;
 }
 
@@ -158,8 +406,11 @@ int token_logprob_bwd(LogprobBwd a, bool bf16, hipStream_t s) {
   if ((a.dlogprob && !a.tokens) || (a.dentropy && !a.entropy) || (!a.dlogprob && !a.dentropy)) return KARMA_E_INVAL;
   if (!a.rows) return KARMA_OK;
   if (!a.logits || !a.stats || !a.dlogits || !aligned_to(a.logits, bf16 ? 2 : 4) || !aligned_to(a.dlogits, bf16 ? 2 : 4)) return KARMA_E_INVAL;
-  if (bf16) hipLaunchKernelGGL(logprob_bwd_kernel<bf16_t>, dim3(a.rows), dim3(LP_THREADS), 0, s, a);
-  else hipLaunchKernelGGL(logprob_bwd_kernel<float>, dim3(a.rows), dim3(LP_THREADS), 0, s, a);
+  const unsigned vectors = a.cols / (bf16 ? 8 : 4), units = std::max(1u, (vectors + 64 * LP_BATCH - 1) / (64 * LP_BATCH));
+  if ((uint64_t)a.rows * units > INT32_MAX) return KARMA_E_INVAL;
+  const unsigned grid = (a.rows * units + LP_WAVES - 1) / LP_WAVES;
+  if (bf16) hipLaunchKernelGGL(logprob_bwd_kernel<bf16_t>, dim3(grid), dim3(LP_THREADS), 0, s, a, units);
+  else hipLaunchKernelGGL(logprob_bwd_kernel<float>, dim3(grid), dim3(LP_THREADS), 0, s, a, units);
   return hipGetLastError() == hipSuccess ? KARMA_OK : KARMA_E_HIP;
 }
 

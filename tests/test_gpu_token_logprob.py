@@ -92,8 +92,9 @@ class Problem:
         want = F.logprob_backward(z, tokens, self.scale, dl, de)
         e = F.logprob_bounds(z, self.scale)
         p, q, H = e["p"], np.where(e["p"] > 0, e["forward"]["q"], 0.0), e["forward"]["entropy"][:, None]
-        # p is off by its exponential and its argument; each product and sum by a rounding
-        ep = p * (e["q"] + 8 * F.U)
+        # p is off by its exponential and its argument, and below the smallest normal number of fp32 (2^-126) it may be 0: an exponential
+        # of less has no more bits to give; each product and sum by a rounding
+        ep = p * (e["q"] + 8 * F.U) + np.where(p < 2.0 ** -125, 2.0 ** -126, 0.0)
         bound = np.zeros_like(p)
         if dl is not None:
             bound += np.abs(dl)[:, None] * (ep + 2 * F.U * p)
@@ -304,11 +305,10 @@ def test_offsets_beyond_32_bits(torch):
     rows, cols, ld = 1030, 100, 4200000
     p = Problem(torch, 19, rows, cols, top=3)
     both(p)
-    want = [t.clone() for t in (p.logprob, p.top_id, p.d)]
     wide = torch.zeros(rows * ld, dtype=torch.bfloat16, device="cuda").view(rows, ld)
     wide[:, :cols] = p.z
     p.z, p.d = wide[:, :cols], wide[:, cols:2 * cols]
     p.forward()
     p.backward()
-    torch.cuda.synchronize()
-    assert all(torch.equal(a, b) for a, b in zip((p.logprob, p.top_id, p.d), want))
+    p.check_forward()       # (not the same bits: rows on other boundaries are added up in another order)
+    p.check_backward()
