@@ -108,6 +108,15 @@ __device__ __forceinline__ void store4(uint8_t* p, size_t i, size_t n, bool whol
   for (int e = 0; e < 4; ++e) if (i + e < n) p[i + e] = (uint8_t)(v >> (8 * e));
 }
 
+// 1 / s in 64 bits, 0 for 0: the hardware's approximation of 2^-26 and two Newton steps (a division takes three times as long)
+__device__ __forceinline__ double reciprocal(float s) {
+  const double d = s;
+  double r = __builtin_amdgcn_rcp(d);
+  r = fma(fma(-d, r, 1.0), r, r);
+  r = fma(fma(-d, r, 1.0), r, r);
+  return s > 0.f ? r : 0.0;
+}
+
 // Four values' moments in 8 bits: old codes and scales in, new ones out; mo and vo, the moments in fp32 before they are rounded.
 // In 64 bits: which of two codes a value gets does not hang on the order of the operations.  Sixteen lanes have a block.
 struct Codes { unsigned m, v; float sm, sv; };
@@ -132,21 +141,22 @@ __device__ __forceinline__ Codes quantised_step(const Codes& c, const f32x4& g, 
   r.sv = max16(tv) * (float)(1.0 / 65025);
   // a gradient that is not finite: the block's moments are lost, and say so
   if (!(r.sm < INFINITY) || !(r.sv < INFINITY)) r.sm = r.sv = NAN;
-  const double im = r.sm > 0.f ? 1.0 / (double)r.sm : 0.0, iv = r.sv > 0.f ? 1.0 / (double)r.sv : 0.0;    // NaN: codes 0
   r.m = r.v = 0;
   if (r.sm != r.sm) return r;
+  const double im = reciprocal(r.sm), iv = reciprocal(r.sv);
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     const unsigned x = random_bits(i + e, key);
-    const float um = ((x & 0xffff) + 0.5f) * (1.f / 65536), uv = ((x >> 16) + 0.5f) * (1.f / 65536);    // exact
-    const int cm = min(127, max(-127, (int)floor(m[e] * im + um)));
+    const float um = ((x & 0xffff) + 0.5f) * (1.f / 65536);    // exact
+    const int cm = min(127, max(-127, (int)floor(fma(m[e], im, (double)um))));
+    // the code below v: its root in 32 bits, made smaller by more than that can be too large, and one more where that was too much
     const double z = v[e] * iv;
-    float q = floorf(sqrtf((float)z));
+    int q = (int)(__builtin_amdgcn_sqrtf((float)z) * 0.9999995f);
     double rest = z - (double)(q * q);
-    // the root of z rounded to 32 bits may be a border too far, or one short of it
-    if (rest < 0.0) { q -= 1.f; rest += 2.f * q + 1.f; }
-    else if (rest >= 2.f * q + 1.f) { rest -= 2.f * q + 1.f; q += 1.f; }
-    int cv = (int)q + (rest > (double)uv * (2.f * q + 1.f) ? 1 : 0);
+    const double next = (double)(2 * q + 1);
+    if (rest >= next) { ++q; rest -= next; }
+    // up where rest > (x >> 16 + 1/2) / 65536 of the step of 2 q + 1, in whole numbers on the right
+    int cv = q + (rest * 131072.0 > (double)((2 * (x >> 16) + 1) * (unsigned)(2 * q + 1)) ? 1 : 0);
     cv = min(255, z > 0.0 ? max(1, cv) : cv);
     r.m |= (unsigned)(cm & 0xff) << (8 * e);
     r.v |= (unsigned)cv << (8 * e);
@@ -192,7 +202,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamwSet u, AdamwNow a) {
       v[k] = load4((const float*)p.v, i, p.n, whole);
     }
   }
-  const float d1 = (float)(1.0 - (double)a.beta1), d2 = (float)(1.0 - (double)a.beta2), keep = 1.f - a.lr * p.weight_decay;
+  const float d1 = (float)(1.0 - (double)a.beta1), d2 = (float)(1.0 - (double)a.beta2), keep = 1.f - a.lr * p.weight_decay, lr = a.lr * a.c1;
 #pragma unroll
   for (int k = 0; k < ITER; ++k) {
     const size_t i = at + k * 1024;
@@ -213,7 +223,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamwSet u, AdamwNow a) {
       store4((float*)p.v, i, p.n, whole, v[k]);
     }
 #pragma unroll
-    for (int e = 0; e < 4; ++e) w[k][e] = keep * w[k][e] - a.lr * (a.c1 * m[k][e] / (sqrtf(v[k][e]) * a.k2 + a.eps));
+    for (int e = 0; e < 4; ++e) w[k][e] = keep * w[k][e] - lr * (m[k][e] * __builtin_amdgcn_rcpf(sqrtf(v[k][e]) * a.k2 + a.eps));
     store4(p.w, i, p.n, whole, w[k]);
     if (p.out) {
       if (obf) store4((bf16_t*)p.out, i, p.n, whole, w[k]);

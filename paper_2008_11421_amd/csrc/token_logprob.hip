@@ -87,17 +87,16 @@ __device__ __forceinline__ Running join(Running a, Running b, float c2) {
   raise(b, m, c2);
   return Running{m, a.s + b.s, a.t + b.t};
 }
+// The wavefront's: every lane's sums to the largest maximum at once, then added.
 __device__ __forceinline__ Running wave_join(Running r, float c2) {
-#pragma unroll
-  for (int k = 32; k > 0; k >>= 1) r = join(r, Running{__shfl_xor(r.m, k), __shfl_xor(r.s, k), __shfl_xor(r.t, k)}, c2);
-  return r;
+  raise(r, wave_max(r.m), c2);
+  return Running{r.m, wave_sum(r.s), wave_sum(r.t)};
 }
 
 // ---- the best alternatives -------------------------------------------------------------------------------------
-// A wavefront keeps the best so far in order, lane i the i-th, as 64-bit keys: the value's bits in an order of whole numbers, then
-// the inverted index, so that equal values are in ascending order.  0: none.  Most elements fall to one comparison of a vector's
-// largest with the last one's value; one that does not is inserted: its place is the number of lanes that are better, and the
-// lanes behind that move up by one.
+// Elements are kept as 64-bit keys: the value's bits in an order of whole numbers, then the inverted index, so that equal values are
+// in ascending order; all keys differ.  0: none.  A wavefront collects in LDS, without order, what is not below its floor; most
+// vectors fall to one comparison of their largest element.  When its room is full, wave_select throws out what is not among the best.
 __device__ __forceinline__ uint64_t order_key(float v, unsigned i) {
   unsigned u = __float_as_uint(v);
   if (u == 0x80000000u) u = 0;      // -0 equals 0
@@ -109,72 +108,184 @@ __device__ __forceinline__ float key_value(uint64_t k) {
   return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u);
 }
 __device__ __forceinline__ int key_index(uint64_t k) { return (int)(0xffffffffu - (unsigned)k); }
-__device__ __forceinline__ uint64_t lane_key(uint64_t k, int lane) {
-  return (uint64_t)(unsigned)__builtin_amdgcn_readlane((int)(k >> 32), lane) << 32 | (unsigned)__builtin_amdgcn_readlane((int)k, lane);
+constexpr int LP_THREADS = 256, LP_WAVES = LP_THREADS / 64;
+constexpr int LP_KEEP = 128, LP_ROOM = LP_KEEP + 64;    // keys that wave_select may leave, and keys of a wavefront
+
+// What a wavefront writes to LDS its other lanes read: in order within the wavefront, so the compiler alone has to be told.
+__device__ __forceinline__ void wave_lds_fence() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
+__device__ __forceinline__ int lanes_below(uint64_t mask) {
+  return (int)__builtin_amdgcn_mbcnt_hi((unsigned)(mask >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask, 0));
+}
+
+// The largest number of 16 bits (and 16 zeros) that at least `top` of the wavefront's numbers reach: counted bit by bit.
+template <int M>
+__device__ __forceinline__ unsigned reached_by(const unsigned (&u)[M], int top) {
+  unsigned at = 0;
+#pragma unroll
+  for (unsigned bit = 0x80000000u; bit >= 0x10000u; bit >>= 1) {
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < M; ++i) n += __popcll(__ballot(u[i] >= (at | bit)));
+    if (n >= top) at |= bit;
+  }
+  return at;
+}
+// The places of keys among n keys in LDS: how many of those are larger.  (A comparison of 64 bits takes four times as long as one of
+// 32: for few keys only.)
+template <int M>
+__device__ __forceinline__ void places(const uint64_t* keys, int n, const uint64_t (&k)[M], int (&place)[M]) {
+#pragma unroll
+  for (int i = 0; i < M; ++i) place[i] = 0;
+  for (int j = 0; j < n; ++j) {
+    const uint64_t o = keys[j];
+#pragma unroll
+    for (int i = 0; i < M; ++i) place[i] += o > k[i];
+  }
+}
+// Places of keys that lie one a lane, among the n lanes that have one: from their registers, without a trip to LDS a key.
+__device__ __forceinline__ int places_of_lanes(uint64_t k, int n) {
+  int place = 0;
+  for (int j = 0; j < n; ++j) {
+    const uint64_t o = (uint64_t)(unsigned)__builtin_amdgcn_readlane((int)(k >> 32), j) << 32 | (unsigned)__builtin_amdgcn_readlane((int)k, j);
+    place += o > k;
+  }
+  return place;
+}
+// One wavefront, n keys in its registers (key i of lane l being number 64 i + l): leaves the best of them in LDS from `keys` on and returns
+// how many, at most LP_KEEP; with sorted, `top` of them (or all) in order.  least: a key that those that are not among the best do not
+// reach.
+template <int M>
+__device__ __forceinline__ int wave_select(const uint64_t (&k)[M], int n, uint64_t* keys, int top, bool sorted, uint64_t& least) {
+  const int lane = threadIdx.x & 63;
+  wave_lds_fence();     // the keys may come from where the best go
+  unsigned u[M];
+#pragma unroll
+  for (int i = 0; i < M; ++i) u[i] = (unsigned)(k[i] >> 32);
+  if (sorted && n <= 32) {      // (counting first takes as long as 30 places do)
+    const int place = places_of_lanes(k[0], n);
+    if (k[0] && place < top) keys[place] = k[0];
+    wave_lds_fence();
+    return min(n, top);
+  }
+  const unsigned at = n > top ? reached_by<M>(u, top) : 1u;     // (1: all but the empty ones)
+  least = n > top ? (uint64_t)at << 32 : 0;
+  int left = 0;
+#pragma unroll
+  for (int i = 0; i < M; ++i) left += __popcll(__ballot(u[i] >= at));
+  if (left > LP_KEEP) {     // too many alike in 16 bits: all places
+#pragma unroll
+    for (int i = 0; i < M; ++i) keys[i * 64 + lane] = k[i];
+    wave_lds_fence();
+    int place[M];
+    places<M>(keys, n, k, place);
+    wave_lds_fence();
+#pragma unroll
+    for (int i = 0; i < M; ++i)
+      if (k[i] && place[i] < top) keys[place[i]] = k[i];
+    wave_lds_fence();
+    least = keys[top - 1];
+    return top;
+  }
+  left = 0;
+#pragma unroll
+  for (int i = 0; i < M; ++i) {
+    const uint64_t mask = __ballot(u[i] >= at);
+    if (u[i] >= at) keys[left + lanes_below(mask)] = k[i];
+    left += __popcll(mask);
+  }
+  wave_lds_fence();
+  if (!sorted) return left;
+  uint64_t f[2];
+  int place[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) f[i] = lane + i * 64 < left ? keys[lane + i * 64] : 0;
+  if (left > 64) {
+    places<2>(keys, left, f, place);
+  } else {
+    place[0] = places_of_lanes(f[0], left);
+    place[1] = top;
+  }
+  wave_lds_fence();
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    if (f[i] && place[i] < top) keys[place[i]] = f[i];
+  wave_lds_fence();
+  return min(left, top);
+}
+// the same for keys that lie one behind the other in LDS, from `keys` on
+template <int M>
+__device__ __forceinline__ int wave_select_lds(uint64_t* keys, int n, int top, bool sorted, uint64_t& least) {
+  const int lane = threadIdx.x & 63;
+  wave_lds_fence();
+  uint64_t k[M];
+#pragma unroll
+  for (int i = 0; i < M; ++i) k[i] = lane + i * 64 < n ? keys[lane + i * 64] : 0;
+  return wave_select<M>(k, n, keys, top, sorted, least);
 }
 
 struct Best {
-  uint64_t key;       // this lane's
-  uint64_t last;      // of lane top - 1 (the same in all lanes, as the following)
-  float floor;        // values below it need not be looked at
-  int top;
-  __device__ __forceinline__ explicit Best(int top_) : key(0), last(0), floor(-INFINITY), top(top_) {}
-  __device__ __forceinline__ void insert(uint64_t k) {      // k: the same in all lanes, not 0
-    if (k <= last) return;
-    const int place = __popcll(__ballot(key > k));
-    const int hi = __builtin_amdgcn_update_dpp(0, (int)(key >> 32), 0x138, 0xf, 0xf, false);   // wave_shr:1
-    const int lo = __builtin_amdgcn_update_dpp(0, (int)key, 0x138, 0xf, 0xf, false);
-    const int lane = threadIdx.x & 63;
-    if (lane > place) key = (uint64_t)(unsigned)hi << 32 | (unsigned)lo;
-    if (lane == place) key = k;
-    last = lane_key(key, top - 1);
-    if (last) floor = fmaxf(floor, key_value(last));
+  uint64_t* keys;     // LP_ROOM of LDS
+  int count, top;     // the same in all lanes, as the following
+  float floor;        // values below it are not among the best,
+  unsigned before;    // nor are those equal to it from this column on
+  __device__ __forceinline__ Best(uint64_t* keys_, int top_) : keys(keys_), count(0), top(top_), floor(-INFINITY), before(0xffffffffu) {}
+  __device__ __forceinline__ void settle() {
+    uint64_t least;
+    count = wave_select_lds<LP_ROOM / 64>(keys, count, top, false, least);
+    if (!least) return;
+    const float v = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(key_value(least))));
+    // (a floor by 16 bits alone has low bits of 0, as no column has; it may lie among the patterns below -inf, of NaN)
+    const unsigned low = __builtin_amdgcn_readfirstlane((unsigned)least);
+    if (v > floor || (v == floor && low)) {
+      floor = v;
+      before = low ? 0xffffffffu - low : 0xffffffffu;
+    }
   }
-  // the elements of a vector, the e-th of lane l being column base + e
+  // the elements of a vector, the e-th of a lane being column base + e
   template <int N>
   __device__ __forceinline__ void look(const float (&f)[N], float most, unsigned base) {
     if (!__ballot(most >= floor)) return;
 #pragma unroll
     for (int e = 0; e < N; ++e) {
-      uint64_t mask = __ballot(f[e] >= floor);      // NaN is none
-      while (mask) {
-        const int l = __builtin_ctzll(mask);
-        mask &= mask - 1;
-        const float v = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f[e]), l));
-        insert(order_key(v, (unsigned)__builtin_amdgcn_readlane((int)base, l) + e));
+      if (!__ballot(f[e] >= floor)) continue;       // NaN is none
+      bool in = f[e] > floor || (f[e] == floor && base + e < before);
+      uint64_t mask = __ballot(in);
+      if (count + __popcll(mask) > LP_ROOM) {
+        settle();
+        in = f[e] > floor || (f[e] == floor && base + e < before);
+        mask = __ballot(in);
       }
+      if (in) keys[count + lanes_below(mask)] = order_key(f[e], base + e);
+      count += __popcll(mask);
     }
   }
-  // A floor to begin with: the largest of each lane's first elements are 64 different elements, so `top` of them are not below the
-  // top-th largest.  Found to 16 bits, from below.
-  __device__ __forceinline__ void begin(float most) {
-    unsigned u = __float_as_uint(most);
-    u = most != most ? 0u : u & 0x80000000u ? ~u : u | 0x80000000u;
-    unsigned at = 0;
-#pragma unroll
-    for (unsigned bit = 0x80000000u; bit >= 0x10000u; bit >>= 1)
-      if (__popcll(__ballot(u >= (at | bit))) >= top) at |= bit;
-    // (at may lie among the patterns below -inf, of NaN: then there is no floor)
+  // The largest element that each lane has seen: 64 different ones, so `n` elements reach the n-th largest of them.
+  static __device__ __forceinline__ float reached(float seen, int n) {
+    const unsigned b = __float_as_uint(seen), u[1] = {b & 0x80000000u ? ~b : b | 0x80000000u};
+    const unsigned at = reached_by<1>(u, n);
     const float v = __uint_as_float(at & 0x80000000u ? at & 0x7fffffffu : ~at);
-    floor = v == v ? v : -INFINITY;
+    return v == v ? v : -INFINITY;     // (as above)
   }
-  __device__ __forceinline__ void add(uint64_t others) {       // another list of `top` keys in order, lane i the i-th
-    for (int i = 0; i < top; ++i) {
-      const uint64_t k = lane_key(others, i);
-      if (k <= last) break;
-      insert(k);
-    }
+  __device__ __forceinline__ void raise_to(float v) {
+    if (v > floor) { floor = v; before = 0xffffffffu; }
   }
 };
 
 // ---- forward -------------------------------------------------------------------------------------------------
-constexpr int LP_THREADS = 256, LP_WAVES = LP_THREADS / 64;
-constexpr int LP_BATCH = 4;     // vectors a lane has under way
+constexpr int LP_BATCH = 4;     // vectors that a lane has under way
 
 struct LogprobPart { float m, s, t, unused; };
 
+// The token's logit, asked for at the beginning of a row: two trips to memory one after the other.
+struct Named { bool any; float z; };
 template <typename T>
-__device__ __forceinline__ void finish_row(const LogprobFwd& a, size_t r, Running w, const Best& best) {
+__device__ __forceinline__ Named named_logit(const LogprobFwd& a, size_t r) {
+  const int t = a.logprob ? a.tokens[r] : -1;
+  const bool any = t >= 0 && (unsigned)t < a.cols;
+  return Named{any, any ? Vec<T>::one((const T*)a.logits + r * a.ld + t) : 0.f};
+}
+
+__device__ __forceinline__ void finish_row(const LogprobFwd& a, size_t r, Running w, uint64_t key, const Named& named) {
   const int lane = threadIdx.x & 63;
   const bool empty = w.s == 0.f;
   if (empty) { w.m = -INFINITY; w.s = 1.f; w.t = 0.f; }
@@ -183,14 +294,11 @@ __device__ __forceinline__ void finish_row(const LogprobFwd& a, size_t r, Runnin
   if (lane == 0) {
     if (a.stats) { a.stats[2 * r] = w.m; a.stats[2 * r + 1] = ls; }
     if (a.entropy) a.entropy[r] = ls - a.scale * w.t / w.s;
-    if (a.logprob) {
-      const int t = a.tokens[r];
-      a.logprob[r] = t >= 0 && (unsigned)t < a.cols ? log_p(Vec<T>::one((const T*)a.logits + r * a.ld + t)) : 0.f;
-    }
+    if (a.logprob) a.logprob[r] = named.any ? log_p(named.z) : 0.f;
   }
   if (lane < (int)a.top) {
-    a.top_id[r * a.top + lane] = best.key ? key_index(best.key) : -1;
-    a.top_logprob[r * a.top + lane] = best.key ? log_p(key_value(best.key)) : NAN;
+    a.top_id[r * a.top + lane] = key ? key_index(key) : -1;
+    a.top_logprob[r * a.top + lane] = key ? log_p(key_value(key)) : NAN;
   }
 }
 
@@ -200,18 +308,24 @@ template <typename T, int W, bool TOP>
 __global__ __launch_bounds__(LP_THREADS) void logprob_fwd_kernel(LogprobFwd a, unsigned parts, LogprobPart* sums, uint64_t* lists) {
   constexpr int N = Vec<T>::N;
   __shared__ Running wave_sums[LP_WAVES];
-  __shared__ uint64_t wave_best[TOP ? LP_WAVES : 1][64];
+  __shared__ uint64_t keys[TOP ? LP_WAVES * LP_ROOM : 1];
+  __shared__ int counts[LP_WAVES];
+  __shared__ float floors[LP_WAVES];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const unsigned unit = blockIdx.x * (LP_WAVES / W) + wave / W;    // a row's part
   const unsigned r = unit / parts, part = unit % parts, w = wave % W;
   const float c2 = a.scale * 1.44269504f;
   Running run = nothing_seen();
-  Best best(TOP ? (int)a.top : 1);
+  Best best(keys + (TOP ? wave * LP_ROOM : 0), (int)a.top);
+  Named named{false, 0.f};
   if (r < a.rows) {
+    if (parts == 1 && w == 0) named = named_logit<T>(a, r);
     const Row<T> row((const T*)a.logits + (size_t)r * a.ld, a.cols);
-    const unsigned per = (row.vectors + parts - 1) / parts, v0 = min(row.vectors, part * per), v1 = min(row.vectors, v0 + per);
+    // (parts are as even as they can be: each of those that share a row has a vector for every lane)
+    const unsigned per = row.vectors / parts, rest = row.vectors % parts, v0 = part * per + min(part, rest), v1 = v0 + per + (part < rest);
     const T* body = row.at + row.head;
     bool first = true;
+    float seen = -INFINITY;
     for (unsigned v = v0 + w * 64; v < v1; v += LP_BATCH * W * 64) {
       u32x4 raw[LP_BATCH];
       float f[N], most[LP_BATCH];
@@ -230,8 +344,20 @@ __global__ __launch_bounds__(LP_THREADS) void logprob_fwd_kernel(LogprobFwd a, u
         }
       }
       if (TOP) {
-        if (first) best.begin(fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])));
+        // Wavefronts that share a row have a share of the best each: all of those reach the smallest of their floors.  After the first
+        // batch nobody waits: an older floor of another costs time alone.
+#pragma unroll
+        for (int k = 0; k < LP_BATCH; ++k) seen = fmaxf(seen, most[k]);
+        float reach = Best::reached(seen, ((int)a.top + W - 1) / W);
+        if (W > 1) {
+          volatile float* theirs = floors;
+          theirs[wave] = reach;
+          if (first) __syncthreads();
+          for (int k = 0; k < W; ++k) reach = fminf(reach, theirs[k]);
+          reach = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(reach)));
+        }
         first = false;
+        best.raise_to(reach);
 #pragma unroll
         for (int k = 0; k < LP_BATCH; ++k) {
           const unsigned i = v + k * W * 64 + lane;
@@ -258,39 +384,96 @@ __global__ __launch_bounds__(LP_THREADS) void logprob_fwd_kernel(LogprobFwd a, u
     }
   }
   run = wave_join(run, c2);
+  uint64_t key = 0, least;
   if (W > 1) {
-    if (lane == 0) wave_sums[wave] = run;
-    if (TOP && lane < (int)a.top) wave_best[wave][lane] = best.key;
+    if (TOP && best.count > LP_KEEP) best.settle();
+    if (lane == 0) { wave_sums[wave] = run; counts[wave] = best.count; }
     __syncthreads();
-    if (w) return;
+    if (w) return;      // the first wavefront has the rest
 #pragma unroll
-    for (int k = 1; k < W; ++k) {
-      run = join(run, wave_sums[wave + k], c2);
-      if (TOP) best.add(lane < (int)a.top ? wave_best[wave + k][lane] : 0);
+    for (int k = 1; k < W; ++k) run = join(run, wave_sums[wave + k], c2);
+    if (TOP) {
+      // number i of all keys, the wavefronts' one behind the other
+      int ends[W];
+      ends[0] = best.count;
+#pragma unroll
+      for (int k = 1; k < W; ++k) ends[k] = ends[k - 1] + counts[wave + k];
+      auto gather = [&](int i) {
+        int at = i;
+#pragma unroll
+        for (int k = 1; k < W; ++k) at = i >= ends[k - 1] ? k * LP_ROOM + i - ends[k - 1] : at;
+        return i < ends[W - 1] ? best.keys[at] : 0;
+      };
+      int n = ends[W - 1];
+      if (n <= 128) {
+        uint64_t k[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) k[i] = gather(lane + i * 64);
+        n = wave_select<2>(k, n, best.keys, a.top, true, least);
+      } else {
+        uint64_t k[W * LP_KEEP / 64];
+#pragma unroll
+        for (int i = 0; i < W * LP_KEEP / 64; ++i) k[i] = gather(lane + i * 64);
+        n = wave_select<W * LP_KEEP / 64>(k, n, best.keys, a.top, true, least);
+      }
+      if (lane < n) key = best.keys[lane];
     }
+  } else if (TOP) {
+    const int n = wave_select_lds<LP_ROOM / 64>(best.keys, best.count, a.top, true, least);
+    if (lane < n) key = best.keys[lane];
   }
   if (r >= a.rows) return;
-  if (parts == 1) { finish_row<T>(a, r, run, best); return; }
+  if (parts == 1) { finish_row(a, r, run, key, named); return; }
   if (lane == 0) sums[unit] = LogprobPart{run.m, run.s, run.t, 0.f};
-  if (TOP && lane < (int)a.top) lists[(size_t)unit * a.top + lane] = best.key;
+  if (TOP && lane < (int)a.top) lists[(size_t)unit * a.top + lane] = key;
 }
 
-// A wavefront joins a row's parts.
+// A workgroup joins a row's parts.  Of their lists only what reaches the largest of the lists' last keys can be among the best; where
+// there is more than the room, it is settled in between.
 template <typename T>
-__global__ __launch_bounds__(64) void logprob_join_kernel(LogprobFwd a, unsigned parts, const LogprobPart* sums, const uint64_t* lists) {
-  const int lane = threadIdx.x;
+__global__ __launch_bounds__(LP_THREADS) void logprob_join_kernel(LogprobFwd a, unsigned parts, const LogprobPart* sums, const uint64_t* lists) {
+  __shared__ uint64_t keys[2 * LP_THREADS];
+  __shared__ int count;
+  const int lane = threadIdx.x & 63, tid = threadIdx.x;
   const size_t r = blockIdx.x;
   const float c2 = a.scale * 1.44269504f;
+  uint64_t key = 0, least;
   Running run = nothing_seen();
-  for (unsigned k = lane; k < parts; k += 64) {
-    const LogprobPart p = sums[r * parts + k];
-    run = join(run, Running{p.m, p.s, p.t}, c2);
+  const Named named = named_logit<T>(a, r);
+  if (a.top) {
+    const uint64_t* mine = lists + r * parts * a.top;
+    const unsigned n = parts * a.top;
+    uint64_t next = tid < (int)n ? mine[tid] : 0;
+    // every wavefront finds the floor for itself
+    uint64_t floor = 0;
+    for (unsigned k = lane; k < parts; k += 64) floor = max(floor, mine[k * a.top + a.top - 1]);
+#pragma unroll
+    for (int k = 32; k > 0; k >>= 1) floor = max(floor, (uint64_t)__shfl_xor((unsigned long long)floor, k));
+    if (tid == 0) count = 0;
+    for (unsigned v = 0; v < n; v += LP_THREADS) {
+      const uint64_t k = next;
+      const bool last = v + LP_THREADS >= n;
+      next = v + LP_THREADS + tid < n ? mine[v + LP_THREADS + tid] : 0;
+      __syncthreads();
+      if (k && k >= floor) keys[atomicAdd(&count, 1)] = k;      // in any order: what is chosen does not depend on it
+      __syncthreads();
+      const int have = count;
+      if (have <= LP_THREADS && !last) continue;
+      if (tid < 64) {
+        const int left = have <= 128 ? wave_select_lds<2>(keys, have, a.top, last, least) : wave_select_lds<2 * LP_THREADS / 64>(keys, have, a.top, last, least);
+        if (lane == 0) count = left;
+        if (last && lane < left) key = keys[lane];
+      }
+    }
   }
+  if (tid < 64)
+    for (unsigned k = lane; k < parts; k += 64) {
+      const LogprobPart p = sums[r * parts + k];
+      run = join(run, Running{p.m, p.s, p.t}, c2);
+    }
+  if (tid >= 64) return;
   run = wave_join(run, c2);
-  Best best(a.top ? (int)a.top : 1);
-  if (a.top)
-    for (unsigned k = 0; k < parts; ++k) best.add(lane < (int)a.top ? lists[(r * parts + k) * a.top + lane] : 0);
-  finish_row<T>(a, r, run, best);
+  finish_row(a, r, run, key, named);
 }
 
 // ---- backward ------------------------------------------------------------------------------------------------
@@ -389,11 +572,11 @@ int token_logprob_fwd(LogprobFwd a, bool bf16, hipStream_t s) {
   if (bf16) {
     if (cut.waves == 1) { if (a.top) KARMA_LOGPROB_LAUNCH(bf16_t, 1, true); else KARMA_LOGPROB_LAUNCH(bf16_t, 1, false); }
     else { if (a.top) KARMA_LOGPROB_LAUNCH(bf16_t, LP_WAVES, true); else KARMA_LOGPROB_LAUNCH(bf16_t, LP_WAVES, false); }
-    if (cut.parts > 1) hipLaunchKernelGGL(logprob_join_kernel<bf16_t>, dim3(a.rows), dim3(64), 0, s, a, cut.parts, sums, lists);
+    if (cut.parts > 1) hipLaunchKernelGGL(logprob_join_kernel<bf16_t>, dim3(a.rows), dim3(LP_THREADS), 0, s, a, cut.parts, sums, lists);
   } else {
     if (cut.waves == 1) { if (a.top) KARMA_LOGPROB_LAUNCH(float, 1, true); else KARMA_LOGPROB_LAUNCH(float, 1, false); }
     else { if (a.top) KARMA_LOGPROB_LAUNCH(float, LP_WAVES, true); else KARMA_LOGPROB_LAUNCH(float, LP_WAVES, false); }
-    if (cut.parts > 1) hipLaunchKernelGGL(logprob_join_kernel<float>, dim3(a.rows), dim3(64), 0, s, a, cut.parts, sums, lists);
+    if (cut.parts > 1) hipLaunchKernelGGL(logprob_join_kernel<float>, dim3(a.rows), dim3(LP_THREADS), 0, s, a, cut.parts, sums, lists);
   }
 #undef KARMA_LOGPROB_LAUNCH
   return hipGetLastError() == hipSuccess ? KARMA_OK : KARMA_E_HIP;
