@@ -607,7 +607,7 @@ int karma_k_attention_bwd_bf16(const void* qkv_dev, const void* ctx_dev, const v
  * Errors: KARMA_E_INVAL, KARMA_E_OOM (ws_bytes too small). */
 #define KARMA_SCAN_MARK 256u
 typedef struct {
-  uint64_t tokens;              /* rows of the tensors, < 2^31 */
+  uint64_t tokens;              /* rows of the tensors, < 2^31 - 1024 */
   uint32_t channels, sequences; /* at least one of each */
   uint64_t ld_gate, ld_x, ld_h, ld_dgate, ld_dx; /* elements; ld_h: of h and of dh */
 } karma_scan_shape;

@@ -6,6 +6,8 @@
 // and 1 - b rounded to 32 bits would lose it.  States and carries are fp32.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "device_utils.h"
 #include "karma.h"
 #include "kernels.h"
@@ -13,94 +15,687 @@
 namespace karma {
 namespace {
 
-template <typename T>
-__device__ __forceinline__ float load1(const T* p);
+// ---- a lane's channels -----------------------------------------------------------------------------------------
+// V neighbouring channels of one token, raw as loaded: bf16 pairs where everything is on 4-byte boundaries, else one value.
+template <typename T, int V>
+struct Lane;
 template <>
-__device__ __forceinline__ float load1<bf16_t>(const bf16_t* p) { return bf2f(*p); }
+struct Lane<bf16_t, 2> {
+  typedef unsigned Raw;
+  static __device__ __forceinline__ void get(Raw r, float (&v)[2]) { v[0] = __uint_as_float(r << 16); v[1] = __uint_as_float(r & 0xffff0000u); }
+  static __device__ __forceinline__ Raw put(const float (&v)[2]) { return pack2(v[0], v[1]); }
+};
 template <>
-__device__ __forceinline__ float load1<float>(const float* p) { return *p; }
-__device__ __forceinline__ void store1(bf16_t* p, float v) { *p = f2bf(v); }
-__device__ __forceinline__ void store1(float* p, float v) { *p = v; }
+struct Lane<bf16_t, 1> {
+  typedef bf16_t Raw;
+  static __device__ __forceinline__ void get(Raw r, float (&v)[1]) { v[0] = bf2f(r); }
+  static __device__ __forceinline__ Raw put(const float (&v)[1]) { return f2bf(v[0]); }
+};
+template <>
+struct Lane<float, 1> {
+  typedef float Raw;
+  static __device__ __forceinline__ void get(Raw r, float (&v)[1]) { v[0] = r; }
+  static __device__ __forceinline__ Raw put(const float (&v)[1]) { return v[0]; }
+};
 
-__device__ __forceinline__ float share_of(float f) { return 1.f / (1.f + __expf(f)); }
+// b = 1 / (1 + e^f): 1 for -inf, 0 for +inf
+__device__ __forceinline__ float share_of(float f) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(f * 1.44269504f)); }
+__device__ __forceinline__ float step_of(float b, float x, float h) { return fmaf(b, x - h, h); }
 
-struct ScanSpan { long first, last; };   // tokens [first, last) of a sequence
-__device__ __forceinline__ ScanSpan span_of(const int* starts, long tokens, unsigned sequences, unsigned j) {
-  if (!starts) { const long n = tokens / sequences; return ScanSpan{j * n, (j + 1) * n}; }
-  // whatever the starts say, no token outside the tensors is touched
-  const long a = starts[j], e = starts[j + 1];
-  return ScanSpan{a < 0 ? 0 : a > tokens ? tokens : a, e < 0 ? 0 : e > tokens ? tokens : e};
-}
-
-template <typename T>
-__global__ __launch_bounds__(64) void scan_fwd_kernel(ScanFwd a) {
-  const unsigned cols = (a.s.channels + 63) / 64, j = blockIdx.x / cols, c = blockIdx.x % cols * 64 + threadIdx.x;
-  if (c >= a.s.channels) return;
-  const ScanSpan p = span_of(a.starts, a.s.tokens, a.s.sequences, j);
-  float h = a.h0 ? a.h0[(size_t)j * a.s.channels + c] : 0.f;
-  for (long t = p.first; t < p.last; ++t) {
-    if (a.marks && t % KARMA_SCAN_MARK == 0) a.marks[(size_t)(t / KARMA_SCAN_MARK) * a.s.channels + c] = h;
-    const float b = share_of(load1((const T*)a.gate + t * a.s.ld_gate + c)), x = load1((const T*)a.x + t * a.s.ld_x + c);
-    h = fmaf(b, x - h, h);
-    store1((T*)a.h + t * a.s.ld_h + c, h);
+// ---- sequences -------------------------------------------------------------------------------------------------
+struct Spans {
+  const int* starts;
+  int tokens, sequences, each;      // each: their length where starts is null
+  // tokens [first, last) of sequence j; whatever the starts say, no token outside the tensors is touched
+  __device__ __forceinline__ int at(int j) const {
+    if (!starts) return j * each;
+    const int t = starts[j];
+    return t < 0 ? 0 : t > tokens ? tokens : t;
   }
-  if (a.h_last) a.h_last[(size_t)j * a.s.channels + c] = h;
+  // the last sequence that begins at or before token t (-1: none)
+  __device__ __forceinline__ int find(int t) const {
+    if (!starts) return t / each;
+    int lo = 0, hi = sequences + 1;     // entries below lo are <= t, those from hi on are not
+    while (lo < hi) {
+      const int mid = (lo + hi) / 2;
+      if (at(mid) <= t) lo = mid + 1;
+      else hi = mid;
+    }
+    return lo - 1;
+  }
+  // from sequence j on to the one that token t begins, or back to the one that token t ends
+  __device__ __forceinline__ int next(int j, int t) const {
+    if (!starts) return t / each;
+    while (j + 1 < sequences && at(j + 1) <= t) ++j;
+    return j;
+  }
+  __device__ __forceinline__ int previous(int j, int t) const {
+    if (!starts) return t / each;
+    while (j > 0 && at(j) > t) --j;
+    return j;
+  }
+  __device__ __forceinline__ size_t row(int j, int channels) const { return (size_t)(j < 0 ? 0 : j >= sequences ? sequences - 1 : j) * channels; }
+};
+
+// The tokens of a wavefront, t0 .. t0 + L - 1, L <= 32
+struct Part {
+  unsigned begins;      // tokens that begin a sequence,
+  unsigned ends;        // that end one,
+  unsigned inside;      // that belong to one
+  int seq;              // the last sequence that begins at or before t0
+};
+// word: 8 bytes of LDS of the wavefront's own
+template <int L>
+__device__ __forceinline__ Part part_of(const Spans& p, int t0, unsigned long long* word) {
+  const int lane = threadIdx.x & 63;
+  unsigned long long bounds = 0;     // bit i: a boundary before token t0 + i, 0 <= i <= L
+  Part r;
+  r.seq = __builtin_amdgcn_readfirstlane(p.find(t0));
+  const int first = __builtin_amdgcn_readfirstlane(p.at(0)), last = __builtin_amdgcn_readfirstlane(p.at(p.sequences));
+  if (!p.starts) {
+    for (int t = r.seq * p.each; t <= t0 + L && t <= last; t += p.each)
+      if (t >= t0) bounds |= 1ull << (t - t0);
+  } else {
+    if (lane == 0) *word = 0;
+    for (int k = r.seq < 0 ? 0 : r.seq; k <= p.sequences; k += 64) {
+      const int t = k + lane <= p.sequences ? p.at(k + lane) : INT32_MAX;
+      if (t >= t0 && t - t0 <= L) atomicOr(word, 1ull << (t - t0));
+      if (__ballot(t - t0 <= L) != ~0ull) break;
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    bounds = *word;
+    bounds = (unsigned long long)(unsigned)__builtin_amdgcn_readfirstlane((int)(bounds >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)bounds);
+  }
+  const unsigned all = L == 32 ? ~0u : (1u << L) - 1;
+  const int lo = first - t0, hi = last - t0;
+  r.inside = lo >= L || hi <= 0 ? 0 : (lo > 0 ? all << lo : all) & (hi < L ? (1u << hi) - 1 : all) & all;
+  r.begins = (unsigned)bounds & r.inside;
+  r.ends = (unsigned)(bounds >> 1) & r.inside;
+  return r;
 }
 
-template <typename T>
-__global__ __launch_bounds__(64) void scan_bwd_kernel(ScanBwd a) {
-  __shared__ float before[KARMA_SCAN_MARK][64];
-  const unsigned cols = (a.s.channels + 63) / 64, j = blockIdx.x / cols, c = blockIdx.x % cols * 64 + threadIdx.x;
-  if (c >= a.s.channels) return;
-  const ScanSpan p = span_of(a.starts, a.s.tokens, a.s.sequences, j);
-  const size_t at = (size_t)j * a.s.channels + c;
-  float g = a.dh_last ? a.dh_last[at] : 0.f;
-  for (long end = p.last; end > p.first;) {
-    const long mark = (end - 1) / KARMA_SCAN_MARK * KARMA_SCAN_MARK, begin = mark > p.first ? mark : p.first;
-    float h = mark > p.first ? a.marks[(size_t)(mark / KARMA_SCAN_MARK) * a.s.channels + c] : a.h0 ? a.h0[at] : 0.f;
-    for (long t = begin; t < end; ++t) {
-      before[t - begin][threadIdx.x] = h;
-      const float b = share_of(load1((const T*)a.gate + t * a.s.ld_gate + c)), x = load1((const T*)a.x + t * a.s.ld_x + c);
-      h = fmaf(b, x - h, h);
-    }
-    for (long t = end - 1; t >= begin; --t) {
-      const float b = share_of(load1((const T*)a.gate + t * a.s.ld_gate + c)), x = load1((const T*)a.x + t * a.s.ld_x + c);
-      const float D = load1((const T*)a.dh + t * a.s.ld_h + c) + g;
-      store1((T*)a.dx + t * a.s.ld_dx + c, b * D);
-      store1((T*)a.dgate + t * a.s.ld_dgate + c, D * (before[t - begin][threadIdx.x] - x) * fmaf(-b, b, b));
-      g = fmaf(-b, D, D);
-    }
-    end = begin;
-  }
-  if (a.dh0) a.dh0[at] = g;
+// ---- the chain of workgroups ------------------------------------------------------------------------------------
+// A chunk of KARMA_SCAN_MARK tokens and some channels belongs to a workgroup.  What it does to the state that comes in is
+// out = A in + H; it publishes both at once (8 bytes a channel; A below 0: out = H, a sequence began in it) and waits for the state
+// behind the chunk before it, which one wavefront per block of channels carries through all chunks in their order: the same sums in
+// the same order every time, without a trip to memory between one chunk and the next.  Workgroups take their work by a counter, the
+// carriers first, so whoever is waited for is already running.  A word of all ones is not there yet.  A wait that never ends (a
+// workspace that another call is using) is given up, and the states become NaN.
+struct Chain {
+  unsigned* ticket;
+  unsigned long long* effect;   // [chunk][channel]
+  unsigned* state;              // behind the chunk
+  int chunks, blocks, width;    // blocks of channels, channels of all blocks; chunks == 1: no chain
+};
+constexpr int CHAIN_LIMIT = 1 << 21;    // looks at a word, a microsecond or so each
+
+__device__ __forceinline__ unsigned long long effect_word(float A, float H, bool cut) {
+  const unsigned long long w = (unsigned long long)__float_as_uint(H) << 32 | __float_as_uint(cut ? -1.f : A);
+  return w == ~0ull ? 0x7fc000007fc00000ull : w;
 }
+template <int V>
+__device__ __forceinline__ void publish(const Chain& c, int chunk, int channel, const float (&A)[V], const float (&H)[V], bool cut) {
+#pragma unroll
+  for (int e = 0; e < V; ++e)
+    __hip_atomic_store(c.effect + (size_t)chunk * c.width + channel + e, effect_word(A[e], H[e], cut), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+template <int V>
+__device__ __forceinline__ void await(const Chain& c, int chunk, int channel, float (&in)[V]) {
+  unsigned w[V];
+  for (int n = 0; n < CHAIN_LIMIT; ++n) {
+    bool missing = false;
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      w[e] = __hip_atomic_load(c.state + (size_t)chunk * c.width + channel + e, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      missing |= w[e] == ~0u;
+    }
+    if (!__ballot(missing)) break;
+    __builtin_amdgcn_s_sleep(1);
+  }
+#pragma unroll
+  for (int e = 0; e < V; ++e) in[e] = __uint_as_float(w[e]);    // all ones are a NaN
+}
+// from chunk 0 up, or from the last one down
+template <int V>
+__device__ __forceinline__ void carry(const Chain& c, int channel, bool up) {
+  constexpr int AHEAD = 8;
+  float s[V] = {};
+  int n = 0;
+  for (int done = 0; done < c.chunks - 1;) {
+    unsigned long long w[AHEAD][V];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      const int k = min(done + i, c.chunks - 1);
+#pragma unroll
+      for (int e = 0; e < V; ++e)
+        w[i][e] = __hip_atomic_load(c.effect + (size_t)(up ? k : c.chunks - 1 - k) * c.width + channel + e, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    if (++n > CHAIN_LIMIT) return;
+    const int before = done;
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      bool missing = false;
+#pragma unroll
+      for (int e = 0; e < V; ++e) missing |= w[i][e] == ~0ull;
+      if (done != before + i || done >= c.chunks - 1 || __ballot(missing)) continue;
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const float A = __uint_as_float((unsigned)w[i][e]), H = __uint_as_float((unsigned)(w[i][e] >> 32));
+        s[e] = A < 0.f ? H : fmaf(A, s[e], H);
+        const unsigned u = __float_as_uint(s[e]);
+        __hip_atomic_store(c.state + (size_t)(up ? done : c.chunks - 1 - done) * c.width + channel + e, u == ~0u ? 0x7fc00000u : u, __ATOMIC_RELAXED,
+                           __HIP_MEMORY_SCOPE_AGENT);
+      }
+      ++done;
+    }
+    if (done != before) n = 0;
+  }
+}
+__global__ void chain_clear_kernel(Chain c) {
+  const size_t n = (size_t)c.chunks * c.width, i = (size_t)blockIdx.x * blockDim.x + threadIdx.x;
+  if (i == 0) *c.ticket = 0;
+  if (i < n) { c.effect[i] = ~0ull; c.state[i] = ~0u; }
+}
+
+// The work of this workgroup: a chunk and a block of channels, or false for a carrier, which has then done its work.
+template <int V>
+__device__ __forceinline__ bool take_work(const Chain& c, bool up, int& chunk, int& block) {
+  __shared__ unsigned ticket;
+  int unit = blockIdx.x;
+  if (c.chunks > 1) {
+    if (threadIdx.x == 0) ticket = atomicAdd(c.ticket, 1u);
+    __syncthreads();
+    unit = __builtin_amdgcn_readfirstlane((int)ticket);
+    if (unit < c.blocks) {
+      if (threadIdx.x < 64) carry<V>(c, unit * 64 * V + threadIdx.x * V, up);
+      return false;
+    }
+    unit -= c.blocks;
+  }
+  chunk = unit / c.blocks;
+  if (!up) chunk = c.chunks - 1 - chunk;
+  block = unit % c.blocks;
+  return true;
+}
+
+// ---- forward ----------------------------------------------------------------------------------------------------
+// W wavefronts have the chunk's tokens one part behind the other, L each, a lane V channels, everything in registers: one pass over
+// memory.  Each runs through its part once for A and H, and, when the state before it is known, again for the states themselves.
+template <typename T, int V, int L, int W>
+__global__ __launch_bounds__(64 * W) void scan_fwd_kernel(ScanFwd a, Spans p, Chain chain) {
+  typedef Lane<T, V> Ln;
+  static_assert(L * W == KARMA_SCAN_MARK, "a chunk is what lies between two marks");
+  __shared__ float effects[W][2][64 * V];
+  __shared__ float incoming[64 * V];
+  __shared__ unsigned long long words[W];
+  __shared__ int cuts[W];
+  int chunk, block;
+  if (!take_work<V>(chain, true, chunk, block)) return;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), C = (int)a.s.channels;
+  const int channel = block * 64 * V + lane * V, c = channel < C ? channel : C - V;     // (lanes without a channel repeat the last one)
+  const bool mine = channel < C;
+  const int t0 = chunk * KARMA_SCAN_MARK + w * L;
+  typename Ln::Raw rf[L], rx[L];
+#pragma unroll
+  for (int i = 0; i < L; ++i) {
+    const size_t t = min(t0 + i, p.tokens - 1);
+    rf[i] = *(const typename Ln::Raw*)((const T*)a.gate + t * a.s.ld_gate + c);
+    rx[i] = *(const typename Ln::Raw*)((const T*)a.x + t * a.s.ld_x + c);
+  }
+  const Part q = part_of<L>(p, t0, words + w);
+  const unsigned all = L == 32 ? ~0u : (1u << (L & 31)) - 1;
+  const bool plain = q.inside == all && !q.begins && !q.ends;
+  float b[L][V], A[V], h[V], begun[V] = {};
+#pragma unroll
+  for (int e = 0; e < V; ++e) { A[e] = 1.f; h[e] = 0.f; }
+#pragma unroll
+  for (int i = 0; i < L; ++i) {
+    Ln::get(rf[i], b[i]);
+#pragma unroll
+    for (int e = 0; e < V; ++e) b[i][e] = share_of(b[i][e]);
+  }
+  auto initial = [&](int j, float (&v)[V]) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] = a.h0 ? a.h0[p.row(j, C) + c + e] : 0.f;
+  };
+  if (plain) {
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+      float x[V];
+      Ln::get(rx[i], x);
+#pragma unroll
+      for (int e = 0; e < V; ++e) { h[e] = step_of(b[i][e], x[e], h[e]); A[e] = fmaf(-b[i][e], A[e], A[e]); }
+    }
+  } else {
+    int j = q.seq;
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+      if (q.begins >> i & 1) {
+        j = p.next(j, t0 + i);
+        initial(j, begun);      // of the last one kept: by the second run h_last may lie over it
+#pragma unroll
+        for (int e = 0; e < V; ++e) h[e] = begun[e];
+      }
+      if (!(q.inside >> i & 1)) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) b[i][e] = 0.f;
+        continue;
+      }
+      float x[V];
+      Ln::get(rx[i], x);
+#pragma unroll
+      for (int e = 0; e < V; ++e) { h[e] = step_of(b[i][e], x[e], h[e]); A[e] = fmaf(-b[i][e], A[e], A[e]); }
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < V; ++e) { effects[w][0][lane * V + e] = A[e]; effects[w][1][lane * V + e] = h[e]; }
+  if (lane == 0) cuts[w] = q.begins != 0;
+  __syncthreads();
+  // what the wavefronts before this one do together; the first wavefront has the whole chunk's
+  float PA[V], PH[V];
+  bool cut = false;
+#pragma unroll
+  for (int e = 0; e < V; ++e) { PA[e] = 1.f; PH[e] = 0.f; }
+  for (int k = 0; k < (w == 0 ? W : w); ++k) {
+    const bool fresh = cuts[k];
+    cut |= fresh;
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      const float Ak = effects[k][0][lane * V + e], Hk = effects[k][1][lane * V + e];
+      PH[e] = fresh ? Hk : fmaf(Ak, PH[e], Hk);
+      PA[e] *= Ak;
+    }
+  }
+  const bool wants = chain.chunks > 1 && chunk > 0;
+  if (w == 0 && chain.chunks > 1) {
+    float in[V] = {};
+    publish<V>(chain, chunk, channel, PA, PH, cut);
+    if (wants && !(q.begins & 1)) await<V>(chain, chunk - 1, channel, in);
+#pragma unroll
+    for (int e = 0; e < V; ++e) incoming[lane * V + e] = in[e];
+  }
+  if (chain.chunks > 1) __syncthreads();
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+    const float in = chain.chunks > 1 ? incoming[lane * V + e] : 0.f;
+    h[e] = w == 0 ? in : cut ? PH[e] : fmaf(PA[e], in, PH[e]);
+  }
+  if (w == 0 && a.marks && mine) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) a.marks[(size_t)chunk * C + c + e] = h[e];
+  }
+  auto store = [&](int i) {
+    if (mine) *(typename Ln::Raw*)((T*)a.h + (size_t)(t0 + i) * a.s.ld_h + c) = Ln::put(h);
+  };
+  if (plain) {
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+      float x[V];
+      Ln::get(rx[i], x);
+#pragma unroll
+      for (int e = 0; e < V; ++e) h[e] = step_of(b[i][e], x[e], h[e]);
+      store(i);
+    }
+  } else {
+    int j = q.seq;
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+      if (q.begins >> i & 1) {
+        j = p.next(j, t0 + i);
+        if (q.begins >> i == 1) {
+#pragma unroll
+          for (int e = 0; e < V; ++e) h[e] = begun[e];
+        } else {
+          initial(j, h);
+        }
+      }
+      if (!(q.inside >> i & 1)) continue;
+      float x[V];
+      Ln::get(rx[i], x);
+#pragma unroll
+      for (int e = 0; e < V; ++e) h[e] = step_of(b[i][e], x[e], h[e]);
+      store(i);
+      if ((q.ends >> i & 1) && a.h_last && mine) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) a.h_last[p.row(j, C) + c + e] = h[e];
+      }
+    }
+  }
+  // sequences without tokens keep their states: each chunk has a share of all sequences
+  if (a.h_last && p.starts && mine) {
+    const long share = ((long)p.sequences + chain.chunks - 1) / chain.chunks;
+    for (long k = chunk * share + w; k < min((long)p.sequences, (chunk + 1) * share); k += W)
+      if (p.at((int)k) >= p.at((int)k + 1)) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) a.h_last[k * C + c + e] = a.h0 ? a.h0[k * C + c + e] : 0.f;
+      }
+  }
+}
+
+// Short sequences (single tokens among them): a wavefront has a whole one, eight tokens under way.
+template <typename T, int V>
+__global__ __launch_bounds__(256) void scan_fwd_short_kernel(ScanFwd a, Spans p, int blocks, int units) {
+  typedef Lane<T, V> Ln;
+  constexpr int L = 8;
+  const int unit = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+  if (unit >= units) return;
+  const int j = unit / blocks, C = (int)a.s.channels, c = (unit % blocks) * 64 * V + (threadIdx.x & 63) * V;
+  if (c >= C) return;
+  const int first = p.at(j), last = p.at(j + 1);
+  float h[V];
+#pragma unroll
+  for (int e = 0; e < V; ++e) h[e] = a.h0 ? a.h0[(size_t)j * C + c + e] : 0.f;
+  for (int t0 = first; t0 < last; t0 += L) {
+    typename Ln::Raw rf[L], rx[L];
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+      const size_t t = min(t0 + i, last - 1);
+      rf[i] = *(const typename Ln::Raw*)((const T*)a.gate + t * a.s.ld_gate + c);
+      rx[i] = *(const typename Ln::Raw*)((const T*)a.x + t * a.s.ld_x + c);
+    }
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+      const int t = t0 + i;
+      if (t >= last) break;
+      float b[V], x[V];
+      Ln::get(rf[i], b);
+      Ln::get(rx[i], x);
+      if (a.marks && t % KARMA_SCAN_MARK == 0) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) a.marks[(size_t)(t / KARMA_SCAN_MARK) * C + c + e] = h[e];
+      }
+#pragma unroll
+      for (int e = 0; e < V; ++e) h[e] = step_of(share_of(b[e]), x[e], h[e]);
+      *(typename Ln::Raw*)((T*)a.h + (size_t)t * a.s.ld_h + c) = Ln::put(h);
+    }
+  }
+  if (a.h_last) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) a.h_last[(size_t)j * C + c + e] = h[e];
+  }
+}
+
+// ---- backward ---------------------------------------------------------------------------------------------------
+// As forward, with the chain from the last chunk to the first: the gradient g of the state behind a part goes in, that of the state
+// before it comes out, out = A g + R.  The states are run through again from the chunk's mark.
+template <typename T, int V, int L, int W>
+__global__ __launch_bounds__(64 * W) void scan_bwd_kernel(ScanBwd a, Spans p, Chain chain) {
+  typedef Lane<T, V> Ln;
+  static_assert(L * W == KARMA_SCAN_MARK, "a chunk is what lies between two marks");
+  __shared__ float effects[W][3][64 * V];
+  __shared__ float incoming[64 * V];
+  __shared__ unsigned long long words[W];
+  __shared__ int cuts[W];       // 1: a sequence begins in the part, 2: one ends in it
+  int chunk, block;
+  if (!take_work<V>(chain, false, chunk, block)) return;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), C = (int)a.s.channels;
+  const int channel = block * 64 * V + lane * V, c = channel < C ? channel : C - V;
+  const bool mine = channel < C;
+  const int t0 = chunk * KARMA_SCAN_MARK + w * L;
+  typename Ln::Raw rf[L], rx[L], rd[L];
+#pragma unroll
+  for (int i = 0; i < L; ++i) {
+    const size_t t = min(t0 + i, p.tokens - 1);
+    rf[i] = *(const typename Ln::Raw*)((const T*)a.gate + t * a.s.ld_gate + c);
+    rx[i] = *(const typename Ln::Raw*)((const T*)a.x + t * a.s.ld_x + c);
+    rd[i] = *(const typename Ln::Raw*)((const T*)a.dh + t * a.s.ld_h + c);
+  }
+  float mark[V];
+#pragma unroll
+  for (int e = 0; e < V; ++e) mark[e] = a.marks[(size_t)chunk * C + c + e];
+  const Part q = part_of<L>(p, t0, words + w);
+  const unsigned all = L == 32 ? ~0u : (1u << (L & 31)) - 1;
+  const bool plain = q.inside == all && !q.begins && !q.ends;
+  float b[L][V], A[V], h[V], g[V];
+#pragma unroll
+  for (int e = 0; e < V; ++e) { A[e] = 1.f; h[e] = 0.f; g[e] = 0.f; }
+#pragma unroll
+  for (int i = 0; i < L; ++i) {
+    Ln::get(rf[i], b[i]);
+#pragma unroll
+    for (int e = 0; e < V; ++e) b[i][e] = share_of(b[i][e]);
+  }
+  auto initial = [&](int j, float (&v)[V]) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] = a.h0 ? a.h0[p.row(j, C) + c + e] : 0.f;
+  };
+  auto final_gradient = [&](int j, float (&v)[V]) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] = a.dh_last ? a.dh_last[p.row(j, C) + c + e] : 0.f;
+  };
+  auto gradient = [&](int i, float (&d)[V]) { Ln::get(rd[i], d); };
+  int last_seq = q.seq;     // of the part's last token
+  if (plain) {
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+      float x[V];
+      Ln::get(rx[i], x);
+#pragma unroll
+      for (int e = 0; e < V; ++e) { h[e] = step_of(b[i][e], x[e], h[e]); A[e] = fmaf(-b[i][e], A[e], A[e]); }
+    }
+#pragma unroll
+    for (int i = L - 1; i >= 0; --i) {
+      float d[V];
+      gradient(i, d);
+#pragma unroll
+      for (int e = 0; e < V; ++e) { const float D = d[e] + g[e]; g[e] = fmaf(-b[i][e], D, D); }
+    }
+  } else {
+    int j = q.seq;
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+      if (q.begins >> i & 1) {
+        j = p.next(j, t0 + i);
+        initial(j, h);
+      }
+      if (!(q.inside >> i & 1)) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) b[i][e] = 0.f;
+        continue;
+      }
+      float x[V];
+      Ln::get(rx[i], x);
+#pragma unroll
+      for (int e = 0; e < V; ++e) { h[e] = step_of(b[i][e], x[e], h[e]); A[e] = fmaf(-b[i][e], A[e], A[e]); }
+    }
+    last_seq = j;
+#pragma unroll
+    for (int i = L - 1; i >= 0; --i) {
+      if (!(q.inside >> i & 1)) continue;
+      if (q.ends >> i & 1) {
+        j = p.previous(j, t0 + i);
+        final_gradient(j, g);
+      }
+      float d[V];
+      gradient(i, d);
+#pragma unroll
+      for (int e = 0; e < V; ++e) { const float D = d[e] + g[e]; g[e] = fmaf(-b[i][e], D, D); }
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+    effects[w][0][lane * V + e] = A[e];
+    effects[w][1][lane * V + e] = h[e];
+    effects[w][2][lane * V + e] = g[e];
+  }
+  if (lane == 0) cuts[w] = (q.begins ? 1 : 0) | (q.ends ? 2 : 0);
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < V; ++e) h[e] = mark[e];
+  for (int k = 0; k < w; ++k) {
+    const bool fresh = cuts[k] & 1;
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      const float Hk = effects[k][1][lane * V + e];
+      h[e] = fresh ? Hk : fmaf(effects[k][0][lane * V + e], h[e], Hk);
+    }
+  }
+  // what the wavefronts behind this one do together; the last wavefront has the whole chunk's
+  float PA[V], PR[V];
+  bool cut = false;
+#pragma unroll
+  for (int e = 0; e < V; ++e) { PA[e] = 1.f; PR[e] = 0.f; }
+  for (int k = W - 1; k > (w == W - 1 ? -1 : w); --k) {
+    const bool fresh = cuts[k] & 2;
+    cut |= fresh;
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      const float Ak = effects[k][0][lane * V + e], Rk = effects[k][2][lane * V + e];
+      PR[e] = fresh ? Rk : fmaf(Ak, PR[e], Rk);
+      PA[e] *= Ak;
+    }
+  }
+  if (w == W - 1 && chain.chunks > 1) {
+    float in[V] = {};
+    publish<V>(chain, chunk, channel, PA, PR, cut);
+    if (chunk < chain.chunks - 1 && !(q.ends >> (L - 1) & 1)) await<V>(chain, chunk + 1, channel, in);
+#pragma unroll
+    for (int e = 0; e < V; ++e) incoming[lane * V + e] = in[e];
+  }
+  if (chain.chunks > 1) __syncthreads();
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+    const float in = chain.chunks > 1 ? incoming[lane * V + e] : 0.f;
+    g[e] = w == W - 1 ? in : cut ? PR[e] : fmaf(PA[e], in, PR[e]);
+  }
+  float gap[L][V];      // h_{t-1} - x_t
+  auto finish = [&](int i) {
+    float d[V], dx[V], df[V];
+    gradient(i, d);
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      const float D = d[e] + g[e];
+      dx[e] = b[i][e] * D;
+      df[e] = D * gap[i][e] * fmaf(-b[i][e], b[i][e], b[i][e]);
+      g[e] = fmaf(-b[i][e], D, D);
+    }
+    if (!mine) return;
+    *(typename Ln::Raw*)((T*)a.dx + (size_t)(t0 + i) * a.s.ld_dx + c) = Ln::put(dx);
+    *(typename Ln::Raw*)((T*)a.dgate + (size_t)(t0 + i) * a.s.ld_dgate + c) = Ln::put(df);
+  };
+  if (plain) {
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+      float x[V];
+      Ln::get(rx[i], x);
+#pragma unroll
+      for (int e = 0; e < V; ++e) { gap[i][e] = h[e] - x[e]; h[e] = step_of(b[i][e], x[e], h[e]); }
+    }
+#pragma unroll
+    for (int i = L - 1; i >= 0; --i) finish(i);
+  } else {
+    int j = q.seq;
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+      if (q.begins >> i & 1) {
+        j = p.next(j, t0 + i);
+        initial(j, h);
+      }
+      float x[V];
+      Ln::get(rx[i], x);
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        gap[i][e] = h[e] - x[e];
+        if (q.inside >> i & 1) h[e] = step_of(b[i][e], x[e], h[e]);
+      }
+    }
+    j = last_seq;
+#pragma unroll
+    for (int i = L - 1; i >= 0; --i) {
+      if (!(q.inside >> i & 1)) continue;
+      if (q.ends >> i & 1) {
+        j = p.previous(j, t0 + i);
+        final_gradient(j, g);
+      }
+      finish(i);
+      if ((q.begins >> i & 1) && a.dh0 && mine) {
+        const int k = p.previous(j, t0 + i);
+#pragma unroll
+        for (int e = 0; e < V; ++e) a.dh0[p.row(k, C) + c + e] = g[e];
+      }
+    }
+  }
+  if (a.dh0 && p.starts && mine) {
+    const long share = ((long)p.sequences + chain.chunks - 1) / chain.chunks;
+    for (long k = chunk * share + w; k < min((long)p.sequences, (chunk + 1) * share); k += W)
+      if (p.at((int)k) >= p.at((int)k + 1)) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) a.dh0[k * C + c + e] = a.dh_last ? a.dh_last[k * C + c + e] : 0.f;
+      }
+  }
+}
+
+__global__ void copy_or_zero_kernel(const float* x, float* y, size_t n) {
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+  if (i < n) y[i] = x ? x[i] : 0.f;
+}
+
+constexpr int SCAN_SHORT = 32;      // tokens a sequence, on average, up to which a wavefront takes whole ones
+
+// chunks of a call; channels of all blocks whatever a lane has
+uint64_t scan_chunks(uint64_t tokens) { return std::max<uint64_t>(1, (tokens + KARMA_SCAN_MARK - 1) / KARMA_SCAN_MARK); }
+uint64_t scan_width(uint32_t channels) { return ((uint64_t)channels + 127) / 128 * 128; }
 
 // Sizes and strides as a call may give them; a stride of 0 becomes the number of channels.
 int check_scan(karma_scan_shape& s, const void* starts) {
-  if (!s.channels || !s.sequences || s.tokens > INT32_MAX || s.channels > INT32_MAX || s.sequences >= INT32_MAX) return KARMA_E_INVAL;
+  if (!s.channels || !s.sequences || s.tokens > INT32_MAX - 1024 || s.channels > INT32_MAX || s.sequences >= INT32_MAX) return KARMA_E_INVAL;
   if (!starts && s.tokens % s.sequences) return KARMA_E_INVAL;
   for (uint64_t* ld : {&s.ld_gate, &s.ld_x, &s.ld_h, &s.ld_dgate, &s.ld_dx}) {
     if (!*ld) *ld = s.channels;
     if (*ld < s.channels || *ld > INT64_MAX / 8 / (s.tokens + 1)) return KARMA_E_INVAL;
   }
-  if ((uint64_t)((s.channels + 63) / 64) * s.sequences > INT32_MAX) return KARMA_E_INVAL;
+  if ((uint64_t)((s.channels + 63) / 64) * std::max<uint64_t>(s.sequences, scan_chunks(s.tokens) + 1) > INT32_MAX) return KARMA_E_INVAL;
   return KARMA_OK;
 }
 bool aligned_to(const void* p, size_t n) { return (uintptr_t)p % n == 0; }
 
 }  // namespace
 
-size_t gated_scan_ws_bytes(const karma_scan_shape&) { return 0; }
+constexpr size_t CHAIN_HEAD = 256;      // the counter
+
+size_t gated_scan_ws_bytes(const karma_scan_shape& given) {
+  karma_scan_shape shape = given;
+  const int any = 0;      // (whether all sequences have one length does not matter here)
+  if (check_scan(shape, &any)) return 0;
+  const uint64_t chunks = scan_chunks(shape.tokens);
+  return chunks > 1 ? CHAIN_HEAD + chunks * scan_width(shape.channels) * 12 : 0;
+}
+
+static Spans spans_of(const karma_scan_shape& s, const int* starts) {
+  return Spans{starts, (int)s.tokens, (int)s.sequences, starts ? 0 : (int)(s.tokens / s.sequences)};
+}
+// V channels a lane; the chain is cleared by a kernel ahead (a call that is captured has kernels alone)
+static Chain chain_of(const karma_scan_shape& s, int V, void* ws, hipStream_t stream) {
+  const uint64_t chunks = scan_chunks(s.tokens), width = scan_width(s.channels);
+  unsigned long long* effect = (unsigned long long*)((char*)ws + CHAIN_HEAD);
+  const Chain c{(unsigned*)ws, effect, (unsigned*)(effect + chunks * width), (int)chunks, (int)((s.channels + 64 * V - 1) / (64 * V)), (int)width};
+  if (chunks > 1) hipLaunchKernelGGL(chain_clear_kernel, dim3((unsigned)((chunks * width + 255) / 256)), dim3(256), 0, stream, c);
+  return c;
+}
+static unsigned chain_grid(const Chain& c) { return (unsigned)c.blocks * (unsigned)(c.chunks > 1 ? c.chunks + 1 : 1); }
 
 int gated_scan_fwd(ScanFwd a, bool bf16, hipStream_t s) {
   const size_t e = bf16 ? 2 : 4;
   if (int st = check_scan(a.s, a.starts)) return st;
   if (a.s.tokens && (!a.gate || !a.x || !a.h)) return KARMA_E_INVAL;
-  if (!aligned_to(a.gate, e) || !aligned_to(a.x, e) || !aligned_to(a.h, e)) return KARMA_E_INVAL;
+  if (!aligned_to(a.gate, e) || !aligned_to(a.x, e) || !aligned_to(a.h, e) || !aligned_to(a.ws, 16)) return KARMA_E_INVAL;
   if (a.ws_bytes < gated_scan_ws_bytes(a.s)) return KARMA_E_OOM;
-  const dim3 grid((a.s.channels + 63) / 64 * a.s.sequences);
-  if (bf16) hipLaunchKernelGGL(scan_fwd_kernel<bf16_t>, grid, dim3(64), 0, s, a);
-  else hipLaunchKernelGGL(scan_fwd_kernel<float>, grid, dim3(64), 0, s, a);
+  const bool pairs = bf16 && a.s.channels % 2 == 0 && (a.s.ld_gate | a.s.ld_x | a.s.ld_h) % 2 == 0 && aligned_to(a.gate, 4) && aligned_to(a.x, 4) &&
+                     aligned_to(a.h, 4);
+  const Spans p = spans_of(a.s, a.starts);
+  if (a.s.tokens <= (uint64_t)SCAN_SHORT * a.s.sequences) {
+    const int blocks = (int)((a.s.channels + (pairs ? 127 : 63)) / (pairs ? 128 : 64)), units = blocks * (int)a.s.sequences;
+    const dim3 grid((units + 3) / 4);
+    if (pairs) hipLaunchKernelGGL((scan_fwd_short_kernel<bf16_t, 2>), grid, dim3(256), 0, s, a, p, blocks, units);
+    else if (bf16) hipLaunchKernelGGL((scan_fwd_short_kernel<bf16_t, 1>), grid, dim3(256), 0, s, a, p, blocks, units);
+    else hipLaunchKernelGGL((scan_fwd_short_kernel<float, 1>), grid, dim3(256), 0, s, a, p, blocks, units);
+  } else {
+    const Chain c = chain_of(a.s, pairs ? 2 : 1, a.ws, s);
+    const dim3 grid(chain_grid(c));
+    if (pairs) hipLaunchKernelGGL((scan_fwd_kernel<bf16_t, 2, 32, 8>), grid, dim3(512), 0, s, a, p, c);
+    else if (bf16) hipLaunchKernelGGL((scan_fwd_kernel<bf16_t, 1, 32, 8>), grid, dim3(512), 0, s, a, p, c);
+    else hipLaunchKernelGGL((scan_fwd_kernel<float, 1, 32, 8>), grid, dim3(512), 0, s, a, p, c);
+  }
   return hipGetLastError() == hipSuccess ? KARMA_OK : KARMA_E_HIP;
 }
 
@@ -108,11 +703,24 @@ int gated_scan_bwd(ScanBwd a, bool bf16, hipStream_t s) {
   const size_t e = bf16 ? 2 : 4;
   if (int st = check_scan(a.s, a.starts)) return st;
   if (a.s.tokens && (!a.gate || !a.x || !a.marks || !a.dh || !a.dgate || !a.dx)) return KARMA_E_INVAL;
-  if (!aligned_to(a.gate, e) || !aligned_to(a.x, e) || !aligned_to(a.dh, e) || !aligned_to(a.dgate, e) || !aligned_to(a.dx, e)) return KARMA_E_INVAL;
+  if (!aligned_to(a.gate, e) || !aligned_to(a.x, e) || !aligned_to(a.dh, e) || !aligned_to(a.dgate, e) || !aligned_to(a.dx, e) ||
+      !aligned_to(a.ws, 16)) return KARMA_E_INVAL;
   if (a.ws_bytes < gated_scan_ws_bytes(a.s)) return KARMA_E_OOM;
-  const dim3 grid((a.s.channels + 63) / 64 * a.s.sequences);
-  if (bf16) hipLaunchKernelGGL(scan_bwd_kernel<bf16_t>, grid, dim3(64), 0, s, a);
-  else hipLaunchKernelGGL(scan_bwd_kernel<float>, grid, dim3(64), 0, s, a);
+  if (!a.s.tokens) {      // the gradient of a state that no token changed
+    if (!a.dh0) return KARMA_OK;
+    const size_t n = (size_t)a.s.sequences * a.s.channels;
+    if (n > (size_t)INT32_MAX * 256) return KARMA_E_INVAL;
+    hipLaunchKernelGGL(copy_or_zero_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, a.dh_last, a.dh0, n);
+    return hipGetLastError() == hipSuccess ? KARMA_OK : KARMA_E_HIP;
+  }
+  const bool pairs = bf16 && a.s.channels % 2 == 0 && (a.s.ld_gate | a.s.ld_x | a.s.ld_h | a.s.ld_dgate | a.s.ld_dx) % 2 == 0 &&
+                     aligned_to(a.gate, 4) && aligned_to(a.x, 4) && aligned_to(a.dh, 4) && aligned_to(a.dgate, 4) && aligned_to(a.dx, 4);
+  const Spans p = spans_of(a.s, a.starts);
+  const Chain c = chain_of(a.s, pairs ? 2 : 1, a.ws, s);
+  const dim3 grid(chain_grid(c));
+  if (pairs) hipLaunchKernelGGL((scan_bwd_kernel<bf16_t, 2, 16, 16>), grid, dim3(1024), 0, s, a, p, c);
+  else if (bf16) hipLaunchKernelGGL((scan_bwd_kernel<bf16_t, 1, 16, 16>), grid, dim3(1024), 0, s, a, p, c);
+  else hipLaunchKernelGGL((scan_bwd_kernel<float, 1, 16, 16>), grid, dim3(1024), 0, s, a, p, c);
   return hipGetLastError() == hipSuccess ? KARMA_OK : KARMA_E_HIP;
 }
 

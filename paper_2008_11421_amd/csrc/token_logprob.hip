@@ -537,7 +537,7 @@ struct LogprobCut { unsigned waves, parts; };
 LogprobCut cut_rows(uint32_t rows, uint32_t cols, bool bf16) {
   const uint32_t vectors = cols / (bf16 ? 8 : 4);
   const uint64_t parts = std::min<uint64_t>((2048 + rows - 1) / std::max(rows, 1u), vectors / LP_THREADS);
-  if (parts <= 1) return LogprobCut{vectors <= LP_THREADS ? 1u : (unsigned)LP_WAVES, 1};
+  if (parts <= 1) return LogprobCut{vectors <= (rows >= 4096 ? 512u : (unsigned)LP_THREADS) ? 1u : (unsigned)LP_WAVES, 1};
   return LogprobCut{(unsigned)LP_WAVES, (unsigned)parts};
 }
 size_t up16(size_t b) { return (b + 15) / 16 * 16; }

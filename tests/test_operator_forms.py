@@ -99,7 +99,7 @@ def test_scan_refusals():
     good = dict(tokens=512, channels=8, sequences=2)
     S = lambda **k: K.ScanShape(**{**good, **k})
     assert scan_fwd(None) == K.E_INVAL
-    for bad in (dict(channels=0), dict(sequences=0), dict(tokens=511), dict(tokens=1 << 31), dict(ld_gate=7), dict(ld_x=4), dict(ld_h=1),
+    for bad in (dict(channels=0), dict(sequences=0), dict(tokens=511), dict(tokens=(1 << 31) - 1024), dict(ld_gate=7), dict(ld_x=4), dict(ld_h=1),
                 dict(ld_dx=7), dict(channels=1 << 31), dict(ld_gate=1 << 62)):
         assert scan_fwd(S(**bad)) == K.E_INVAL, bad
         assert K.gated_scan_ws_bytes(S(**bad)) == 0 or bad == dict(tokens=511), bad
