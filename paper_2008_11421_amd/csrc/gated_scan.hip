@@ -42,6 +42,18 @@ struct Lane<float, 1> {
 __device__ __forceinline__ float share_of(float f) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(f * 1.44269504f)); }
 __device__ __forceinline__ float step_of(float b, float x, float h) { return fmaf(b, x - h, h); }
 
+// The compiler is not to keep what it made of a value that is used again later: the unpacked inputs of two runs through a part, and the
+// addresses of all its rows, would take twice the registers (240 instead of 120 in the forward kernel).
+template <typename R>
+__device__ __forceinline__ R as_new(R r) {
+  asm volatile("" : "+v"(r));
+  return r;
+}
+__device__ __forceinline__ int as_new_scalar(int i) {
+  asm volatile("" : "+s"(i));
+  return i;
+}
+
 // ---- sequences -------------------------------------------------------------------------------------------------
 struct Spans {
   const int* starts;
@@ -65,12 +77,10 @@ struct Spans {
   }
   // from sequence j on to the one that token t begins, or back to the one that token t ends
   __device__ __forceinline__ int next(int j, int t) const {
-    if (!starts) return t / each;
     while (j + 1 < sequences && at(j + 1) <= t) ++j;
     return j;
   }
   __device__ __forceinline__ int previous(int j, int t) const {
-    if (!starts) return t / each;
     while (j > 0 && at(j) > t) --j;
     return j;
   }
@@ -84,6 +94,15 @@ struct Part {
   unsigned inside;      // that belong to one
   int seq;              // the last sequence that begins at or before t0
 };
+// Runs of tokens of one sequence: the one that begins with the lowest token left, and the one that ends with the highest.
+__device__ __forceinline__ unsigned first_run(const Part& q, unsigned left) {
+  const unsigned later = q.begins & left & (left - 1);      // (the lowest token left, if it begins one, begins this run)
+  return later ? left & ((later & -later) - 1) : left;
+}
+__device__ __forceinline__ unsigned last_run(const Part& q, unsigned left) {
+  const unsigned earlier = q.ends & left & ~(0x80000000u >> __builtin_clz(left));
+  return earlier ? left & ~((0xffffffffu >> __builtin_clz(earlier))) : left;
+}
 // word: 8 bytes of LDS of the wavefront's own
 template <int L>
 __device__ __forceinline__ Part part_of(const Spans& p, int t0, unsigned long long* word) {
@@ -191,10 +210,11 @@ __device__ __forceinline__ void carry(const Chain& c, int channel, bool up) {
     if (done != before) n = 0;
   }
 }
-__global__ void chain_clear_kernel(Chain c) {
-  const size_t n = (size_t)c.chunks * c.width, i = (size_t)blockIdx.x * blockDim.x + threadIdx.x;
+// all words behind the counter, 12 bytes a chunk and channel, widths being multiples of 128
+__global__ __launch_bounds__(256) void chain_clear_kernel(Chain c, size_t pieces) {
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
   if (i == 0) *c.ticket = 0;
-  if (i < n) { c.effect[i] = ~0ull; c.state[i] = ~0u; }
+  if (i < pieces) ((u32x4*)c.effect)[i] = u32x4{~0u, ~0u, ~0u, ~0u};
 }
 
 // The work of this workgroup: a chunk and a block of channels, or false for a carrier, which has then done its work.
@@ -222,7 +242,7 @@ __device__ __forceinline__ bool take_work(const Chain& c, bool up, int& chunk, i
 // W wavefronts have the chunk's tokens one part behind the other, L each, a lane V channels, everything in registers: one pass over
 // memory.  Each runs through its part once for A and H, and, when the state before it is known, again for the states themselves.
 template <typename T, int V, int L, int W>
-__global__ __launch_bounds__(64 * W) void scan_fwd_kernel(ScanFwd a, Spans p, Chain chain) {
+__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(4))) void scan_fwd_kernel(ScanFwd a, Spans p, Chain chain) {
   typedef Lane<T, V> Ln;
   static_assert(L * W == KARMA_SCAN_MARK, "a chunk is what lies between two marks");
   __shared__ float effects[W][2][64 * V];
@@ -418,12 +438,12 @@ __global__ __launch_bounds__(256) void scan_fwd_short_kernel(ScanFwd a, Spans p,
 // ---- backward ---------------------------------------------------------------------------------------------------
 // As forward, with the chain from the last chunk to the first: the gradient g of the state behind a part goes in, that of the state
 // before it comes out, out = A g + R.  The states are run through again from the chunk's mark.
-template <typename T, int V, int L, int W>
-__global__ __launch_bounds__(64 * W) void scan_bwd_kernel(ScanBwd a, Spans p, Chain chain) {
+template <typename T, int V, int L, int W, bool STATES>
+__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(5))) void scan_bwd_kernel(ScanBwd a, Spans p, Chain chain) {
   typedef Lane<T, V> Ln;
   static_assert(L * W == KARMA_SCAN_MARK, "a chunk is what lies between two marks");
   __shared__ float effects[W][3][64 * V];
-  __shared__ float incoming[64 * V];
+  __shared__ float incoming[64 * V], marks[64 * V];
   __shared__ unsigned long long words[W];
   __shared__ int cuts[W];       // 1: a sequence begins in the part, 2: one ends in it
   int chunk, block;
@@ -440,12 +460,11 @@ __global__ __launch_bounds__(64 * W) void scan_bwd_kernel(ScanBwd a, Spans p, Ch
     rx[i] = *(const typename Ln::Raw*)((const T*)a.x + t * a.s.ld_x + c);
     rd[i] = *(const typename Ln::Raw*)((const T*)a.dh + t * a.s.ld_h + c);
   }
-  float mark[V];
+  if (w == 0) {
 #pragma unroll
-  for (int e = 0; e < V; ++e) mark[e] = a.marks[(size_t)chunk * C + c + e];
+    for (int e = 0; e < V; ++e) marks[lane * V + e] = a.marks[(size_t)chunk * C + c + e];
+  }
   const Part q = part_of<L>(p, t0, words + w);
-  const unsigned all = L == 32 ? ~0u : (1u << (L & 31)) - 1;
-  const bool plain = q.inside == all && !q.begins && !q.ends;
   float b[L][V], A[V], h[V], g[V];
 #pragma unroll
   for (int e = 0; e < V; ++e) { A[e] = 1.f; h[e] = 0.f; g[e] = 0.f; }
@@ -453,64 +472,45 @@ __global__ __launch_bounds__(64 * W) void scan_bwd_kernel(ScanBwd a, Spans p, Ch
   for (int i = 0; i < L; ++i) {
     Ln::get(rf[i], b[i]);
 #pragma unroll
-    for (int e = 0; e < V; ++e) b[i][e] = share_of(b[i][e]);
+    for (int e = 0; e < V; ++e) b[i][e] = q.inside >> i & 1 ? share_of(b[i][e]) : 0.f;
   }
   auto initial = [&](int j, float (&v)[V]) {
 #pragma unroll
-    for (int e = 0; e < V; ++e) v[e] = a.h0 ? a.h0[p.row(j, C) + c + e] : 0.f;
+    for (int e = 0; e < V; ++e) v[e] = STATES && a.h0 ? a.h0[p.row(j, C) + c + e] : 0.f;
   };
   auto final_gradient = [&](int j, float (&v)[V]) {
 #pragma unroll
-    for (int e = 0; e < V; ++e) v[e] = a.dh_last ? a.dh_last[p.row(j, C) + c + e] : 0.f;
+    for (int e = 0; e < V; ++e) v[e] = STATES && a.dh_last ? a.dh_last[p.row(j, C) + c + e] : 0.f;
   };
-  auto gradient = [&](int i, float (&d)[V]) { Ln::get(rd[i], d); };
-  int last_seq = q.seq;     // of the part's last token
-  if (plain) {
+  auto step = [&](int i) {
+    float x[V];
+    Ln::get(as_new(rx[i]), x);
 #pragma unroll
-    for (int i = 0; i < L; ++i) {
-      float x[V];
-      Ln::get(rx[i], x);
+    for (int e = 0; e < V; ++e) { h[e] = step_of(b[i][e], x[e], h[e]); A[e] = fmaf(-b[i][e], A[e], A[e]); }
+  };
+  auto back = [&](int i) {
+    float d[V];
+    Ln::get(as_new(rd[i]), d);
 #pragma unroll
-      for (int e = 0; e < V; ++e) { h[e] = step_of(b[i][e], x[e], h[e]); A[e] = fmaf(-b[i][e], A[e], A[e]); }
+    for (int e = 0; e < V; ++e) { const float D = d[e] + g[e]; g[e] = fmaf(-b[i][e], D, D); }
+  };
+  int j = q.seq;
+#pragma unroll
+  for (int i = 0; i < L; ++i) {
+    if (q.begins >> i & 1) {
+      if (STATES) j = p.next(j, t0 + i);
+      initial(j, h);
     }
+    step(i);
+  }
+  const int last_seq = j;     // of the part's last token
 #pragma unroll
-    for (int i = L - 1; i >= 0; --i) {
-      float d[V];
-      gradient(i, d);
-#pragma unroll
-      for (int e = 0; e < V; ++e) { const float D = d[e] + g[e]; g[e] = fmaf(-b[i][e], D, D); }
+  for (int i = L - 1; i >= 0; --i) {
+    if (q.ends >> i & 1) {
+      if (STATES) j = p.previous(j, t0 + i);
+      final_gradient(j, g);
     }
-  } else {
-    int j = q.seq;
-#pragma unroll
-    for (int i = 0; i < L; ++i) {
-      if (q.begins >> i & 1) {
-        j = p.next(j, t0 + i);
-        initial(j, h);
-      }
-      if (!(q.inside >> i & 1)) {
-#pragma unroll
-        for (int e = 0; e < V; ++e) b[i][e] = 0.f;
-        continue;
-      }
-      float x[V];
-      Ln::get(rx[i], x);
-#pragma unroll
-      for (int e = 0; e < V; ++e) { h[e] = step_of(b[i][e], x[e], h[e]); A[e] = fmaf(-b[i][e], A[e], A[e]); }
-    }
-    last_seq = j;
-#pragma unroll
-    for (int i = L - 1; i >= 0; --i) {
-      if (!(q.inside >> i & 1)) continue;
-      if (q.ends >> i & 1) {
-        j = p.previous(j, t0 + i);
-        final_gradient(j, g);
-      }
-      float d[V];
-      gradient(i, d);
-#pragma unroll
-      for (int e = 0; e < V; ++e) { const float D = d[e] + g[e]; g[e] = fmaf(-b[i][e], D, D); }
-    }
+    back(i);
   }
 #pragma unroll
   for (int e = 0; e < V; ++e) {
@@ -521,7 +521,7 @@ __global__ __launch_bounds__(64 * W) void scan_bwd_kernel(ScanBwd a, Spans p, Ch
   if (lane == 0) cuts[w] = (q.begins ? 1 : 0) | (q.ends ? 2 : 0);
   __syncthreads();
 #pragma unroll
-  for (int e = 0; e < V; ++e) h[e] = mark[e];
+  for (int e = 0; e < V; ++e) h[e] = marks[lane * V + e];
   for (int k = 0; k < w; ++k) {
     const bool fresh = cuts[k] & 1;
 #pragma unroll
@@ -559,63 +559,52 @@ __global__ __launch_bounds__(64 * W) void scan_bwd_kernel(ScanBwd a, Spans p, Ch
     g[e] = w == W - 1 ? in : cut ? PR[e] : fmaf(PA[e], in, PR[e]);
   }
   float gap[L][V];      // h_{t-1} - x_t
+  auto part_from = [&](int i) {
+    float x[V];
+    Ln::get(as_new(rx[i]), x);
+#pragma unroll
+    for (int e = 0; e < V; ++e) { gap[i][e] = h[e] - x[e]; h[e] = fmaf(-b[i][e], gap[i][e], h[e]); }
+  };
   auto finish = [&](int i) {
     float d[V], dx[V], df[V];
-    gradient(i, d);
+    Ln::get(as_new(rd[i]), d);
 #pragma unroll
     for (int e = 0; e < V; ++e) {
       const float D = d[e] + g[e];
       dx[e] = b[i][e] * D;
-      df[e] = D * gap[i][e] * fmaf(-b[i][e], b[i][e], b[i][e]);
-      g[e] = fmaf(-b[i][e], D, D);
+      const float own = as_new(b[i][e]);     // (as above: the product that follows)
+      df[e] = D * gap[i][e] * fmaf(-own, own, own);
+      g[e] = D - dx[e];
     }
-    if (!mine) return;
-    *(typename Ln::Raw*)((T*)a.dx + (size_t)(t0 + i) * a.s.ld_dx + c) = Ln::put(dx);
-    *(typename Ln::Raw*)((T*)a.dgate + (size_t)(t0 + i) * a.s.ld_dgate + c) = Ln::put(df);
+    if (!mine || !(q.inside >> i & 1)) return;
+    const size_t t = as_new_scalar(t0 + i);
+    *(typename Ln::Raw*)((T*)a.dx + t * a.s.ld_dx + c) = Ln::put(dx);
+    *(typename Ln::Raw*)((T*)a.dgate + t * a.s.ld_dgate + c) = Ln::put(df);
   };
-  if (plain) {
+  j = q.seq;
 #pragma unroll
-    for (int i = 0; i < L; ++i) {
-      float x[V];
-      Ln::get(rx[i], x);
-#pragma unroll
-      for (int e = 0; e < V; ++e) { gap[i][e] = h[e] - x[e]; h[e] = step_of(b[i][e], x[e], h[e]); }
+  for (int i = 0; i < L; ++i) {
+    if (q.begins >> i & 1) {
+      if (STATES) j = p.next(j, t0 + i);
+      initial(j, h);
     }
+    part_from(i);
+  }
+  j = last_seq;
 #pragma unroll
-    for (int i = L - 1; i >= 0; --i) finish(i);
-  } else {
-    int j = q.seq;
-#pragma unroll
-    for (int i = 0; i < L; ++i) {
-      if (q.begins >> i & 1) {
-        j = p.next(j, t0 + i);
-        initial(j, h);
-      }
-      float x[V];
-      Ln::get(rx[i], x);
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        gap[i][e] = h[e] - x[e];
-        if (q.inside >> i & 1) h[e] = step_of(b[i][e], x[e], h[e]);
-      }
+  for (int i = L - 1; i >= 0; --i) {
+    if (q.ends >> i & 1) {
+      if (STATES) j = p.previous(j, t0 + i);
+      final_gradient(j, g);
     }
-    j = last_seq;
+    finish(i);
+    if (STATES && (q.begins >> i & 1) && a.dh0 && mine) {
+      j = p.previous(j, t0 + i);
 #pragma unroll
-    for (int i = L - 1; i >= 0; --i) {
-      if (!(q.inside >> i & 1)) continue;
-      if (q.ends >> i & 1) {
-        j = p.previous(j, t0 + i);
-        final_gradient(j, g);
-      }
-      finish(i);
-      if ((q.begins >> i & 1) && a.dh0 && mine) {
-        const int k = p.previous(j, t0 + i);
-#pragma unroll
-        for (int e = 0; e < V; ++e) a.dh0[p.row(k, C) + c + e] = g[e];
-      }
+      for (int e = 0; e < V; ++e) a.dh0[p.row(j, C) + c + e] = g[e];
     }
   }
-  if (a.dh0 && p.starts && mine) {
+  if (STATES && a.dh0 && p.starts && mine) {
     const long share = ((long)p.sequences + chain.chunks - 1) / chain.chunks;
     for (long k = chunk * share + w; k < min((long)p.sequences, (chunk + 1) * share); k += W)
       if (p.at((int)k) >= p.at((int)k + 1)) {
@@ -669,7 +658,8 @@ static Chain chain_of(const karma_scan_shape& s, int V, void* ws, hipStream_t st
   const uint64_t chunks = scan_chunks(s.tokens), width = scan_width(s.channels);
   unsigned long long* effect = (unsigned long long*)((char*)ws + CHAIN_HEAD);
   const Chain c{(unsigned*)ws, effect, (unsigned*)(effect + chunks * width), (int)chunks, (int)((s.channels + 64 * V - 1) / (64 * V)), (int)width};
-  if (chunks > 1) hipLaunchKernelGGL(chain_clear_kernel, dim3((unsigned)((chunks * width + 255) / 256)), dim3(256), 0, stream, c);
+  const size_t pieces = chunks * width * 12 / 16;
+  if (chunks > 1) hipLaunchKernelGGL(chain_clear_kernel, dim3((unsigned)((pieces + 255) / 256)), dim3(256), 0, stream, c, pieces);
   return c;
 }
 static unsigned chain_grid(const Chain& c) { return (unsigned)c.blocks * (unsigned)(c.chunks > 1 ? c.chunks + 1 : 1); }
@@ -718,9 +708,16 @@ int gated_scan_bwd(ScanBwd a, bool bf16, hipStream_t s) {
   const Spans p = spans_of(a.s, a.starts);
   const Chain c = chain_of(a.s, pairs ? 2 : 1, a.ws, s);
   const dim3 grid(chain_grid(c));
-  if (pairs) hipLaunchKernelGGL((scan_bwd_kernel<bf16_t, 2, 16, 16>), grid, dim3(1024), 0, s, a, p, c);
-  else if (bf16) hipLaunchKernelGGL((scan_bwd_kernel<bf16_t, 1, 16, 16>), grid, dim3(1024), 0, s, a, p, c);
-  else hipLaunchKernelGGL((scan_bwd_kernel<float, 1, 16, 16>), grid, dim3(1024), 0, s, a, p, c);
+#define KARMA_SCAN_BWD(T, V)                                                                                           \
+  do {                                                                                                                 \
+    if (states) hipLaunchKernelGGL((scan_bwd_kernel<T, V, 16, 16, true>), grid, dim3(1024), 0, s, a, p, c);            \
+    else hipLaunchKernelGGL((scan_bwd_kernel<T, V, 16, 16, false>), grid, dim3(1024), 0, s, a, p, c);                  \
+  } while (0)
+  const bool states = a.h0 || a.dh_last || a.dh0;
+  if (pairs) KARMA_SCAN_BWD(bf16_t, 2);
+  else if (bf16) KARMA_SCAN_BWD(bf16_t, 1);
+  else KARMA_SCAN_BWD(float, 1);
+#undef KARMA_SCAN_BWD
   return hipGetLastError() == hipSuccess ? KARMA_OK : KARMA_E_HIP;
 }
 

@@ -198,6 +198,19 @@ def test_a_sequence_that_is_lost_stays_alone(torch, tokens, sequences):
         assert not torch.isfinite(t[per:2 * per]).all()
 
 
+@pytest.mark.parametrize("state", [True, False])
+@pytest.mark.parametrize("starts,tokens", [([0, 300, 1000], 1500), ([0, 1, 600], 602), ([0, 512], 1100), ([0, 4, 7], 300), ([0, 2, 2], 9)])
+def test_what_lies_behind_the_last_sequence_is_not_looked_at(torch, starts, tokens, state):
+    p = Problem(torch, 25, tokens, 64, len(starts) - 1, starts, state=state)
+    for t, v in ((p.gate, "nan"), (p.x, "inf"), (p.dh, "nan")):
+        t[starts[-1]:] = float(v)
+    p.forward()
+    p.backward()
+    for t in (p.gate, p.x, p.dh):
+        t[starts[-1]:] = 0      # (the plain form has to be able to subtract)
+    p.check()
+
+
 @pytest.mark.parametrize("tokens,sequences,starts", [(2100, 3, None), (64, 64, None), (2000, 4, [0, 900, 901, 901, 1990])])
 def test_in_place(torch, tokens, sequences, starts):
     a = Problem(torch, 16, tokens, 132, sequences, starts)
