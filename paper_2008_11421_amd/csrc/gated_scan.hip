@@ -244,7 +244,8 @@ __device__ __forceinline__ bool take_work(const Chain& c, bool up, int& chunk, i
 template <typename T, int V, int L, int W>
 __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(4))) void scan_fwd_kernel(ScanFwd a, Spans p, Chain chain) {
   typedef Lane<T, V> Ln;
-  static_assert(L * W == KARMA_SCAN_MARK, "a chunk is what lies between two marks");
+  constexpr int TOKENS = L * W;
+  static_assert(KARMA_SCAN_MARK % L == 0, "marks lie between the wavefronts' parts");
   __shared__ float effects[W][2][64 * V];
   __shared__ float incoming[64 * V];
   __shared__ unsigned long long words[W];
@@ -254,7 +255,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(4))) voi
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), C = (int)a.s.channels;
   const int channel = block * 64 * V + lane * V, c = channel < C ? channel : C - V;     // (lanes without a channel repeat the last one)
   const bool mine = channel < C;
-  const int t0 = chunk * KARMA_SCAN_MARK + w * L;
+  const int t0 = chunk * TOKENS + w * L;
   typename Ln::Raw rf[L], rx[L];
 #pragma unroll
   for (int i = 0; i < L; ++i) {
@@ -340,9 +341,9 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(4))) voi
     const float in = chain.chunks > 1 ? incoming[lane * V + e] : 0.f;
     h[e] = w == 0 ? in : cut ? PH[e] : fmaf(PA[e], in, PH[e]);
   }
-  if (w == 0 && a.marks && mine) {
+  if (a.marks && mine && t0 % KARMA_SCAN_MARK == 0 && t0 < p.tokens) {
 #pragma unroll
-    for (int e = 0; e < V; ++e) a.marks[(size_t)chunk * C + c + e] = h[e];
+    for (int e = 0; e < V; ++e) a.marks[(size_t)(t0 / KARMA_SCAN_MARK) * C + c + e] = h[e];
   }
   auto store = [&](int i) {
     if (mine) *(typename Ln::Raw*)((T*)a.h + (size_t)(t0 + i) * a.s.ld_h + c) = Ln::put(h);
@@ -619,10 +620,18 @@ __global__ void copy_or_zero_kernel(const float* x, float* y, size_t n) {
   if (i < n) y[i] = x ? x[i] : 0.f;
 }
 
-constexpr int SCAN_SHORT = 32;      // tokens a sequence, on average, up to which a wavefront takes whole ones
+// Whether wavefronts take whole sequences (`units` of them).  Sequences of one length, 1024 channels in bf16, us by whole sequences /
+// in chunks: 4096 x 1 token 17.9 / 41.8, 64 x 32 8.0 / 15.7, 64 x 64 14.9 / 17.3, 64 x 128 26.2 / 26.3, 16 x 64 12.6 / 15.0,
+// 16 x 256 47.9 / 16.7; with many sequences 512 x 64 42.8 / 65.6, 256 x 128 43.1 / 64.5, 128 x 256 63.2 / 63.9.  Packed ones can have one
+// much longer than the others, which a single wavefront would be left alone with: half as many tokens on average.
+bool whole_sequences(const karma_scan_shape& s, bool packed, uint64_t units) {
+  const uint64_t most = packed ? 32 : units >= 2048 ? 128 : 64;
+  return s.tokens <= most * s.sequences;
+}
 
 // chunks of a call; channels of all blocks whatever a lane has
-uint64_t scan_chunks(uint64_t tokens) { return std::max<uint64_t>(1, (tokens + KARMA_SCAN_MARK - 1) / KARMA_SCAN_MARK); }
+uint64_t scan_chunks(uint64_t tokens, int per) { return std::max<uint64_t>(1, (tokens + per - 1) / per); }
+constexpr int FWD_TOKENS = 256;    // of a forward chunk
 uint64_t scan_width(uint32_t channels) { return ((uint64_t)channels + 127) / 128 * 128; }
 
 // Sizes and strides as a call may give them; a stride of 0 becomes the number of channels.
@@ -633,7 +642,7 @@ int check_scan(karma_scan_shape& s, const void* starts) {
     if (!*ld) *ld = s.channels;
     if (*ld < s.channels || *ld > INT64_MAX / 8 / (s.tokens + 1)) return KARMA_E_INVAL;
   }
-  if ((uint64_t)((s.channels + 63) / 64) * std::max<uint64_t>(s.sequences, scan_chunks(s.tokens) + 1) > INT32_MAX) return KARMA_E_INVAL;
+  if ((uint64_t)((s.channels + 63) / 64) * std::max<uint64_t>(s.sequences, scan_chunks(s.tokens, FWD_TOKENS) + 1) > INT32_MAX) return KARMA_E_INVAL;
   return KARMA_OK;
 }
 bool aligned_to(const void* p, size_t n) { return (uintptr_t)p % n == 0; }
@@ -646,7 +655,7 @@ size_t gated_scan_ws_bytes(const karma_scan_shape& given) {
   karma_scan_shape shape = given;
   const int any = 0;      // (whether all sequences have one length does not matter here)
   if (check_scan(shape, &any)) return 0;
-  const uint64_t chunks = scan_chunks(shape.tokens);
+  const uint64_t chunks = scan_chunks(shape.tokens, FWD_TOKENS);
   return chunks > 1 ? CHAIN_HEAD + chunks * scan_width(shape.channels) * 12 : 0;
 }
 
@@ -654,8 +663,8 @@ static Spans spans_of(const karma_scan_shape& s, const int* starts) {
   return Spans{starts, (int)s.tokens, (int)s.sequences, starts ? 0 : (int)(s.tokens / s.sequences)};
 }
 // V channels a lane; the chain is cleared by a kernel ahead (a call that is captured has kernels alone)
-static Chain chain_of(const karma_scan_shape& s, int V, void* ws, hipStream_t stream) {
-  const uint64_t chunks = scan_chunks(s.tokens), width = scan_width(s.channels);
+static Chain chain_of(const karma_scan_shape& s, int V, int per, void* ws, hipStream_t stream) {
+  const uint64_t chunks = scan_chunks(s.tokens, per), width = scan_width(s.channels);
   unsigned long long* effect = (unsigned long long*)((char*)ws + CHAIN_HEAD);
   const Chain c{(unsigned*)ws, effect, (unsigned*)(effect + chunks * width), (int)chunks, (int)((s.channels + 64 * V - 1) / (64 * V)), (int)width};
   const size_t pieces = chunks * width * 12 / 16;
@@ -673,18 +682,18 @@ int gated_scan_fwd(ScanFwd a, bool bf16, hipStream_t s) {
   const bool pairs = bf16 && a.s.channels % 2 == 0 && (a.s.ld_gate | a.s.ld_x | a.s.ld_h) % 2 == 0 && aligned_to(a.gate, 4) && aligned_to(a.x, 4) &&
                      aligned_to(a.h, 4);
   const Spans p = spans_of(a.s, a.starts);
-  if (a.s.tokens <= (uint64_t)SCAN_SHORT * a.s.sequences) {
-    const int blocks = (int)((a.s.channels + (pairs ? 127 : 63)) / (pairs ? 128 : 64)), units = blocks * (int)a.s.sequences;
+  const int blocks = (int)((a.s.channels + (pairs ? 127 : 63)) / (pairs ? 128 : 64)), units = blocks * (int)a.s.sequences;
+  if (whole_sequences(a.s, a.starts != nullptr, units)) {
     const dim3 grid((units + 3) / 4);
     if (pairs) hipLaunchKernelGGL((scan_fwd_short_kernel<bf16_t, 2>), grid, dim3(256), 0, s, a, p, blocks, units);
     else if (bf16) hipLaunchKernelGGL((scan_fwd_short_kernel<bf16_t, 1>), grid, dim3(256), 0, s, a, p, blocks, units);
     else hipLaunchKernelGGL((scan_fwd_short_kernel<float, 1>), grid, dim3(256), 0, s, a, p, blocks, units);
   } else {
-    const Chain c = chain_of(a.s, pairs ? 2 : 1, a.ws, s);
+    const Chain c = chain_of(a.s, pairs ? 2 : 1, FWD_TOKENS, a.ws, s);
     const dim3 grid(chain_grid(c));
-    if (pairs) hipLaunchKernelGGL((scan_fwd_kernel<bf16_t, 2, 32, 8>), grid, dim3(512), 0, s, a, p, c);
-    else if (bf16) hipLaunchKernelGGL((scan_fwd_kernel<bf16_t, 1, 32, 8>), grid, dim3(512), 0, s, a, p, c);
-    else hipLaunchKernelGGL((scan_fwd_kernel<float, 1, 32, 8>), grid, dim3(512), 0, s, a, p, c);
+    if (pairs) hipLaunchKernelGGL((scan_fwd_kernel<bf16_t, 2, 32, FWD_TOKENS / 32>), grid, dim3(FWD_TOKENS * 2), 0, s, a, p, c);
+    else if (bf16) hipLaunchKernelGGL((scan_fwd_kernel<bf16_t, 1, 32, FWD_TOKENS / 32>), grid, dim3(FWD_TOKENS * 2), 0, s, a, p, c);
+    else hipLaunchKernelGGL((scan_fwd_kernel<float, 1, 32, FWD_TOKENS / 32>), grid, dim3(FWD_TOKENS * 2), 0, s, a, p, c);
   }
   return hipGetLastError() == hipSuccess ? KARMA_OK : KARMA_E_HIP;
 }
@@ -706,7 +715,7 @@ int gated_scan_bwd(ScanBwd a, bool bf16, hipStream_t s) {
   const bool pairs = bf16 && a.s.channels % 2 == 0 && (a.s.ld_gate | a.s.ld_x | a.s.ld_h | a.s.ld_dgate | a.s.ld_dx) % 2 == 0 &&
                      aligned_to(a.gate, 4) && aligned_to(a.x, 4) && aligned_to(a.dh, 4) && aligned_to(a.dgate, 4) && aligned_to(a.dx, 4);
   const Spans p = spans_of(a.s, a.starts);
-  const Chain c = chain_of(a.s, pairs ? 2 : 1, a.ws, s);
+  const Chain c = chain_of(a.s, pairs ? 2 : 1, KARMA_SCAN_MARK, a.ws, s);
   const dim3 grid(chain_grid(c));
 #define KARMA_SCAN_BWD(T, V)                                                                                           \
   do {                                                                                                                 \
