@@ -8,9 +8,7 @@
 // place and the call's seed.  v > 0 never becomes code 0: m over eps alone would be a huge step.
 #include <hip/hip_runtime.h>
 
-#include <algorithm>
 #include <cmath>
-#include <cstring>
 
 #include "device_utils.h"
 #include "karma.h"
@@ -19,21 +17,45 @@
 namespace karma {
 namespace {
 
-constexpr int ADAMW_TENSORS = 44;       // of one launch: their descriptors travel as kernel arguments (4 KB)
-
+// The tensors of one launch: their descriptors travel as kernel arguments, 4 KB in all.
+template <bool EIGHT>
+struct AdamwTensor {
+  float* w; void* m; void* v; const void* grad; void* out;
+  size_t n;
+  float decay;
+  unsigned flags;
+};
+template <>
+struct AdamwTensor<true> : AdamwTensor<false> {
+  float* m_scale; float* v_scale;
+  unsigned key;     // of the tensor's random bits, the seed aside
+};
+template <bool EIGHT>
 struct AdamwSet {
-  karma_adamw_tensor t[ADAMW_TENSORS];
-  unsigned first[ADAMW_TENSORS + 1];    // tensor k has workgroups [first[k], first[k + 1])
-  unsigned key[ADAMW_TENSORS];          // of the tensor's random bits, the seed aside
+  static constexpr int MOST = EIGHT ? 46 : 66;
+  AdamwTensor<EIGHT> t[MOST];
+  unsigned first[MOST + 1];     // tensor k has workgroups [first[k], first[k + 1])
   int n;
 };
 struct AdamwNow {
   float lr, beta1, beta2, eps, grad_scale;
-  float c1, k2;                         // not with live
+  float c1, k2;                 // not with live
   unsigned seed;
   const karma_adamw_live* live;
 };
-static_assert(sizeof(AdamwSet) + sizeof(AdamwNow) <= 4096, "kernel arguments");
+static_assert(sizeof(AdamwSet<false>) + sizeof(AdamwNow) <= 4096 && sizeof(AdamwSet<true>) + sizeof(AdamwNow) <= 4096, "kernel arguments");
+
+// the tensor of this workgroup
+template <typename Set>
+__device__ __forceinline__ int tensor_of(const Set& u) {
+  int lo = 0, hi = u.n - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) / 2;
+    if (blockIdx.x >= u.first[mid]) lo = mid;
+    else hi = mid - 1;
+  }
+  return lo;
+}
 
 // 1 - beta^step by repeated squaring: one rounding a multiplication, the same on the host and on the device
 __host__ __device__ inline double one_minus_power(float beta, unsigned long long step) {
@@ -164,112 +186,88 @@ __device__ __forceinline__ Codes quantised_step(const Codes& c, const f32x4& g, 
   return r;
 }
 
-// A workgroup has ITER * 1024 consecutive values, a lane four of each 1024: 16-byte accesses of the fp32 buffers.  Reads and
-// writes 28 bytes a value (bf16 gradient and weight), 16.25 with 8-bit moments: bound by memory.
-template <bool EIGHT, int ITER>
-__global__ __launch_bounds__(256) void adamw_kernel(AdamwSet u, AdamwNow a) {
-  int lo = 0, hi = u.n - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) / 2;
-    if (blockIdx.x >= u.first[mid]) lo = mid;
-    else hi = mid - 1;
-  }
-  const karma_adamw_tensor p = u.t[lo];
+// A workgroup has 1024 consecutive values, a lane four of them: 16-byte accesses of the fp32 buffers.  Reads and writes 28 bytes a
+// value (bf16 gradient and weight), 16.25 with 8-bit moments: bound by memory.  217 M values in 8 bits take 711 us, 5.0 TB/s, 63 M in
+// 609 tensors 376 us; four groups of 1024 a workgroup, loaded ahead, take 813 and 430 (more registers, fewer wavefronts).
+constexpr unsigned ADAMW_SPAN = 1024;
+template <bool EIGHT>
+__global__ __launch_bounds__(256) void adamw_kernel(AdamwSet<EIGHT> u, AdamwNow a) {
+  const int tensor = tensor_of(u);
+  const AdamwTensor<EIGHT> p = u.t[tensor];
   if (a.live) {
     a.lr = a.live->lr; a.grad_scale = a.live->grad_scale; a.seed = a.live->seed;
     corrections(a, a.live->step ? a.live->step : 1);
   }
-  const unsigned key = u.key[lo] + a.seed * 0x9e3779b1u;
   const bool gbf = p.flags & KARMA_ADAMW_GRAD_BF16, obf = p.flags & KARMA_ADAMW_OUT_BF16;
   const uintptr_t odd = (uintptr_t)p.w | (EIGHT ? ((uintptr_t)p.m | (uintptr_t)p.v) * 4 : (uintptr_t)p.m | (uintptr_t)p.v) |
                         (uintptr_t)p.grad * (gbf ? 2 : 1) | (uintptr_t)p.out * (obf ? 2 : 1);
-  const bool vec = odd % 16 == 0;
-  const size_t at = (size_t)(blockIdx.x - u.first[lo]) * (ITER * 1024) + threadIdx.x * 4;
-  f32x4 g[ITER], w[ITER], m[ITER], v[ITER];
-  Codes c[ITER];
+  const size_t i = (size_t)(blockIdx.x - u.first[tensor]) * ADAMW_SPAN + threadIdx.x * 4;
+  const bool whole = odd % 16 == 0 && i + 4 <= p.n;
+  const f32x4 g = gbf ? load4((const bf16_t*)p.grad, i, p.n, whole) : load4((const float*)p.grad, i, p.n, whole);
+  f32x4 w = load4(p.w, i, p.n, whole), m, v;
+  if constexpr (EIGHT) {
+    const bool some = i / 64 * 64 < p.n;      // the block exists
+    const Codes c{load4((const uint8_t*)p.m, i, p.n, whole), load4((const uint8_t*)p.v, i, p.n, whole), some ? p.m_scale[i / 64] : 0.f,
+                  some ? p.v_scale[i / 64] : 0.f};
+    const Codes r = quantised_step(c, g, a, p.key + a.seed * 0x9e3779b1u, i, m, v);
+    store4((uint8_t*)p.m, i, p.n, whole, r.m);
+    store4((uint8_t*)p.v, i, p.n, whole, r.v);
+    if (threadIdx.x % 16 == 0 && some) { p.m_scale[i / 64] = r.sm; p.v_scale[i / 64] = r.sv; }
+  } else {
+    m = load4((const float*)p.m, i, p.n, whole);
+    v = load4((const float*)p.v, i, p.n, whole);
+    const float d1 = (float)(1.0 - (double)a.beta1), d2 = (float)(1.0 - (double)a.beta2);
 #pragma unroll
-  for (int k = 0; k < ITER; ++k) {
-    const size_t i = at + k * 1024;
-    const bool whole = vec && i + 4 <= p.n;
-    g[k] = gbf ? load4((const bf16_t*)p.grad, i, p.n, whole) : load4((const float*)p.grad, i, p.n, whole);
-    w[k] = load4(p.w, i, p.n, whole);
-    if (EIGHT) {
-      const bool some = i / 64 * 64 < p.n;
-      c[k] = Codes{load4((const uint8_t*)p.m, i, p.n, whole), load4((const uint8_t*)p.v, i, p.n, whole), some ? p.m_scale[i / 64] : 0.f,
-                   some ? p.v_scale[i / 64] : 0.f};
-    } else {
-      m[k] = load4((const float*)p.m, i, p.n, whole);
-      v[k] = load4((const float*)p.v, i, p.n, whole);
+    for (int e = 0; e < 4; ++e) {
+      const float gs = g[e] * a.grad_scale;
+      m[e] = a.beta1 * m[e] + d1 * gs;
+      v[e] = a.beta2 * v[e] + d2 * gs * gs;
     }
+    store4((float*)p.m, i, p.n, whole, m);
+    store4((float*)p.v, i, p.n, whole, v);
   }
-  const float d1 = (float)(1.0 - (double)a.beta1), d2 = (float)(1.0 - (double)a.beta2), keep = 1.f - a.lr * p.weight_decay, lr = a.lr * a.c1;
+  const float keep = 1.f - a.lr * p.decay, lr = a.lr * a.c1;
 #pragma unroll
-  for (int k = 0; k < ITER; ++k) {
-    const size_t i = at + k * 1024;
-    const bool whole = vec && i + 4 <= p.n;
-    if (EIGHT) {
-      const Codes r = quantised_step(c[k], g[k], a, key, i, m[k], v[k]);
-      store4((uint8_t*)p.m, i, p.n, whole, r.m);
-      store4((uint8_t*)p.v, i, p.n, whole, r.v);
-      if (threadIdx.x % 16 == 0 && i < p.n) { p.m_scale[i / 64] = r.sm; p.v_scale[i / 64] = r.sv; }
-    } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float gs = g[k][e] * a.grad_scale;
-        m[k][e] = a.beta1 * m[k][e] + d1 * gs;
-        v[k][e] = a.beta2 * v[k][e] + d2 * gs * gs;
-      }
-      store4((float*)p.m, i, p.n, whole, m[k]);
-      store4((float*)p.v, i, p.n, whole, v[k]);
-    }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) w[k][e] = keep * w[k][e] - lr * (m[k][e] * __builtin_amdgcn_rcpf(sqrtf(v[k][e]) * a.k2 + a.eps));
-    store4(p.w, i, p.n, whole, w[k]);
-    if (p.out) {
-      if (obf) store4((bf16_t*)p.out, i, p.n, whole, w[k]);
-      else store4((float*)p.out, i, p.n, whole, w[k]);
-    }
+  for (int e = 0; e < 4; ++e) w[e] = keep * w[e] - lr * (m[e] * __builtin_amdgcn_rcpf(sqrtf(v[e]) * a.k2 + a.eps));
+  store4(p.w, i, p.n, whole, w);
+  if (p.out) {
+    if (obf) store4((bf16_t*)p.out, i, p.n, whole, w);
+    else store4((float*)p.out, i, p.n, whole, w);
   }
 }
 
-// the moments that 8-bit states stand for
+// The moments that 8-bit states stand for: four values a lane; 2.1 bytes in, 8 out (217 M values 391 us, 5.7 TB/s).
+struct StatesTensor {
+  const uint8_t* m; const uint8_t* v;
+  const float* m_scale; const float* v_scale;
+  float* m_out; float* v_out;
+  size_t n;
+};
 struct StatesSet {
-  const int8_t* m[ADAMW_TENSORS]; const uint8_t* v[ADAMW_TENSORS];
-  const float* m_scale[ADAMW_TENSORS]; const float* v_scale[ADAMW_TENSORS];
-  float* m_out[ADAMW_TENSORS]; float* v_out[ADAMW_TENSORS];
-  unsigned long long size[ADAMW_TENSORS];
-  unsigned first[ADAMW_TENSORS + 1];
+  static constexpr int MOST = 64;
+  StatesTensor t[MOST];
+  unsigned first[MOST + 1];
   int n;
 };
 static_assert(sizeof(StatesSet) <= 4096, "kernel arguments");
-constexpr unsigned STATES_SPAN = 4096;
-// four values a lane; 2.1 bytes in, 8 out
 __global__ __launch_bounds__(256) void adamw_states_kernel(StatesSet u) {
-  int lo = 0, hi = u.n - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) / 2;
-    if (blockIdx.x >= u.first[mid]) lo = mid;
-    else hi = mid - 1;
-  }
-  const size_t n = u.size[lo];
-  const uintptr_t odd = ((uintptr_t)u.m[lo] | (uintptr_t)u.v[lo]) * 4 | (uintptr_t)u.m_out[lo] | (uintptr_t)u.v_out[lo];
+  const int tensor = tensor_of(u);
+  const StatesTensor p = u.t[tensor];
+  const uintptr_t odd = ((uintptr_t)p.m | (uintptr_t)p.v) * 4 | (uintptr_t)p.m_out | (uintptr_t)p.v_out;
+  const size_t i = (size_t)(blockIdx.x - u.first[tensor]) * ADAMW_SPAN + threadIdx.x * 4;
+  if (i >= p.n) return;
+  const bool whole = odd % 16 == 0 && i + 4 <= p.n;
+  const unsigned cm = load4(p.m, i, p.n, whole), cv = load4(p.v, i, p.n, whole);
+  const float sm = p.m_scale[i / 64], sv = p.v_scale[i / 64];
+  f32x4 m, v;
 #pragma unroll
-  for (int k = 0; k < STATES_SPAN / 1024; ++k) {
-    const size_t i = (size_t)(blockIdx.x - u.first[lo]) * STATES_SPAN + k * 1024 + threadIdx.x * 4;
-    if (i >= n) return;
-    const bool whole = odd % 16 == 0 && i + 4 <= n;
-    const unsigned cm = load4((const uint8_t*)u.m[lo], i, n, whole), cv = load4(u.v[lo], i, n, whole);
-    const float sm = u.m_scale[lo][i / 64], sv = u.v_scale[lo][i / 64];
-    f32x4 m, v;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int q = (cv >> (8 * e)) & 0xff;
-      m[e] = (float)((int)(cm << (24 - 8 * e)) >> 24) * sm;
-      v[e] = (float)(q * q) * sv;
-    }
-    store4(u.m_out[lo], i, n, whole, m);
-    store4(u.v_out[lo], i, n, whole, v);
+  for (int e = 0; e < 4; ++e) {
+    const int q = (cv >> (8 * e)) & 0xff;
+    m[e] = (float)((int)(cm << (24 - 8 * e)) >> 24) * sm;
+    v[e] = (float)(q * q) * sv;
   }
+  store4(p.m_out, i, p.n, whole, m);
+  store4(p.v_out, i, p.n, whole, v);
 }
 
 bool aligned_to(const void* p, size_t n) { return (uintptr_t)p % n == 0; }
@@ -280,6 +278,42 @@ bool good_states(const karma_adamw_tensor& t) {
   if (!t.m || !t.v) return false;
   if (eight_bits(t)) return t.m_scale && t.v_scale && aligned_to(t.m_scale, 4) && aligned_to(t.v_scale, 4);
   return aligned_to(t.m, 4) && aligned_to(t.v, 4);
+}
+
+// Launches over the tensors of a list for which `fill` fills in a descriptor, as many at a time as the arguments hold.
+template <typename Set, typename Fill, typename Launch>
+bool in_sets(const karma_adamw_tensor* tensors, uint32_t n, Fill fill, Launch launch) {
+  bool launched = false;
+  for (uint32_t k = 0; k < n;) {
+    Set u;
+    u.n = 0;
+    u.first[0] = 0;
+    uint64_t blocks = 0;
+    for (; k < n && u.n < Set::MOST; ++k) {
+      const uint64_t more = (tensors[k].n + ADAMW_SPAN - 1) / ADAMW_SPAN;     // (2^30 at most)
+      if (!more || !fill(u.t[u.n], k)) continue;
+      if (blocks + more > INT32_MAX) break;
+      blocks += more;
+      u.first[++u.n] = (unsigned)blocks;
+    }
+    if (!u.n) continue;
+    launch(u, (unsigned)blocks);
+    launched = true;
+  }
+  return launched;
+}
+template <bool EIGHT>
+bool adamw_sets(const karma_adamw_tensor* tensors, uint32_t n, const AdamwNow& a, hipStream_t s) {
+  return in_sets<AdamwSet<EIGHT>>(
+      tensors, n,
+      [&](AdamwTensor<EIGHT>& d, uint32_t k) {
+        const karma_adamw_tensor& t = tensors[k];
+        if (eight_bits(t) != EIGHT) return false;
+        d.w = t.w; d.m = t.m; d.v = t.v; d.grad = t.grad; d.out = t.out; d.n = t.n; d.decay = t.weight_decay; d.flags = t.flags;
+        if constexpr (EIGHT) { d.m_scale = t.m_scale; d.v_scale = t.v_scale; d.key = (k + 1) * 0x7f4a7c15u; }
+        return true;
+      },
+      [&](const AdamwSet<EIGHT>& u, unsigned blocks) { hipLaunchKernelGGL(adamw_kernel<EIGHT>, dim3(blocks), dim3(256), 0, s, u, a); });
 }
 
 }  // namespace
@@ -295,33 +329,8 @@ int adamw(const karma_adamw_tensor* tensors, uint32_t n, const karma_adamw_step&
   }
   AdamwNow a{now.lr, now.beta1, now.beta2, now.eps, now.grad_scale, 0.f, 0.f, now.seed, live};
   if (!live) corrections(a, now.step);
-  uint64_t total = 0;
-  for (uint32_t k = 0; k < n; ++k) total += tensors[k].n;
-  // four groups of 1024 values a workgroup, one where the chip would not be full of those
-  const unsigned span = total >= (uint64_t)compute_units() * 4 * 4096 ? 4096 : 1024;
-  bool launched = false;
-  for (int eight = 0; eight < 2; ++eight) {
-    for (uint32_t k = 0; k < n;) {
-      AdamwSet u;
-      u.n = 0;
-      u.first[0] = 0;
-      uint64_t blocks = 0;
-      for (; k < n && u.n < ADAMW_TENSORS; ++k) {
-        if (!tensors[k].n || eight_bits(tensors[k]) != (eight != 0)) continue;
-        const uint64_t more = (tensors[k].n + span - 1) / span;
-        if (blocks + more > INT32_MAX) break;
-        blocks += more;
-        u.t[u.n] = tensors[k];
-        u.key[u.n] = (k + 1) * 0x7f4a7c15u;
-        u.first[++u.n] = (unsigned)blocks;
-      }
-      if (!u.n) continue;
-      auto* kernel = eight ? (span == 4096 ? adamw_kernel<true, 4> : adamw_kernel<true, 1>) : (span == 4096 ? adamw_kernel<false, 4> : adamw_kernel<false, 1>);
-      hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, s, u, a);
-      launched = true;
-    }
-  }
-  return !launched || hipGetLastError() == hipSuccess ? KARMA_OK : KARMA_E_HIP;
+  const bool wide = adamw_sets<false>(tensors, n, a, s), narrow = adamw_sets<true>(tensors, n, a, s);
+  return !(wide || narrow) || hipGetLastError() == hipSuccess ? KARMA_OK : KARMA_E_HIP;
 }
 
 int adamw_states(const karma_adamw_tensor* tensors, uint32_t n, float* const* m_out, float* const* v_out, hipStream_t s) {
@@ -330,26 +339,14 @@ int adamw_states(const karma_adamw_tensor* tensors, uint32_t n, float* const* m_
     if (!eight_bits(t) || !good_states(t)) return KARMA_E_INVAL;
     if (t.n && (!m_out[k] || !v_out[k] || !aligned_to(m_out[k], 4) || !aligned_to(v_out[k], 4))) return KARMA_E_INVAL;
   }
-  bool launched = false;
-  for (uint32_t k = 0; k < n;) {
-    StatesSet u;
-    u.n = 0;
-    u.first[0] = 0;
-    uint64_t blocks = 0;
-    for (; k < n && u.n < ADAMW_TENSORS; ++k) {
-      const karma_adamw_tensor& t = tensors[k];
-      if (!t.n) continue;
-      const uint64_t more = (t.n + STATES_SPAN - 1) / STATES_SPAN;
-      if (blocks + more > INT32_MAX) break;
-      blocks += more;
-      u.m[u.n] = (const int8_t*)t.m; u.v[u.n] = (const uint8_t*)t.v; u.m_scale[u.n] = t.m_scale; u.v_scale[u.n] = t.v_scale;
-      u.m_out[u.n] = m_out[k]; u.v_out[u.n] = v_out[k]; u.size[u.n] = t.n;
-      u.first[++u.n] = (unsigned)blocks;
-    }
-    if (!u.n) continue;
-    hipLaunchKernelGGL(adamw_states_kernel, dim3((unsigned)blocks), dim3(256), 0, s, u);
-    launched = true;
-  }
+  const bool launched = in_sets<StatesSet>(
+      tensors, n,
+      [&](StatesTensor& d, uint32_t k) {
+        const karma_adamw_tensor& t = tensors[k];
+        d = StatesTensor{(const uint8_t*)t.m, (const uint8_t*)t.v, t.m_scale, t.v_scale, m_out[k], v_out[k], (size_t)t.n};
+        return true;
+      },
+      [&](const StatesSet& u, unsigned blocks) { hipLaunchKernelGGL(adamw_states_kernel, dim3(blocks), dim3(256), 0, s, u); });
   return !launched || hipGetLastError() == hipSuccess ? KARMA_OK : KARMA_E_HIP;
 }
 
