@@ -428,7 +428,7 @@ int karma_get_op_times(karma_ctx* ctx, karma_op* ops_out, float* ms_out, uint32_
  * KARMA_E_OOM with the count when the capacity is too small. */
 int karma_get_op_starts(karma_ctx* ctx, float* start_ms_out, uint32_t* n_inout);
 
-/* ---- single kernels (device pointers, launched on `stream`, asynchronous) --------
+/* ---- single kernels (device pointers, launched on `stream`, asynchronous; the stream's device is the current one) --------
  * Exposed so that each can be checked against the CPU oracle on its own.  Shapes are
  * row-major.  bf16 tensors are uint16_t bit patterns. */
 
@@ -630,8 +630,8 @@ int karma_k_gated_scan_bwd_f32(const float* gate_dev, const float* x_dev, const 
                                float* dh0_dev, const karma_scan_shape* shape, void* ws_dev, uint64_t ws_bytes, void* stream);
 
 /* ---- log probabilities of given tokens, entropies and best alternatives of rows of logits ---------
- * logits_dev [rows][ld], cols <= ld used (ld 0: cols); q_j = scale z_j - ln sum_i e^(scale z_i), scale > 0 (one over the
- * temperature).  Outputs, each NULL where it is not wanted (not all of them):
+ * logits_dev [rows][ld], cols <= ld used (ld 0: cols); q_j = scale z_j - ln sum_i e^(scale z_i), scale from 1e-20
+ * to 1e20 (one over the temperature).  Outputs, each NULL where it is not wanted (not all of them):
  *   logprob_dev fp32 [rows]     q of tokens_dev[row]; 0 where the token is none of the columns (-1: padding)
  *   entropy_dev fp32 [rows]     -sum_j e^q_j q_j
  *   stats_dev fp32 [rows][2]    the largest z and ln sum_j e^(scale (z_j - largest)), for the backward pass
@@ -667,7 +667,8 @@ int karma_k_token_logprob_bwd_f32(const float* logits_dev, uint64_t ld, const in
  * v_scale, fp32 [ceil(n / KARMA_ADAMW_BLOCK)]: m = code * m_scale, v = code^2 * v_scale (all zeros: states at the beginning).
  * The step is computed from the moments before they are rounded; each then becomes one of the two codes around it at random, its
  * expectation kept (v > 0 becomes at least code 1).  The random bits follow from `seed`, the tensor's place in the list and the element's:
- * give every step another seed.  A gradient that is not finite makes the scales, and with them the moments, of its block NaN.
+ * give every step another seed.  A gradient that is not finite, or whose square is not, makes the scales, and with them the
+ * moments, of its block NaN.
  * Without the flag m and v are fp32 [n].  Tensors overlap nothing, other tensors of the list included; n may be 0.
  * tensors is a host array, read during the call.  live_dev (may be NULL): lr, grad_scale, step and seed are read from there when
  * the kernels run, not from `now`: for a captured graph, which is replayed with other values (a step of 0 counts as 1).

@@ -75,14 +75,15 @@ struct Spans {
     }
     return lo - 1;
   }
-  // from sequence j on to the one that token t begins, or back to the one that token t ends
+  // from sequence j on to the one that token t begins, or back to the one that token t ends: most often its neighbour, else searched for
+  // (any number of sequences without tokens may lie between)
   __device__ __forceinline__ int next(int j, int t) const {
-    while (j + 1 < sequences && at(j + 1) <= t) ++j;
-    return j;
+    if (j + 1 < sequences && at(j + 1) <= t) ++j;
+    return j + 1 < sequences && at(j + 1) <= t ? find(t) : j;
   }
   __device__ __forceinline__ int previous(int j, int t) const {
-    while (j > 0 && at(j) > t) --j;
-    return j;
+    if (j > 0 && at(j) > t) --j;
+    return j > 0 && at(j) > t ? find(t) : j;
   }
   __device__ __forceinline__ size_t row(int j, int channels) const { return (size_t)(j < 0 ? 0 : j >= sequences ? sequences - 1 : j) * channels; }
 };
@@ -112,7 +113,7 @@ __device__ __forceinline__ Part part_of(const Spans& p, int t0, unsigned long lo
   r.seq = __builtin_amdgcn_readfirstlane(p.find(t0));
   const int first = __builtin_amdgcn_readfirstlane(p.at(0)), last = __builtin_amdgcn_readfirstlane(p.at(p.sequences));
   if (!p.starts) {
-    for (int t = r.seq * p.each; t <= t0 + L && t <= last; t += p.each)
+    for (long t = (long)r.seq * p.each; t <= t0 + L && t <= last; t += p.each)
       if (t >= t0) bounds |= 1ull << (t - t0);
   } else {
     if (lane == 0) *word = 0;
@@ -146,7 +147,7 @@ struct Chain {
   unsigned* state;              // behind the chunk
   int chunks, blocks, width;    // blocks of channels, channels of all blocks; chunks == 1: no chain
 };
-constexpr int CHAIN_LIMIT = 1 << 21;    // looks at a word, a microsecond or so each
+constexpr int CHAIN_LIMIT = 1 << 20;    // looks at a word, a microsecond or so each
 
 __device__ __forceinline__ unsigned long long effect_word(float A, float H, bool cut) {
   const unsigned long long w = (unsigned long long)__float_as_uint(H) << 32 | __float_as_uint(cut ? -1.f : A);
@@ -244,8 +245,7 @@ __device__ __forceinline__ bool take_work(const Chain& c, bool up, int& chunk, i
 template <typename T, int V, int L, int W>
 __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(4))) void scan_fwd_kernel(ScanFwd a, Spans p, Chain chain) {
   typedef Lane<T, V> Ln;
-  constexpr int TOKENS = L * W;
-  static_assert(KARMA_SCAN_MARK % L == 0, "marks lie between the wavefronts' parts");
+  static_assert(L * W == KARMA_SCAN_MARK, "a chunk is what lies between two marks");
   __shared__ float effects[W][2][64 * V];
   __shared__ float incoming[64 * V];
   __shared__ unsigned long long words[W];
@@ -255,7 +255,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(4))) voi
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), C = (int)a.s.channels;
   const int channel = block * 64 * V + lane * V, c = channel < C ? channel : C - V;     // (lanes without a channel repeat the last one)
   const bool mine = channel < C;
-  const int t0 = chunk * TOKENS + w * L;
+  const int t0 = chunk * KARMA_SCAN_MARK + w * L;
   typename Ln::Raw rf[L], rx[L];
 #pragma unroll
   for (int i = 0; i < L; ++i) {
@@ -341,9 +341,9 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(4))) voi
     const float in = chain.chunks > 1 ? incoming[lane * V + e] : 0.f;
     h[e] = w == 0 ? in : cut ? PH[e] : fmaf(PA[e], in, PH[e]);
   }
-  if (a.marks && mine && t0 % KARMA_SCAN_MARK == 0 && t0 < p.tokens) {
+  if (w == 0 && a.marks && mine) {
 #pragma unroll
-    for (int e = 0; e < V; ++e) a.marks[(size_t)(t0 / KARMA_SCAN_MARK) * C + c + e] = h[e];
+    for (int e = 0; e < V; ++e) a.marks[(size_t)chunk * C + c + e] = h[e];
   }
   auto store = [&](int i) {
     if (mine) *(typename Ln::Raw*)((T*)a.h + (size_t)(t0 + i) * a.s.ld_h + c) = Ln::put(h);
@@ -630,8 +630,7 @@ bool whole_sequences(const karma_scan_shape& s, bool packed, uint64_t units) {
 }
 
 // chunks of a call; channels of all blocks whatever a lane has
-uint64_t scan_chunks(uint64_t tokens, int per) { return std::max<uint64_t>(1, (tokens + per - 1) / per); }
-constexpr int FWD_TOKENS = 256;    // of a forward chunk
+uint64_t scan_chunks(uint64_t tokens) { return std::max<uint64_t>(1, (tokens + KARMA_SCAN_MARK - 1) / KARMA_SCAN_MARK); }
 uint64_t scan_width(uint32_t channels) { return ((uint64_t)channels + 127) / 128 * 128; }
 
 // Sizes and strides as a call may give them; a stride of 0 becomes the number of channels.
@@ -642,7 +641,7 @@ int check_scan(karma_scan_shape& s, const void* starts) {
     if (!*ld) *ld = s.channels;
     if (*ld < s.channels || *ld > INT64_MAX / 8 / (s.tokens + 1)) return KARMA_E_INVAL;
   }
-  if ((uint64_t)((s.channels + 63) / 64) * std::max<uint64_t>(s.sequences, scan_chunks(s.tokens, FWD_TOKENS) + 1) > INT32_MAX) return KARMA_E_INVAL;
+  if ((uint64_t)((s.channels + 63) / 64) * std::max<uint64_t>(s.sequences, scan_chunks(s.tokens) + 1) > INT32_MAX) return KARMA_E_INVAL;
   return KARMA_OK;
 }
 bool aligned_to(const void* p, size_t n) { return (uintptr_t)p % n == 0; }
@@ -655,7 +654,7 @@ size_t gated_scan_ws_bytes(const karma_scan_shape& given) {
   karma_scan_shape shape = given;
   const int any = 0;      // (whether all sequences have one length does not matter here)
   if (check_scan(shape, &any)) return 0;
-  const uint64_t chunks = scan_chunks(shape.tokens, FWD_TOKENS);
+  const uint64_t chunks = scan_chunks(shape.tokens);
   return chunks > 1 ? CHAIN_HEAD + chunks * scan_width(shape.channels) * 12 : 0;
 }
 
@@ -663,8 +662,8 @@ static Spans spans_of(const karma_scan_shape& s, const int* starts) {
   return Spans{starts, (int)s.tokens, (int)s.sequences, starts ? 0 : (int)(s.tokens / s.sequences)};
 }
 // V channels a lane; the chain is cleared by a kernel ahead (a call that is captured has kernels alone)
-static Chain chain_of(const karma_scan_shape& s, int V, int per, void* ws, hipStream_t stream) {
-  const uint64_t chunks = scan_chunks(s.tokens, per), width = scan_width(s.channels);
+static Chain chain_of(const karma_scan_shape& s, int V, void* ws, hipStream_t stream) {
+  const uint64_t chunks = scan_chunks(s.tokens), width = scan_width(s.channels);
   unsigned long long* effect = (unsigned long long*)((char*)ws + CHAIN_HEAD);
   const Chain c{(unsigned*)ws, effect, (unsigned*)(effect + chunks * width), (int)chunks, (int)((s.channels + 64 * V - 1) / (64 * V)), (int)width};
   const size_t pieces = chunks * width * 12 / 16;
@@ -689,11 +688,11 @@ int gated_scan_fwd(ScanFwd a, bool bf16, hipStream_t s) {
     else if (bf16) hipLaunchKernelGGL((scan_fwd_short_kernel<bf16_t, 1>), grid, dim3(256), 0, s, a, p, blocks, units);
     else hipLaunchKernelGGL((scan_fwd_short_kernel<float, 1>), grid, dim3(256), 0, s, a, p, blocks, units);
   } else {
-    const Chain c = chain_of(a.s, pairs ? 2 : 1, FWD_TOKENS, a.ws, s);
+    const Chain c = chain_of(a.s, pairs ? 2 : 1, a.ws, s);
     const dim3 grid(chain_grid(c));
-    if (pairs) hipLaunchKernelGGL((scan_fwd_kernel<bf16_t, 2, 32, FWD_TOKENS / 32>), grid, dim3(FWD_TOKENS * 2), 0, s, a, p, c);
-    else if (bf16) hipLaunchKernelGGL((scan_fwd_kernel<bf16_t, 1, 32, FWD_TOKENS / 32>), grid, dim3(FWD_TOKENS * 2), 0, s, a, p, c);
-    else hipLaunchKernelGGL((scan_fwd_kernel<float, 1, 32, FWD_TOKENS / 32>), grid, dim3(FWD_TOKENS * 2), 0, s, a, p, c);
+    if (pairs) hipLaunchKernelGGL((scan_fwd_kernel<bf16_t, 2, 32, 8>), grid, dim3(512), 0, s, a, p, c);
+    else if (bf16) hipLaunchKernelGGL((scan_fwd_kernel<bf16_t, 1, 32, 8>), grid, dim3(512), 0, s, a, p, c);
+    else hipLaunchKernelGGL((scan_fwd_kernel<float, 1, 32, 8>), grid, dim3(512), 0, s, a, p, c);
   }
   return hipGetLastError() == hipSuccess ? KARMA_OK : KARMA_E_HIP;
 }
@@ -715,7 +714,7 @@ int gated_scan_bwd(ScanBwd a, bool bf16, hipStream_t s) {
   const bool pairs = bf16 && a.s.channels % 2 == 0 && (a.s.ld_gate | a.s.ld_x | a.s.ld_h | a.s.ld_dgate | a.s.ld_dx) % 2 == 0 &&
                      aligned_to(a.gate, 4) && aligned_to(a.x, 4) && aligned_to(a.dh, 4) && aligned_to(a.dgate, 4) && aligned_to(a.dx, 4);
   const Spans p = spans_of(a.s, a.starts);
-  const Chain c = chain_of(a.s, pairs ? 2 : 1, KARMA_SCAN_MARK, a.ws, s);
+  const Chain c = chain_of(a.s, pairs ? 2 : 1, a.ws, s);
   const dim3 grid(chain_grid(c));
 #define KARMA_SCAN_BWD(T, V)                                                                                           \
   do {                                                                                                                 \

@@ -7,7 +7,6 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
-#include <cmath>
 
 #include "device_utils.h"
 #include "karma.h"
@@ -272,6 +271,7 @@ struct Best {
 };
 
 // ---- forward -------------------------------------------------------------------------------------------------
+constexpr uint32_t LP_PLACES = 7 * 256;
 constexpr int LP_BATCH = 4;     // vectors that a lane has under way
 
 struct LogprobPart { float m, s, t, unused; };
@@ -531,14 +531,14 @@ __global__ __launch_bounds__(LP_THREADS) void logprob_bwd_kernel(LogprobBwd a, u
   }
 }
 
-// Wavefronts for a row: one where four would not have a vector for every lane.  Parts of a row: enough for 2048 workgroups (eight on
-// each of 256 compute units), none smaller than one vector a lane.
+// Wavefronts for a row: one where four would not have a vector for every lane, and for rows of up to 512 vectors where there are many
+// (16000 x 4000 in bf16: 29.5 us instead of 33.0, with 5 alternatives 41 instead of 57; 4097 x 8000: 25.7 and 25.0).  Parts of a row: as
+// many as there is room for at once (seven workgroups on each of 256 compute units), none smaller than one vector a lane.
 struct LogprobCut { unsigned waves, parts; };
 LogprobCut cut_rows(uint32_t rows, uint32_t cols, bool bf16) {
-  const uint32_t vectors = cols / (bf16 ? 8 : 4);
-  const uint64_t parts = std::min<uint64_t>((2048 + rows - 1) / std::max(rows, 1u), vectors / LP_THREADS);
+  const uint32_t vectors = cols / (bf16 ? 8 : 4), parts = std::min(LP_PLACES / std::max(rows, 1u), vectors / LP_THREADS);
   if (parts <= 1) return LogprobCut{vectors <= (rows >= 4096 ? 512u : (unsigned)LP_THREADS) ? 1u : (unsigned)LP_WAVES, 1};
-  return LogprobCut{(unsigned)LP_WAVES, (unsigned)parts};
+  return LogprobCut{(unsigned)LP_WAVES, parts};
 }
 size_t up16(size_t b) { return (b + 15) / 16 * 16; }
 
@@ -557,7 +557,7 @@ size_t token_logprob_ws_bytes(uint32_t rows, uint32_t cols, uint32_t top) {
 
 int token_logprob_fwd(LogprobFwd a, bool bf16, hipStream_t s) {
   if (!a.ld) a.ld = a.cols;
-  if (!good_rows(a.rows, a.cols, a.ld) || !(a.scale > 0.f) || !std::isfinite(a.scale)) return KARMA_E_INVAL;
+  if (!good_rows(a.rows, a.cols, a.ld) || !(a.scale >= 1e-20f && a.scale <= 1e20f)) return KARMA_E_INVAL;
   if (a.top > KARMA_TOP_MAX || a.top > a.cols || (a.top && (!a.top_logprob || !a.top_id))) return KARMA_E_INVAL;
   if ((a.logprob && !a.tokens) || (!a.logprob && !a.entropy && !a.stats && !a.top)) return KARMA_E_INVAL;
   if (!a.rows) return KARMA_OK;
@@ -585,7 +585,7 @@ int token_logprob_fwd(LogprobFwd a, bool bf16, hipStream_t s) {
 int token_logprob_bwd(LogprobBwd a, bool bf16, hipStream_t s) {
   if (!a.ld) a.ld = a.cols;
   if (!a.ld_d) a.ld_d = a.cols;
-  if (!good_rows(a.rows, a.cols, a.ld) || !good_rows(a.rows, a.cols, a.ld_d) || !(a.scale > 0.f) || !std::isfinite(a.scale)) return KARMA_E_INVAL;
+  if (!good_rows(a.rows, a.cols, a.ld) || !good_rows(a.rows, a.cols, a.ld_d) || !(a.scale >= 1e-20f && a.scale <= 1e20f)) return KARMA_E_INVAL;
   if ((a.dlogprob && !a.tokens) || (a.dentropy && !a.entropy) || (!a.dlogprob && !a.dentropy)) return KARMA_E_INVAL;
   if (!a.rows) return KARMA_OK;
   if (!a.logits || !a.stats || !a.dlogits || !aligned_to(a.logits, bf16 ? 2 : 4) || !aligned_to(a.dlogits, bf16 ? 2 : 4)) return KARMA_E_INVAL;

@@ -126,7 +126,7 @@ def logprob_bwd(rows=4, cols=100, ld=0, ld_d=0, scale=1.0, logits=P, tokens=P, s
 
 
 def test_logprob_refusals():
-    for bad in (dict(cols=0), dict(ld=99), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(tokens=None),
+    for bad in (dict(cols=0), dict(ld=99), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=1e21), dict(scale=1e-21), dict(tokens=None),
                 dict(logprob=None), dict(top=2), dict(top=2, top_lp=P), dict(top=65, top_lp=P, top_id=P), dict(cols=3, top=4, top_lp=P, top_id=P),
                 dict(logits=None), dict(logits=C.c_void_p(4097)), dict(logits=C.c_void_p(4098), fn="f32"), dict(rows=1 << 31), dict(ld=1 << 62),
                 dict(cols=1 << 31)):
