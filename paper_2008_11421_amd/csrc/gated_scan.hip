@@ -95,15 +95,6 @@ struct Part {
   unsigned inside;      // that belong to one
   int seq;              // the last sequence that begins at or before t0
 };
-// Runs of tokens of one sequence: the one that begins with the lowest token left, and the one that ends with the highest.
-__device__ __forceinline__ unsigned first_run(const Part& q, unsigned left) {
-  const unsigned later = q.begins & left & (left - 1);      // (the lowest token left, if it begins one, begins this run)
-  return later ? left & ((later & -later) - 1) : left;
-}
-__device__ __forceinline__ unsigned last_run(const Part& q, unsigned left) {
-  const unsigned earlier = q.ends & left & ~(0x80000000u >> __builtin_clz(left));
-  return earlier ? left & ~((0xffffffffu >> __builtin_clz(earlier))) : left;
-}
 // word: 8 bytes of LDS of the wavefront's own
 template <int L>
 __device__ __forceinline__ Part part_of(const Spans& p, int t0, unsigned long long* word) {
@@ -141,6 +132,9 @@ __device__ __forceinline__ Part part_of(const Spans& p, int t0, unsigned long lo
 // the same order every time, without a trip to memory between one chunk and the next.  Workgroups take their work by a counter, the
 // carriers first, so whoever is waited for is already running.  A word of all ones is not there yet.  A wait that never ends (a
 // workspace that another call is using) is given up, and the states become NaN.
+// 65536 tokens of 2048 channels: 188 us a call, of which 6 to clear the words; 171 in the kernel if nobody waited (what a copy of the same
+// bytes takes is 169); chunks of 128 tokens 225 in the kernel, of 64 373 (a chunk costs the chain 0.35 us), of 512 378 (one workgroup
+// on a compute unit: nothing hides its waits).
 struct Chain {
   unsigned* ticket;
   unsigned long long* effect;   // [chunk][channel]
@@ -232,6 +226,7 @@ __device__ __forceinline__ bool take_work(const Chain& c, bool up, int& chunk, i
       return false;
     }
     unit -= c.blocks;
+    if (unit >= c.blocks * c.chunks) return false;      // (the counter is another call's too)
   }
   chunk = unit / c.blocks;
   if (!up) chunk = c.chunks - 1 - chunk;
@@ -241,7 +236,10 @@ __device__ __forceinline__ bool take_work(const Chain& c, bool up, int& chunk, i
 
 // ---- forward ----------------------------------------------------------------------------------------------------
 // W wavefronts have the chunk's tokens one part behind the other, L each, a lane V channels, everything in registers: one pass over
-// memory.  Each runs through its part once for A and H, and, when the state before it is known, again for the states themselves.
+// memory, which bounds it (6 bytes an element in bf16 against some 20 vector operations, of which the exponential and the reciprocal are
+// eight).  Each wavefront runs through its part once for A and H, and, when the state before it is known, again for the states.  120
+// registers: two workgroups on a compute unit, so that one loads while the other waits.  One channel a lane takes 220 us instead of 191
+// for 65536 x 2048.
 template <typename T, int V, int L, int W>
 __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(4))) void scan_fwd_kernel(ScanFwd a, Spans p, Chain chain) {
   typedef Lane<T, V> Ln;
@@ -438,7 +436,10 @@ __global__ __launch_bounds__(256) void scan_fwd_short_kernel(ScanFwd a, Spans p,
 
 // ---- backward ---------------------------------------------------------------------------------------------------
 // As forward, with the chain from the last chunk to the first: the gradient g of the state behind a part goes in, that of the state
-// before it comes out, out = A g + R.  The states are run through again from the chunk's mark.
+// before it comes out, out = A g + R.  The states are run through again from the chunk's mark: 10 bytes an element in bf16 where reading
+// h would make 12, and exact.  Three inputs, the shares and the gaps leave room for 16 tokens a wavefront, so the chunk takes 16
+// wavefronts; without states (STATES) 90 registers, so that wavefronts of the next chunk begin while the last of this one end: with 32 x
+// 1024 tokens of 1024 channels 87 us, 106 with 128 registers, 173 with spills.  One channel a lane: 120.
 template <typename T, int V, int L, int W, bool STATES>
 __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(5))) void scan_bwd_kernel(ScanBwd a, Spans p, Chain chain) {
   typedef Lane<T, V> Ln;
