@@ -533,10 +533,14 @@ __global__ __launch_bounds__(LP_THREADS) void logprob_bwd_kernel(LogprobBwd a, u
 
 // Wavefronts for a row: one where four would not have a vector for every lane, and for rows of up to 512 vectors where there are many
 // (16000 x 4000 in bf16: 29.5 us instead of 33.0, with 5 alternatives 41 instead of 57; 4097 x 8000: 25.7 and 25.0).  Parts of a row: as
-// many as there is room for at once (seven workgroups on each of 256 compute units), none smaller than one vector a lane.
+// many as there is room for at once (seven workgroups on each of 256 compute units), none smaller than two vectors a lane, and none
+// of rows that four vectors a lane hold twice: their join takes longer than it saves (with 20 alternatives, 1 x 5028 in one part / in
+// parts of one vector a lane 7.2 / 11.0 us in the kernels, 8 x 16000 11.4 / 12.2; in parts of two / of one 1 x 160000 16.9 / 20.5, 64 x 51200
+// 15.8 / 18.0, 8 x 51200 14.6 / 13.6).
 struct LogprobCut { unsigned waves, parts; };
 LogprobCut cut_rows(uint32_t rows, uint32_t cols, bool bf16) {
-  const uint32_t vectors = cols / (bf16 ? 8 : 4), parts = std::min(LP_PLACES / std::max(rows, 1u), vectors / LP_THREADS);
+  const uint32_t vectors = cols / (bf16 ? 8 : 4);
+  const uint32_t parts = vectors < 2 * LP_BATCH * LP_THREADS ? 1 : std::min(LP_PLACES / std::max(rows, 1u), vectors / (2 * LP_THREADS));
   if (parts <= 1) return LogprobCut{vectors <= (rows >= 4096 ? 512u : (unsigned)LP_THREADS) ? 1u : (unsigned)LP_WAVES, 1};
   return LogprobCut{(unsigned)LP_WAVES, parts};
 }
