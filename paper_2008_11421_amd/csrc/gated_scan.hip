@@ -95,6 +95,11 @@ struct Part {
   unsigned inside;      // that belong to one
   int seq;              // the last sequence that begins at or before t0
 };
+// A run of tokens of one sequence: the one that begins with the lowest token left.
+__device__ __forceinline__ unsigned first_run(const Part& q, unsigned left) {
+  const unsigned later = q.begins & left & (left - 1);      // (the lowest token left, if it begins one, begins this run)
+  return later ? left & ((later & -later) - 1) : left;
+}
 // word: 8 bytes of LDS of the wavefront's own
 template <int L>
 __device__ __forceinline__ Part part_of(const Spans& p, int t0, unsigned long long* word) {
@@ -281,29 +286,29 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(4))) voi
 #pragma unroll
     for (int i = 0; i < L; ++i) {
       float x[V];
-      Ln::get(rx[i], x);
+      Ln::get(as_new(rx[i]), x);
 #pragma unroll
       for (int e = 0; e < V; ++e) { h[e] = step_of(b[i][e], x[e], h[e]); A[e] = fmaf(-b[i][e], A[e], A[e]); }
     }
   } else {
     int j = q.seq;
-#pragma unroll
-    for (int i = 0; i < L; ++i) {
-      if (q.begins >> i & 1) {
-        j = p.next(j, t0 + i);
+    for (unsigned left = q.inside; left;) {
+      const unsigned run = first_run(q, left);
+      left &= ~run;
+      if (q.begins & run) {
+        j = p.next(j, t0 + __builtin_ctz(run));
         initial(j, begun);      // of the last one kept: by the second run h_last may lie over it
 #pragma unroll
         for (int e = 0; e < V; ++e) h[e] = begun[e];
       }
-      if (!(q.inside >> i & 1)) {
 #pragma unroll
-        for (int e = 0; e < V; ++e) b[i][e] = 0.f;
-        continue;
+      for (int i = 0; i < L; ++i) {
+        if (!(run >> i & 1)) continue;
+        float x[V];
+        Ln::get(as_new(rx[i]), x);
+#pragma unroll
+        for (int e = 0; e < V; ++e) { h[e] = step_of(b[i][e], x[e], h[e]); A[e] = fmaf(-b[i][e], A[e], A[e]); }
       }
-      float x[V];
-      Ln::get(rx[i], x);
-#pragma unroll
-      for (int e = 0; e < V; ++e) { h[e] = step_of(b[i][e], x[e], h[e]); A[e] = fmaf(-b[i][e], A[e], A[e]); }
     }
   }
 #pragma unroll
@@ -344,37 +349,41 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(4))) voi
     for (int e = 0; e < V; ++e) a.marks[(size_t)chunk * C + c + e] = h[e];
   }
   auto store = [&](int i) {
-    if (mine) *(typename Ln::Raw*)((T*)a.h + (size_t)(t0 + i) * a.s.ld_h + c) = Ln::put(h);
+    if (mine) *(typename Ln::Raw*)((T*)a.h + (size_t)as_new_scalar(t0 + i) * a.s.ld_h + c) = Ln::put(h);
   };
   if (plain) {
 #pragma unroll
     for (int i = 0; i < L; ++i) {
       float x[V];
-      Ln::get(rx[i], x);
+      Ln::get(as_new(rx[i]), x);
 #pragma unroll
       for (int e = 0; e < V; ++e) h[e] = step_of(b[i][e], x[e], h[e]);
       store(i);
     }
   } else {
     int j = q.seq;
-#pragma unroll
-    for (int i = 0; i < L; ++i) {
-      if (q.begins >> i & 1) {
-        j = p.next(j, t0 + i);
-        if (q.begins >> i == 1) {
+    for (unsigned left = q.inside; left;) {
+      const unsigned run = first_run(q, left);
+      left &= ~run;
+      if (q.begins & run) {
+        j = p.next(j, t0 + __builtin_ctz(run));
+        if (q.begins & left) {
+          initial(j, h);
+        } else {
 #pragma unroll
           for (int e = 0; e < V; ++e) h[e] = begun[e];
-        } else {
-          initial(j, h);
         }
       }
-      if (!(q.inside >> i & 1)) continue;
-      float x[V];
-      Ln::get(rx[i], x);
 #pragma unroll
-      for (int e = 0; e < V; ++e) h[e] = step_of(b[i][e], x[e], h[e]);
-      store(i);
-      if ((q.ends >> i & 1) && a.h_last && mine) {
+      for (int i = 0; i < L; ++i) {
+        if (!(run >> i & 1)) continue;
+        float x[V];
+        Ln::get(as_new(rx[i]), x);
+#pragma unroll
+        for (int e = 0; e < V; ++e) h[e] = step_of(b[i][e], x[e], h[e]);
+        store(i);
+      }
+      if ((q.ends & run) && a.h_last && mine) {
 #pragma unroll
         for (int e = 0; e < V; ++e) a.h_last[p.row(j, C) + c + e] = h[e];
       }
