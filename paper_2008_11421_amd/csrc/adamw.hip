@@ -226,9 +226,10 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamwSet<EIGHT> u, AdamwNow 
     store4((float*)p.m, i, p.n, whole, m);
     store4((float*)p.v, i, p.n, whole, v);
   }
-  const float keep = 1.f - a.lr * p.decay, lr = a.lr * a.c1;
+  // decay and step are added up before the weight sees them: 1 - lr decay in 32 bits is off by a large part of a small decay
+  const float shrink = a.lr * p.decay, lr = a.lr * a.c1;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) w[e] = keep * w[e] - lr * (m[e] * __builtin_amdgcn_rcpf(sqrtf(v[e]) * a.k2 + a.eps));
+  for (int e = 0; e < 4; ++e) w[e] -= fmaf(shrink, w[e], lr * (m[e] * __builtin_amdgcn_rcpf(sqrtf(v[e]) * a.k2 + a.eps)));
   store4(p.w, i, p.n, whole, w);
   if (p.out) {
     if (obf) store4((bf16_t*)p.out, i, p.n, whole, w);

@@ -271,7 +271,7 @@ struct Best {
 };
 
 // ---- forward -------------------------------------------------------------------------------------------------
-constexpr uint32_t LP_PLACES = 7 * 256;
+constexpr uint32_t LP_PLACES = 7 * 256;   // workgroups that run at once
 constexpr int LP_BATCH = 4;     // vectors that a lane has under way
 
 struct LogprobPart { float m, s, t, unused; };
@@ -303,7 +303,9 @@ __device__ __forceinline__ void finish_row(const LogprobFwd& a, size_t r, Runnin
 }
 
 // W wavefronts share a part of a row (`parts` parts a row, W = 1: the whole row), lanes side by side on vectors.  One pass: every
-// vector goes into the running sums and past the list of alternatives.
+// vector goes into the running sums and past the list of alternatives.  Bound by memory: 4096 x 32000 in bf16 54 us, 4.8 TB/s (eight
+// vectors under way instead of four: 62); with 5 alternatives 67, with 20 73, with 64 92, which is the work on keys (inserting them one by
+// one into a list in registers took 72, 94 and 127; comparing all candidates with each other 87 with 5).
 template <typename T, int W, bool TOP>
 __global__ __launch_bounds__(LP_THREADS) void logprob_fwd_kernel(LogprobFwd a, unsigned parts, LogprobPart* sums, uint64_t* lists) {
   constexpr int N = Vec<T>::N;
@@ -477,7 +479,8 @@ __global__ __launch_bounds__(LP_THREADS) void logprob_join_kernel(LogprobFwd a, 
 }
 
 // ---- backward ------------------------------------------------------------------------------------------------
-// A wavefront has LP_BATCH vectors of each lane of one row; `units` wavefronts a row.
+// A wavefront has LP_BATCH vectors of each lane of one row; `units` wavefronts a row.  Bound by memory: 4096 x 51200 in bf16 143 us,
+// 5.9 TB/s.
 template <typename T>
 __global__ __launch_bounds__(LP_THREADS) void logprob_bwd_kernel(LogprobBwd a, unsigned units) {
   constexpr int N = Vec<T>::N, SPAN = 64 * LP_BATCH;

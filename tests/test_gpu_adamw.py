@@ -197,6 +197,18 @@ def test_weight_decay_alone_and_no_learning(torch):
     assert torch.equal(w, s.w[0])
 
 
+def test_a_small_decay_is_rounded_once(torch):
+    """lr * decay = 0.6 * 2^-24 takes 0.45 of a step (2^-23) off 1.5: the nearest number is 1.5.  Rounded by itself, 1 - lr * decay would be
+    1 - 2^-24, and 1.5 times that nearest to 1.5 - 2^-23.  At 0.7 * 2^-24 it is 0.525 of a step."""
+    for share, want in ((0.6, 1.5), (0.7, 1.5 - 2.0 ** -23)):
+        s = Step(torch, 7, [(256, False, None, False, share)], lr=2.0 ** -24, beta1=0.0, beta2=0.0, eps=1.0)
+        s.w[0].fill_(1.5)
+        s.g[0].zero_()
+        s.run()
+        torch.cuda.synchronize()
+        assert (s.w[0] == want).all()
+
+
 @pytest.mark.parametrize("step", [1, 2, 1000, 10 ** 6, 2 ** 40])
 def test_step_numbers(torch, step):
     Step(torch, 8, [(300, True, None, False, 0.1), (300, True, None, True, 0.1)], step=step, beta2=0.999).check()
