@@ -269,7 +269,14 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(4))) voi
   const Part q = part_of<L>(p, t0, words + w);
   const unsigned all = L == 32 ? ~0u : (1u << (L & 31)) - 1;
   const bool plain = q.inside == all && !q.begins && !q.ends;
+  auto initial = [&](int j, float (&v)[V]) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] = a.h0 ? a.h0[p.row(j, C) + c + e] : 0.f;
+  };
+  // the state that the last sequence to begin here begins with: asked for while the inputs are under way, and kept, as by the second run
+  // h_last may lie over it
   float b[L][V], A[V], h[V], begun[V] = {};
+  if (q.begins) initial(p.next(q.seq, t0 + 31 - __builtin_clz(q.begins)), begun);
 #pragma unroll
   for (int e = 0; e < V; ++e) { A[e] = 1.f; h[e] = 0.f; }
 #pragma unroll
@@ -278,10 +285,6 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(4))) voi
 #pragma unroll
     for (int e = 0; e < V; ++e) b[i][e] = share_of(b[i][e]);
   }
-  auto initial = [&](int j, float (&v)[V]) {
-#pragma unroll
-    for (int e = 0; e < V; ++e) v[e] = a.h0 ? a.h0[p.row(j, C) + c + e] : 0.f;
-  };
   if (plain) {
 #pragma unroll
     for (int i = 0; i < L; ++i) {
@@ -297,9 +300,12 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(4))) voi
       left &= ~run;
       if (q.begins & run) {
         j = p.next(j, t0 + __builtin_ctz(run));
-        initial(j, begun);      // of the last one kept: by the second run h_last may lie over it
+        if (q.begins & left) {
+          initial(j, h);
+        } else {
 #pragma unroll
-        for (int e = 0; e < V; ++e) h[e] = begun[e];
+          for (int e = 0; e < V; ++e) h[e] = begun[e];
+        }
       }
 #pragma unroll
       for (int i = 0; i < L; ++i) {
