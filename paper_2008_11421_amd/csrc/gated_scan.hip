@@ -406,42 +406,66 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(4))) voi
   }
 }
 
-// Short sequences (single tokens among them): a wavefront has a whole one, eight tokens under way.
+// Short sequences (single tokens among them): a wavefront has a whole one.  Here its tokens t0 .. t0 + n - 1, 1 <= n <= L, of which only
+// the first can have a mark before it; the last one is read again in place of those behind it.
+template <typename T, int V, int L>
+__device__ __forceinline__ void short_part(const ScanFwd& a, int t0, int n, unsigned c, float (&h)[V]) {
+  typedef typename Lane<T, V>::Raw Raw;
+  const T *gate = (const T*)a.gate + (size_t)t0 * a.s.ld_gate, *x = (const T*)a.x + (size_t)t0 * a.s.ld_x;
+  T* out = (T*)a.h + (size_t)t0 * a.s.ld_h;
+  Raw rf[L], rx[L];
+#pragma unroll
+  for (int i = 0; i < L; ++i) {
+    rf[i] = *(const Raw*)(gate + c);
+    rx[i] = *(const Raw*)(x + c);
+    if (i + 1 < n) { gate += a.s.ld_gate; x += a.s.ld_x; }
+  }
+  if (a.marks && t0 % KARMA_SCAN_MARK == 0) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) a.marks[(size_t)(t0 / KARMA_SCAN_MARK) * a.s.channels + c + e] = h[e];
+  }
+  float b[L][V];
+#pragma unroll
+  for (int i = 0; i < L; ++i) {
+    Lane<T, V>::get(rf[i], b[i]);
+#pragma unroll
+    for (int e = 0; e < V; ++e) b[i][e] = share_of(b[i][e]);
+  }
+  auto step = [&](int i) {
+    float in[V];
+    Lane<T, V>::get(rx[i], in);
+#pragma unroll
+    for (int e = 0; e < V; ++e) h[e] = step_of(b[i][e], in[e], h[e]);
+    *(Raw*)(out + c) = Lane<T, V>::put(h);
+    out += a.s.ld_h;
+  };
+  if (n == L) {
+#pragma unroll
+    for (int i = 0; i < L; ++i) step(i);
+  } else {
+#pragma unroll
+    for (int i = 0; i < L - 1; ++i) {
+      if (i >= n) break;
+      step(i);
+    }
+  }
+}
 template <typename T, int V>
 __global__ __launch_bounds__(256) void scan_fwd_short_kernel(ScanFwd a, Spans p, int blocks, int units) {
-  typedef Lane<T, V> Ln;
-  constexpr int L = 8;
   const int unit = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
   if (unit >= units) return;
   const int j = unit / blocks, C = (int)a.s.channels, c = (unit % blocks) * 64 * V + (threadIdx.x & 63) * V;
   if (c >= C) return;
-  const int first = p.at(j), last = p.at(j + 1);
+  const int first = __builtin_amdgcn_readfirstlane(p.at(j)), last = __builtin_amdgcn_readfirstlane(p.at(j + 1));
   float h[V];
 #pragma unroll
   for (int e = 0; e < V; ++e) h[e] = a.h0 ? a.h0[(size_t)j * C + c + e] : 0.f;
-  for (int t0 = first; t0 < last; t0 += L) {
-    typename Ln::Raw rf[L], rx[L];
-#pragma unroll
-    for (int i = 0; i < L; ++i) {
-      const size_t t = min(t0 + i, last - 1);
-      rf[i] = *(const typename Ln::Raw*)((const T*)a.gate + t * a.s.ld_gate + c);
-      rx[i] = *(const typename Ln::Raw*)((const T*)a.x + t * a.s.ld_x + c);
-    }
-#pragma unroll
-    for (int i = 0; i < L; ++i) {
-      const int t = t0 + i;
-      if (t >= last) break;
-      float b[V], x[V];
-      Ln::get(rf[i], b);
-      Ln::get(rx[i], x);
-      if (a.marks && t % KARMA_SCAN_MARK == 0) {
-#pragma unroll
-        for (int e = 0; e < V; ++e) a.marks[(size_t)(t / KARMA_SCAN_MARK) * C + c + e] = h[e];
-      }
-#pragma unroll
-      for (int e = 0; e < V; ++e) h[e] = step_of(share_of(b[e]), x[e], h[e]);
-      *(typename Ln::Raw*)((T*)a.h + (size_t)t * a.s.ld_h + c) = Ln::put(h);
-    }
+  for (int t = first; t < last;) {
+    const int n = min(last - t, (int)KARMA_SCAN_MARK - t % (int)KARMA_SCAN_MARK);
+    if (n >= 16) short_part<T, V, 16>(a, t, 16, c, h);      // (a copy for what most calls of many tokens take: no test a token)
+    else if (n > 4) short_part<T, V, 16>(a, t, n, c, h);
+    else short_part<T, V, 4>(a, t, n, c, h);
+    t += min(n, 16);
   }
   if (a.h_last) {
 #pragma unroll
@@ -636,13 +660,14 @@ __global__ void copy_or_zero_kernel(const float* x, float* y, size_t n) {
   if (i < n) y[i] = x ? x[i] : 0.f;
 }
 
-// Whether wavefronts take whole sequences (`units` of them).  Sequences of one length, 1024 channels in bf16, us by whole sequences /
-// in chunks: 4096 x 1 token 17.9 / 41.8, 64 x 32 8.0 / 15.7, 64 x 64 14.9 / 17.3, 64 x 128 26.2 / 26.3, 16 x 64 12.6 / 15.0,
-// 16 x 256 47.9 / 16.7; with many sequences 512 x 64 42.8 / 65.6, 256 x 128 43.1 / 64.5, 128 x 256 63.2 / 63.9.  Packed ones can have one
-// much longer than the others, which a single wavefront would be left alone with: half as many tokens on average.
+// Whether wavefronts take whole sequences (`units` of them), at 0.09 us a token where they are few.  Sequences of one length, 1024 channels
+// in bf16, us by whole sequences / in chunks: 4096 x 1 token 13.6 / 58.8, 1 x 64 7.0 / 10.5, 16 x 128 12.4 / 15.3, 16 x 256 22.9 / 16.5;
+// where there are 512 units (8 a sequence here) 64 x 256 30.2 / 35.4, 64 x 512 52.7 / 58.2, with fewer 32 x 256 27.4 / 23.2.  Of packed
+// ones nobody here knows the longest: as many tokens as it can have without being slower.  64 x 8 4.7 / 22.2, 63 x 1 and one of 512 43.6 / 59.7,
+// 20 x 1 and one of 512 43.8 / 43.1, of 1024 84 / 44.
 bool whole_sequences(const karma_scan_shape& s, bool packed, uint64_t units) {
-  const uint64_t most = packed ? 32 : units >= 2048 ? 128 : 64;
-  return s.tokens <= most * s.sequences;
+  if (packed) return s.tokens <= s.sequences + 512ull && s.tokens <= 128ull * s.sequences;
+  return s.tokens <= (units >= 512 ? 512ull : 128ull) * s.sequences;
 }
 
 // chunks of a call; channels of all blocks whatever a lane has

@@ -336,3 +336,28 @@ def test_offsets_beyond_32_bits(torch):
                                                C.c_uint64(p.ws_bytes), C.c_void_p(torch.cuda.current_stream().cuda_stream)) == K.OK
     torch.cuda.synchronize()
     assert torch.equal(wide[:, 2 * channels:3 * channels], p.h)
+
+
+@pytest.mark.parametrize("bf16", [True, False])
+@pytest.mark.parametrize("starts,tokens,sequences,channels", [
+    (None, 64 * 300, 64, 1032),                                             # whole sequences with marks at any of their tokens
+    (None, 17 * 93, 17, 70), (None, 21, 1, 33), (None, 3 * 4, 3, 12), (None, 5 * 16, 5, 20),
+    ([0, 250, 262, 262, 300, 513, 514, 520], 523, 7, 50),                   # packed, on both sides of a mark
+    ([0] + [500 + k for k in range(40)], 539, 40, 40),                      # one long one and single tokens
+    ([0] + [600 + k for k in range(40)], 639, 40, 40)])
+def test_short_sequences(torch, starts, tokens, sequences, channels, bf16):
+    both(Problem(torch, 26, tokens, channels, sequences, starts, bf16=bf16))
+
+
+def test_nothing_where_nothing_is_needed(torch):
+    """No workspace where a call needs none, and no tensors where there are no tokens."""
+    p = Problem(torch, 27, 200, 40)
+    assert K.gated_scan_ws_bytes(p.shape) == 0
+    p.ws = None
+    both(p)
+    e = Problem(torch, 28, 0, 40, 3)
+    e.ws = None
+    e.forward(marks=False, gate=None, x=None, h=None)
+    e.backward(gate=None, x=None, marks=None, dh=None, dgate=None, dx=None)
+    torch.cuda.synchronize()
+    assert torch.equal(e.h_last, e.h0) and torch.equal(e.dh0, e.dh_last)

@@ -312,3 +312,19 @@ def test_offsets_beyond_32_bits(torch):
     p.backward()
     p.check_forward()       # (not the same bits: rows on other boundaries are added up in another order)
     p.check_backward()
+
+
+def test_no_workspace_where_none_is_needed(torch):
+    p = Problem(torch, 20, 70, 1500, top=4)
+    assert p.ws_bytes == 0
+    p.ws = None
+    both(p)
+    e = Problem(torch, 21, 0, 1500)
+    e.ws = e.flat = e.z = None
+    fn = K.lib()
+    q = e.q(None)
+    assert fn.karma_k_token_logprob_fwd_bf16(None, C.c_uint64(0), ptr(p.tokens), ptr(p.logprob), None, None, None, None, 0, 1500, 0, C.c_float(1), None,
+                                             C.c_uint64(0), q) == K.OK
+    assert fn.karma_k_token_logprob_bwd_bf16(None, C.c_uint64(0), ptr(p.tokens), None, None, ptr(p.dlogprob), None, None, C.c_uint64(0), 0, 1500,
+                                             C.c_float(1), q) == K.OK
+    p.check_forward()
