@@ -608,7 +608,8 @@ int karma_k_attention_bwd_bf16(const void* qkv_dev, const void* ctx_dev, const v
 #define KARMA_SCAN_MARK 256u
 typedef struct {
   uint64_t tokens;              /* rows of the tensors, < 2^31 - 1024 */
-  uint32_t channels, sequences; /* at least one of each */
+  uint32_t channels, sequences; /* at least one of each.  With channels up to the next multiple of 64: times sequences <= 2^32 - 256, and times
+                                   (256 + tokens up to the next multiple of 256) < 2^36 */
   uint64_t ld_gate, ld_x, ld_h, ld_dgate, ld_dx; /* elements; ld_h: of h and of dh */
 } karma_scan_shape;
 uint64_t karma_k_gated_scan_ws_bytes(const karma_scan_shape* shape);
@@ -640,7 +641,7 @@ int karma_k_gated_scan_bwd_f32(const float* gate_dev, const float* x_dev, const 
  * A logit of -inf is not allowed: its probability is 0.  A row of nothing else has q = -inf, entropy 0 and gradient 0.  +inf
  * or NaN in a row makes its results NaN (NaN is no alternative; where too few are left the index is -1).
  * ws_dev: karma_k_token_logprob_ws_bytes(rows, cols, top) bytes, 16-byte aligned, for one call at a time (0 bytes: may be NULL).
- * Errors: KARMA_E_INVAL, KARMA_E_OOM. */
+ * rows < 2^24, and rows x (cols / 1024, rounded up) <= 2^26 - 4 in the backward pass.  Errors: KARMA_E_INVAL, KARMA_E_OOM. */
 #define KARMA_TOP_MAX 64u
 uint64_t karma_k_token_logprob_ws_bytes(uint32_t rows, uint32_t cols, uint32_t top);
 int karma_k_token_logprob_fwd_bf16(const void* logits_dev, uint64_t ld, const int32_t* tokens_dev, float* logprob_dev, float* entropy_dev,
@@ -669,7 +670,7 @@ int karma_k_token_logprob_bwd_f32(const float* logits_dev, uint64_t ld, const in
  * expectation kept (v > 0 becomes at least code 1).  The random bits follow from `seed`, the tensor's place in the list and the element's:
  * give every step another seed.  A gradient that is not finite, or whose square is not, makes the scales, and with them the
  * moments, of its block NaN.
- * Without the flag m and v are fp32 [n].  Tensors overlap nothing, other tensors of the list included; n may be 0.
+ * Without the flag m and v are fp32 [n].  Tensors overlap nothing, other tensors of the list included; n from 0 to 2^34 - 1024.
  * tensors is a host array, read during the call.  live_dev (may be NULL): lr, grad_scale, step and seed are read from there when
  * the kernels run, not from `now`: for a captured graph, which is replayed with other values (a step of 0 counts as 1).
  * Errors: KARMA_E_INVAL (step 0 and betas outside [0, 1) among them). */

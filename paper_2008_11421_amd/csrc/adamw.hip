@@ -190,6 +190,7 @@ __device__ __forceinline__ Codes quantised_step(const Codes& c, const f32x4& g, 
 // value (bf16 gradient and weight), 16.25 with 8-bit moments: bound by memory.  217 M values in 8 bits take 711 us, 5.0 TB/s, 63 M in
 // 609 tensors 376 us; four groups of 1024 a workgroup, loaded ahead, take 813 and 430 (more registers, fewer wavefronts).
 constexpr unsigned ADAMW_SPAN = 1024;
+constexpr unsigned ADAMW_GRID = (1u << 24) - 1;     // workgroups of 256 lanes in a launch, which has less than 2^32
 template <bool EIGHT>
 __global__ __launch_bounds__(256) void adamw_kernel(AdamwSet<EIGHT> u, AdamwNow a) {
   const int tensor = tensor_of(u);
@@ -274,7 +275,7 @@ __global__ __launch_bounds__(256) void adamw_states_kernel(StatesSet u) {
 bool aligned_to(const void* p, size_t n) { return (uintptr_t)p % n == 0; }
 bool eight_bits(const karma_adamw_tensor& t) { return t.flags & KARMA_ADAMW_STATES_8BIT; }
 bool good_states(const karma_adamw_tensor& t) {
-  if (t.n > ((uint64_t)1 << 40) || (t.flags & ~7u)) return false;
+  if (t.n > (uint64_t)ADAMW_GRID * ADAMW_SPAN || (t.flags & ~7u)) return false;
   if (!t.n) return true;
   if (!t.m || !t.v) return false;
   if (eight_bits(t)) return t.m_scale && t.v_scale && aligned_to(t.m_scale, 4) && aligned_to(t.v_scale, 4);
@@ -291,9 +292,9 @@ bool in_sets(const karma_adamw_tensor* tensors, uint32_t n, Fill fill, Launch la
     u.first[0] = 0;
     uint64_t blocks = 0;
     for (; k < n && u.n < Set::MOST; ++k) {
-      const uint64_t more = (tensors[k].n + ADAMW_SPAN - 1) / ADAMW_SPAN;     // (2^30 at most)
+      const uint64_t more = (tensors[k].n + ADAMW_SPAN - 1) / ADAMW_SPAN;     // (ADAMW_GRID at most)
       if (!more || !fill(u.t[u.n], k)) continue;
-      if (blocks + more > INT32_MAX) break;
+      if (blocks + more > ADAMW_GRID) break;
       blocks += more;
       u.first[++u.n] = (unsigned)blocks;
     }

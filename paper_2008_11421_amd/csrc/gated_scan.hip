@@ -682,7 +682,9 @@ int check_scan(karma_scan_shape& s, const void* starts) {
     if (!*ld) *ld = s.channels;
     if (*ld < s.channels || *ld > INT64_MAX / 8 / (s.tokens + 1)) return KARMA_E_INVAL;
   }
-  if ((uint64_t)((s.channels + 63) / 64) * std::max<uint64_t>(s.sequences, scan_chunks(s.tokens) + 1) > INT32_MAX) return KARMA_E_INVAL;
+  // a launch has less than 2^32 lanes: 64 for a sequence's block of channels, 1024 for a chunk's
+  const uint64_t blocks = ((uint64_t)s.channels + 63) / 64;
+  if (blocks * s.sequences > (1u << 26) - 4 || blocks * (scan_chunks(s.tokens) + 1) >= 1u << 22) return KARMA_E_INVAL;
   return KARMA_OK;
 }
 bool aligned_to(const void* p, size_t n) { return (uintptr_t)p % n == 0; }
@@ -748,7 +750,6 @@ int gated_scan_bwd(ScanBwd a, bool bf16, hipStream_t s) {
   if (!a.s.tokens) {      // the gradient of a state that no token changed
     if (!a.dh0) return KARMA_OK;
     const size_t n = (size_t)a.s.sequences * a.s.channels;
-    if (n > (size_t)INT32_MAX * 256) return KARMA_E_INVAL;
     hipLaunchKernelGGL(copy_or_zero_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, a.dh_last, a.dh0, n);
     return hipGetLastError() == hipSuccess ? KARMA_OK : KARMA_E_HIP;
   }

@@ -547,11 +547,12 @@ LogprobCut cut_rows(uint32_t rows, uint32_t cols, bool bf16) {
   if (parts <= 1) return LogprobCut{vectors <= (rows >= 4096 ? 512u : (unsigned)LP_THREADS) ? 1u : (unsigned)LP_WAVES, 1};
   return LogprobCut{(unsigned)LP_WAVES, parts};
 }
+constexpr uint32_t LP_GRID = (1u << 24) - 1;        // workgroups of 256 lanes in a launch, which has less than 2^32
 size_t up16(size_t b) { return (b + 15) / 16 * 16; }
 
 bool aligned_to(const void* p, size_t n) { return (uintptr_t)p % n == 0; }
 bool good_rows(uint32_t rows, uint32_t cols, uint64_t ld) {
-  return cols && cols <= INT32_MAX && rows <= INT32_MAX && ld >= cols && ld <= INT64_MAX / 8 / ((uint64_t)rows + 1);
+  return cols && cols <= INT32_MAX && rows <= LP_GRID && ld >= cols && ld <= INT64_MAX / 8 / ((uint64_t)rows + 1);
 }
 
 }  // namespace
@@ -597,7 +598,7 @@ int token_logprob_bwd(LogprobBwd a, bool bf16, hipStream_t s) {
   if (!a.rows) return KARMA_OK;
   if (!a.logits || !a.stats || !a.dlogits || !aligned_to(a.logits, bf16 ? 2 : 4) || !aligned_to(a.dlogits, bf16 ? 2 : 4)) return KARMA_E_INVAL;
   const unsigned vectors = a.cols / (bf16 ? 8 : 4), units = std::max(1u, (vectors + 64 * LP_BATCH - 1) / (64 * LP_BATCH));
-  if ((uint64_t)a.rows * units > INT32_MAX) return KARMA_E_INVAL;
+  if ((uint64_t)a.rows * units > (uint64_t)LP_GRID * LP_WAVES) return KARMA_E_INVAL;
   const unsigned grid = (a.rows * units + LP_WAVES - 1) / LP_WAVES;
   if (bf16) hipLaunchKernelGGL(logprob_bwd_kernel<bf16_t>, dim3(grid), dim3(LP_THREADS), 0, s, a, units);
   else hipLaunchKernelGGL(logprob_bwd_kernel<float>, dim3(grid), dim3(LP_THREADS), 0, s, a, units);

@@ -163,3 +163,15 @@ def test_adamw_refusals():
     t = (K.AdamwTensor * 1)(K.AdamwTensor(**dict(tensor, flags=4, m_scale=4096, v_scale=4096)))
     assert lib.karma_k_adamw_states(t, 1, (C.c_void_p * 1)(None), ptrs, None) == K.E_INVAL
     assert lib.karma_k_adamw_states(t, 1, None, ptrs, None) == K.E_INVAL
+
+
+def test_sizes_beyond_a_launch_are_refused():
+    for bad in (dict(tokens=1 << 30, channels=64, sequences=1), dict(tokens=(1 << 31) - 2048, channels=1, sequences=1),
+                dict(tokens=1 << 26, channels=1, sequences=1 << 26), dict(tokens=1024, channels=1 << 27, sequences=2)):
+        assert scan_fwd(K.ScanShape(**bad), ws_bytes=1 << 62) == K.E_INVAL and K.gated_scan_ws_bytes(K.ScanShape(**bad)) == 0, bad
+    assert K.gated_scan_ws_bytes(K.ScanShape(tokens=1 << 29, channels=64, sequences=1)) > 0
+    assert logprob_fwd(rows=1 << 24, cols=4096) == K.E_INVAL and logprob_fwd(rows=1 << 26, cols=8) == K.E_INVAL
+    assert logprob_bwd(rows=1 << 24, cols=8192) == K.E_INVAL and logprob_bwd(rows=1 << 26, cols=8) == K.E_INVAL
+    step = K.AdamwStep(lr=1e-3, beta1=0.9, beta2=0.95, eps=1e-8, grad_scale=1.0, seed=1, step=1)
+    t = (K.AdamwTensor * 1)(K.AdamwTensor(w=4096, m=4096, v=4096, grad=4096, n=1 << 34, flags=0))
+    assert K.lib().karma_k_adamw(t, 1, C.byref(step), None, None) == K.E_INVAL
