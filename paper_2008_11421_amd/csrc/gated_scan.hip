@@ -134,18 +134,19 @@ __device__ __forceinline__ Part part_of(const Spans& p, int t0, unsigned long lo
 // A chunk of KARMA_SCAN_MARK tokens and some channels belongs to a workgroup.  What it does to the state that comes in is
 // out = A in + H; it publishes both at once (8 bytes a channel; A below 0: out = H, a sequence began in it) and waits for the state
 // behind the chunk before it, which one wavefront per block of channels carries through all chunks in their order: the same sums in
-// the same order every time, without a trip to memory between one chunk and the next.  Workgroups take their work by a counter, the
+// the same order every time, without a trip to memory between one chunk and the next.  Workgroups take their work by counters, the
 // carriers first, so whoever is waited for is already running.  A word of all ones is not there yet.  A wait that never ends (a
 // workspace that another call is using) is given up, and the states become NaN.
-// 65536 tokens of 2048 channels: 188 us a call, of which 6 to clear the words; 171 in the kernel if nobody waited (what a copy of the same
+// 65536 tokens of 2048 channels: 175 us a call, of which 6 to clear the words; 171 in the kernel if nobody waited (what a copy of the same
 // bytes takes is 169); chunks of 128 tokens 225 in the kernel, of 64 373 (a chunk costs the chain 0.35 us), of 512 378 (one workgroup
 // on a compute unit: nothing hides its waits).
 struct Chain {
-  unsigned* ticket;
+  unsigned* tickets;            // one for every block of channels, CHAIN_APART numbers from one to the next
   unsigned long long* effect;   // [chunk][channel]
   unsigned* state;              // behind the chunk
   int chunks, blocks, width;    // blocks of channels, channels of all blocks; chunks == 1: no chain
 };
+constexpr int CHAIN_APART = 32;         // 128 bytes: counters of their own cache lines
 constexpr int CHAIN_LIMIT = 1 << 20;    // looks at a word, a microsecond or so each
 
 __device__ __forceinline__ unsigned long long effect_word(float A, float H, bool cut) {
@@ -210,32 +211,36 @@ __device__ __forceinline__ void carry(const Chain& c, int channel, bool up) {
     if (done != before) n = 0;
   }
 }
-// all words behind the counter, 12 bytes a chunk and channel, widths being multiples of 128
+// all words behind the counters, 12 bytes a chunk and channel, widths being multiples of 128
 __global__ __launch_bounds__(256) void chain_clear_kernel(Chain c, size_t pieces) {
   const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
-  if (i == 0) *c.ticket = 0;
+  if (i < (size_t)c.blocks) c.tickets[i * CHAIN_APART] = 0;
   if (i < pieces) ((u32x4*)c.effect)[i] = u32x4{~0u, ~0u, ~0u, ~0u};
 }
 
-// The work of this workgroup: a chunk and a block of channels, or false for a carrier, which has then done its work.
+// The work of this workgroup: a chunk and a block of channels, or false for a carrier, which has then done its work.  Forward, each block of
+// channels has a counter: 512 workgroups that begin at once wait up to 6 us for one (packed prompts 53 us in the kernel instead of
+// 57, 65536 x 2048 180 instead of 187).  Backward they share one: its workgroups gain by not loading all at the same time (86 us, 91 with
+// counters of their own).  Carriers of eight blocks in one workgroup look slower than they save places: 64 us instead of 53.
 template <int V>
 __device__ __forceinline__ bool take_work(const Chain& c, bool up, int& chunk, int& block) {
   __shared__ unsigned ticket;
-  int unit = blockIdx.x;
-  if (c.chunks > 1) {
-    if (threadIdx.x == 0) ticket = atomicAdd(c.ticket, 1u);
-    __syncthreads();
-    unit = __builtin_amdgcn_readfirstlane((int)ticket);
-    if (unit < c.blocks) {
-      if (threadIdx.x < 64) carry<V>(c, unit * 64 * V + threadIdx.x * V, up);
-      return false;
-    }
-    unit -= c.blocks;
-    if (unit >= c.blocks * c.chunks) return false;      // (the counter is another call's too)
+  const unsigned own = blockIdx.x % c.blocks, first = up ? own : 0, sharing = up ? 1 : c.blocks;    // blocks that share the counter
+  chunk = 0;
+  block = own;
+  if (c.chunks == 1) return true;
+  if (threadIdx.x == 0) ticket = atomicAdd(c.tickets + (size_t)first * CHAIN_APART, 1u);
+  __syncthreads();
+  unsigned unit = __builtin_amdgcn_readfirstlane((int)ticket);
+  if (unit < sharing) {
+    if (threadIdx.x < 64) carry<V>(c, (first + unit) * 64 * V + threadIdx.x * V, up);
+    return false;
   }
-  chunk = unit / c.blocks;
+  unit -= sharing;
+  if (unit >= sharing * c.chunks) return false;     // (the counter is another call's too)
+  chunk = unit / sharing;
   if (!up) chunk = c.chunks - 1 - chunk;
-  block = unit % c.blocks;
+  block = first + unit % sharing;
   return true;
 }
 
@@ -691,14 +696,15 @@ bool aligned_to(const void* p, size_t n) { return (uintptr_t)p % n == 0; }
 
 }  // namespace
 
-constexpr size_t CHAIN_HEAD = 256;      // the counter
+// the counters of blocks of 64 channels, which are the more
+static size_t chain_head(uint64_t width) { return width / 64 * CHAIN_APART * sizeof(unsigned); }
 
 size_t gated_scan_ws_bytes(const karma_scan_shape& given) {
   karma_scan_shape shape = given;
   const int any = 0;      // (whether all sequences have one length does not matter here)
   if (check_scan(shape, &any)) return 0;
-  const uint64_t chunks = scan_chunks(shape.tokens);
-  return chunks > 1 ? CHAIN_HEAD + chunks * scan_width(shape.channels) * 12 : 0;
+  const uint64_t chunks = scan_chunks(shape.tokens), width = scan_width(shape.channels);
+  return chunks > 1 ? chain_head(width) + chunks * width * 12 : 0;
 }
 
 static Spans spans_of(const karma_scan_shape& s, const int* starts) {
@@ -707,7 +713,7 @@ static Spans spans_of(const karma_scan_shape& s, const int* starts) {
 // V channels a lane; the chain is cleared by a kernel ahead (a call that is captured has kernels alone)
 static Chain chain_of(const karma_scan_shape& s, int V, void* ws, hipStream_t stream) {
   const uint64_t chunks = scan_chunks(s.tokens), width = scan_width(s.channels);
-  unsigned long long* effect = (unsigned long long*)((char*)ws + CHAIN_HEAD);
+  unsigned long long* effect = (unsigned long long*)((char*)ws + chain_head(width));
   const Chain c{(unsigned*)ws, effect, (unsigned*)(effect + chunks * width), (int)chunks, (int)((s.channels + 64 * V - 1) / (64 * V)), (int)width};
   const size_t pieces = chunks * width * 12 / 16;
   if (chunks > 1) hipLaunchKernelGGL(chain_clear_kernel, dim3((unsigned)((pieces + 255) / 256)), dim3(256), 0, stream, c, pieces);
