@@ -274,6 +274,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(4))) voi
   const Part q = part_of<L>(p, t0, words + w);
   const unsigned all = L == 32 ? ~0u : (1u << (L & 31)) - 1;
   const bool plain = q.inside == all && !q.begins && !q.ends;
+  const int latest = 31 - __builtin_clz(q.begins | 1);      // the last token that begins a sequence, if one does
   auto initial = [&](int j, float (&v)[V]) {
 #pragma unroll
     for (int e = 0; e < V; ++e) v[e] = a.h0 ? a.h0[p.row(j, C) + c + e] : 0.f;
@@ -281,7 +282,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(4))) voi
   // the state that the last sequence to begin here begins with: asked for while the inputs are under way, and kept, as by the second run
   // h_last may lie over it
   float b[L][V], A[V], h[V], begun[V] = {};
-  if (q.begins) initial(p.next(q.seq, t0 + 31 - __builtin_clz(q.begins)), begun);
+  if (q.begins) initial(p.next(q.seq, t0 + latest), begun);
 #pragma unroll
   for (int e = 0; e < V; ++e) { A[e] = 1.f; h[e] = 0.f; }
 #pragma unroll
@@ -299,27 +300,17 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(4))) voi
       for (int e = 0; e < V; ++e) { h[e] = step_of(b[i][e], x[e], h[e]); A[e] = fmaf(-b[i][e], A[e], A[e]); }
     }
   } else {
-    int j = q.seq;
-    for (unsigned left = q.inside; left;) {
-      const unsigned run = first_run(q, left);
-      left &= ~run;
-      if (q.begins & run) {
-        j = p.next(j, t0 + __builtin_ctz(run));
-        if (q.begins & left) {
-          initial(j, h);
-        } else {
+    // (what lies before the last beginning has no effect behind the part)
+    const unsigned run = q.inside & ~0u << latest;
 #pragma unroll
-          for (int e = 0; e < V; ++e) h[e] = begun[e];
-        }
-      }
+    for (int e = 0; e < V; ++e) h[e] = begun[e];
 #pragma unroll
-      for (int i = 0; i < L; ++i) {
-        if (!(run >> i & 1)) continue;
-        float x[V];
-        Ln::get(as_new(rx[i]), x);
+    for (int i = 0; i < L; ++i) {
+      if (!(run >> i & 1)) continue;
+      float x[V];
+      Ln::get(as_new(rx[i]), x);
 #pragma unroll
-        for (int e = 0; e < V; ++e) { h[e] = step_of(b[i][e], x[e], h[e]); A[e] = fmaf(-b[i][e], A[e], A[e]); }
-      }
+      for (int e = 0; e < V; ++e) { h[e] = step_of(b[i][e], x[e], h[e]); A[e] = fmaf(-b[i][e], A[e], A[e]); }
     }
   }
 #pragma unroll
@@ -540,22 +531,20 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(5))) voi
 #pragma unroll
     for (int e = 0; e < V; ++e) { const float D = d[e] + g[e]; g[e] = fmaf(-b[i][e], D, D); }
   };
+  // (what lies before the last beginning has no effect on later states, what lies behind the first end none on earlier gradients)
+  const int latest = 31 - __builtin_clz(q.begins | 1), earliest = __builtin_ctz(q.ends | 1u << (L - 1));
   int j = q.seq;
-#pragma unroll
-  for (int i = 0; i < L; ++i) {
-    if (q.begins >> i & 1) {
-      if (STATES) j = p.next(j, t0 + i);
-      initial(j, h);
-    }
-    step(i);
-  }
+  if (STATES && q.begins) j = p.next(j, t0 + latest);
   const int last_seq = j;     // of the part's last token
 #pragma unroll
+  for (int i = 0; i < L; ++i) {
+    if (i == latest && q.begins) initial(j, h);
+    step(i);
+  }
+  if (STATES && q.ends) j = p.previous(j, t0 + earliest);
+#pragma unroll
   for (int i = L - 1; i >= 0; --i) {
-    if (q.ends >> i & 1) {
-      if (STATES) j = p.previous(j, t0 + i);
-      final_gradient(j, g);
-    }
+    if (i == earliest && q.ends) final_gradient(j, g);
     back(i);
   }
 #pragma unroll
@@ -668,8 +657,8 @@ __global__ void copy_or_zero_kernel(const float* x, float* y, size_t n) {
 // Whether wavefronts take whole sequences (`units` of them), at 0.09 us a token where they are few.  Sequences of one length, 1024 channels
 // in bf16, us by whole sequences / in chunks: 4096 x 1 token 13.6 / 58.8, 1 x 64 7.0 / 10.5, 16 x 128 12.4 / 15.3, 16 x 256 22.9 / 16.5;
 // where there are 512 units (8 a sequence here) 64 x 256 30.2 / 35.4, 64 x 512 52.7 / 58.2, with fewer 32 x 256 27.4 / 23.2.  Of packed
-// ones nobody here knows the longest: as many tokens as it can have without being slower.  64 x 8 4.7 / 22.2, 63 x 1 and one of 512 43.6 / 59.7,
-// 20 x 1 and one of 512 43.8 / 43.1, of 1024 84 / 44.
+// ones nobody here knows the longest: up to 512 tokens more than sequences, of which it can have 513 at most.  64 x 8 4.7 / 18.9,
+// 64 x 16 5.1 / 16.8, 63 x 1 and one of 512 43.6 / 36.2, 20 x 1 and one of 1024 84 / 28, 63 x 1 and one of 1900 180 / 36.7.
 bool whole_sequences(const karma_scan_shape& s, bool packed, uint64_t units) {
   if (packed) return s.tokens <= s.sequences + 512ull && s.tokens <= 128ull * s.sequences;
   return s.tokens <= (units >= 512 ? 512ull : 128ull) * s.sequences;
