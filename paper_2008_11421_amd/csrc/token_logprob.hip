@@ -498,7 +498,9 @@ __global__ __launch_bounds__(LP_THREADS) void logprob_bwd_kernel(LogprobBwd a, u
   const float c2 = a.scale * 1.44269504f, ls2 = ls * 1.44269504f;
   auto grad = [&](float z, unsigned j) {
     const float q2 = fmaf(z - m, c2, -ls2), p = __builtin_amdgcn_exp2f(q2);
-    float v = -p * dl - p * (de * fmaf(fmaxf(q2, -1e30f), 0.693147181f, ent));    // (bounded: -inf times a p of 0)
+    // p = 0: nothing, whatever it is multiplied with (q2 of -inf or -1e20, a de that has overflowed).  NaN is not 0.  Elsewhere q2 is above
+    // -150, and p comes before de: the product of the two is of the order of one.
+    float v = p == 0.f ? 0.f : -p * dl - p * fmaf(q2, 0.693147181f, ent) * de;
     if ((int)j == token) v += dl;
     return empty ? 0.f : v;
   };

@@ -328,3 +328,23 @@ def test_no_workspace_where_none_is_needed(torch):
     assert fn.karma_k_token_logprob_bwd_bf16(None, C.c_uint64(0), ptr(p.tokens), None, None, ptr(p.dlogprob), None, None, C.c_uint64(0), 0, 1500,
                                              C.c_float(1), q) == K.OK
     p.check_forward()
+
+
+@pytest.mark.parametrize("bf16", [True, False])
+@pytest.mark.parametrize("scale,weight,spread", [(1e10, 0.1, 3.0), (1e20, 1.0, 3.0), (1e19, 1.0, 3.0), (1.0, 1e9, 3.0), (1.0, 65536.0 * 1e30, 3.0),
+                                                 (1e-20, 1.0, 3.0), (1e20, 1.0, 1e-20), (1e20, 1e15, 1e-20)])
+@pytest.mark.parametrize("rows,cols", [(7, 900), (2, 30000)])
+def test_entropy_gradient_where_scale_times_gradient_is_large(torch, rows, cols, scale, weight, spread, bf16):
+    """A column that is not allowed, or whose probability is nothing, has no gradient, whatever the entropy's is."""
+    z = np.random.default_rng(22).standard_normal((rows, cols)) * spread
+    z[:, 100:300] = NEG
+    z[0, 1:] = NEG
+    p = Problem(torch, 23, rows, cols, bf16, scale=scale, z=z)
+    p.dentropy.mul_(weight)
+    p.forward()
+    p.backward()
+    p.check_backward()
+    assert (p.d[:, 150:250].masked_fill((p.tokens[:, None] >= 150) & (p.tokens[:, None] < 250), 0) == 0).all()
+    p.backward(dlogprob=None, tokens=None)
+    p.check_backward(dlogprob=False)
+    assert (p.d[:, 100:300] == 0).all()
