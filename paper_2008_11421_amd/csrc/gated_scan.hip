@@ -2,8 +2,8 @@
 //   b_t = 1 / (1 + e^f_t)  (one minus the gate's sigmoid),  h_t = h_{t-1} + b_t (x_t - h_{t-1}).
 // Gradients, from the last token to the first, with g the gradient of the state behind the token:
 //   D_t = dh_t + g,  dx_t = b_t D_t,  df_t = D_t (h_{t-1} - x_t) (b_t - b_t^2),  g = D_t - b_t D_t.
-// The weight b of the new value is computed, not the decay 1 - b: where a state lives for thousands of tokens b is small,
-// and 1 - b rounded to 32 bits would lose it.  States and carries are fp32.
+// Of b and a = 1 - b the smaller one is computed, and the other never: rounded to 32 bits it would lose what the smaller one says, how
+// long a state lives where b is small, what is left of it where a is.  States and carries are fp32.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -38,9 +38,35 @@ struct Lane<float, 1> {
   static __device__ __forceinline__ Raw put(const float (&v)[1]) { return v[0]; }
 };
 
-// b = 1 / (1 + e^f): 1 for -inf, 0 for +inf
-__device__ __forceinline__ float share_of(float f) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(f * 1.44269504f)); }
-__device__ __forceinline__ float step_of(float b, float x, float h) { return fmaf(b, x - h, h); }
+// The smaller share s = e^-|f| / (1 + e^-|f|) with the gate's sign: s = b where f is positive, -s = a = 1 - b where it is negative (a sign
+// of 0 too: both gates of infinity have s = 0).  Then h + b (x - h) is h + s (x - h) or x + s (x - h), and a product with a or b that is
+// not s itself is the factor without its share s.
+__device__ __forceinline__ float share_of(float f) {
+  const float E = __builtin_amdgcn_exp2f(fabsf(f) * -1.44269504f);
+  return copysignf(E * __builtin_amdgcn_rcpf(1.f + E), f);
+}
+__device__ __forceinline__ float step_of(float s, float x, float h) { return fmaf(s, x - h, __builtin_signbitf(s) ? x : h); }
+// The choice by the sign, where a part is run through more than once: a mask of the sign and a merge of bits, in assembly, as the compiler
+// would make comparisons of them and keep all those for the later runs, 64 pairs of scalar registers (and spill a hundred of them).
+__device__ __forceinline__ float by_sign(float s, float positive, float negative) {
+  float r;
+  asm("v_ashrrev_i32 %0, 31, %1\n\tv_bfi_b32 %0, %0, %3, %2" : "=&v"(r) : "v"(s), "v"(positive), "v"(negative));
+  return r;
+}
+__device__ __forceinline__ float where_positive(float s, float v) {
+  float r;
+  asm("v_ashrrev_i32 %0, 31, %1\n\tv_bfi_b32 %0, %0, 0, %2" : "=&v"(r) : "v"(s), "v"(v));
+  return r;
+}
+__device__ __forceinline__ float kept(float s, float v) { return fmaf(-s, v, where_positive(s, v)); }      // a v
+// a step of the state h and of the decay A of all steps so far
+__device__ __forceinline__ void effect_of(float s, float x, float& h, float& A) {
+  float base, rest;
+  asm("v_ashrrev_i32 %0, 31, %2\n\tv_bfi_b32 %1, %0, 0, %5\n\tv_bfi_b32 %0, %0, %4, %3"
+      : "=&v"(base), "=&v"(rest) : "v"(s), "v"(h), "v"(x), "v"(A));
+  h = fmaf(s, x - h, base);
+  A = fmaf(-s, A, rest);
+}
 
 // The compiler is not to keep what it made of a value that is used again later: the unpacked inputs of two runs through a part, and the
 // addresses of all its rows, would take twice the registers (240 instead of 120 in the forward kernel).
@@ -281,15 +307,15 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(4))) voi
   };
   // the state that the last sequence to begin here begins with: asked for while the inputs are under way, and kept, as by the second run
   // h_last may lie over it
-  float b[L][V], A[V], h[V], begun[V] = {};
+  float s[L][V], A[V], h[V], begun[V] = {};
   if (q.begins) initial(p.next(q.seq, t0 + latest), begun);
 #pragma unroll
   for (int e = 0; e < V; ++e) { A[e] = 1.f; h[e] = 0.f; }
 #pragma unroll
   for (int i = 0; i < L; ++i) {
-    Ln::get(rf[i], b[i]);
+    Ln::get(rf[i], s[i]);
 #pragma unroll
-    for (int e = 0; e < V; ++e) b[i][e] = share_of(b[i][e]);
+    for (int e = 0; e < V; ++e) s[i][e] = share_of(s[i][e]);
   }
   if (plain) {
 #pragma unroll
@@ -297,7 +323,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(4))) voi
       float x[V];
       Ln::get(as_new(rx[i]), x);
 #pragma unroll
-      for (int e = 0; e < V; ++e) { h[e] = step_of(b[i][e], x[e], h[e]); A[e] = fmaf(-b[i][e], A[e], A[e]); }
+      for (int e = 0; e < V; ++e) effect_of(s[i][e], x[e], h[e], A[e]);
     }
   } else {
     // (what lies before the last beginning has no effect behind the part)
@@ -310,7 +336,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(4))) voi
       float x[V];
       Ln::get(as_new(rx[i]), x);
 #pragma unroll
-      for (int e = 0; e < V; ++e) { h[e] = step_of(b[i][e], x[e], h[e]); A[e] = fmaf(-b[i][e], A[e], A[e]); }
+      for (int e = 0; e < V; ++e) effect_of(s[i][e], x[e], h[e], A[e]);
     }
   }
 #pragma unroll
@@ -359,7 +385,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(4))) voi
       float x[V];
       Ln::get(as_new(rx[i]), x);
 #pragma unroll
-      for (int e = 0; e < V; ++e) h[e] = step_of(b[i][e], x[e], h[e]);
+      for (int e = 0; e < V; ++e) h[e] = fmaf(s[i][e], x[e] - h[e], by_sign(s[i][e], h[e], x[e]));
       store(i);
     }
   } else {
@@ -382,7 +408,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(4))) voi
         float x[V];
         Ln::get(as_new(rx[i]), x);
 #pragma unroll
-        for (int e = 0; e < V; ++e) h[e] = step_of(b[i][e], x[e], h[e]);
+        for (int e = 0; e < V; ++e) h[e] = fmaf(s[i][e], x[e] - h[e], by_sign(s[i][e], h[e], x[e]));
         store(i);
       }
       if ((q.ends & run) && a.h_last && mine) {
@@ -420,18 +446,18 @@ __device__ __forceinline__ void short_part(const ScanFwd& a, int t0, int n, unsi
 #pragma unroll
     for (int e = 0; e < V; ++e) a.marks[(size_t)(t0 / KARMA_SCAN_MARK) * a.s.channels + c + e] = h[e];
   }
-  float b[L][V];
+  float s[L][V];
 #pragma unroll
   for (int i = 0; i < L; ++i) {
-    Lane<T, V>::get(rf[i], b[i]);
+    Lane<T, V>::get(rf[i], s[i]);
 #pragma unroll
-    for (int e = 0; e < V; ++e) b[i][e] = share_of(b[i][e]);
+    for (int e = 0; e < V; ++e) s[i][e] = share_of(s[i][e]);
   }
   auto step = [&](int i) {
     float in[V];
     Lane<T, V>::get(rx[i], in);
 #pragma unroll
-    for (int e = 0; e < V; ++e) h[e] = step_of(b[i][e], in[e], h[e]);
+    for (int e = 0; e < V; ++e) h[e] = step_of(s[i][e], in[e], h[e]);
     *(Raw*)(out + c) = Lane<T, V>::put(h);
     out += a.s.ld_h;
   };
@@ -502,14 +528,14 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(5))) voi
     for (int e = 0; e < V; ++e) marks[lane * V + e] = a.marks[(size_t)chunk * C + c + e];
   }
   const Part q = part_of<L>(p, t0, words + w);
-  float b[L][V], A[V], h[V], g[V];
+  float s[L][V], A[V], h[V], g[V];
 #pragma unroll
   for (int e = 0; e < V; ++e) { A[e] = 1.f; h[e] = 0.f; g[e] = 0.f; }
 #pragma unroll
   for (int i = 0; i < L; ++i) {
-    Ln::get(rf[i], b[i]);
+    Ln::get(rf[i], s[i]);
 #pragma unroll
-    for (int e = 0; e < V; ++e) b[i][e] = q.inside >> i & 1 ? share_of(b[i][e]) : 0.f;
+    for (int e = 0; e < V; ++e) s[i][e] = q.inside >> i & 1 ? share_of(s[i][e]) : 0.f;
   }
   auto initial = [&](int j, float (&v)[V]) {
 #pragma unroll
@@ -523,13 +549,13 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(5))) voi
     float x[V];
     Ln::get(as_new(rx[i]), x);
 #pragma unroll
-    for (int e = 0; e < V; ++e) { h[e] = step_of(b[i][e], x[e], h[e]); A[e] = fmaf(-b[i][e], A[e], A[e]); }
+    for (int e = 0; e < V; ++e) effect_of(s[i][e], x[e], h[e], A[e]);
   };
   auto back = [&](int i) {
     float d[V];
     Ln::get(as_new(rd[i]), d);
 #pragma unroll
-    for (int e = 0; e < V; ++e) { const float D = d[e] + g[e]; g[e] = fmaf(-b[i][e], D, D); }
+    for (int e = 0; e < V; ++e) g[e] = kept(s[i][e], d[e] + g[e]);
   };
   // (what lies before the last beginning has no effect on later states, what lies behind the first end none on earlier gradients)
   const int latest = 31 - __builtin_clz(q.begins | 1), earliest = __builtin_ctz(q.ends | 1u << (L - 1));
@@ -598,7 +624,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(5))) voi
     float x[V];
     Ln::get(as_new(rx[i]), x);
 #pragma unroll
-    for (int e = 0; e < V; ++e) { gap[i][e] = h[e] - x[e]; h[e] = fmaf(-b[i][e], gap[i][e], h[e]); }
+    for (int e = 0; e < V; ++e) { gap[i][e] = as_new(h[e] - x[e]); h[e] = fmaf(-s[i][e], gap[i][e], by_sign(s[i][e], h[e], x[e])); }
   };
   auto finish = [&](int i) {
     float d[V], dx[V], df[V];
@@ -606,10 +632,10 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(5))) voi
 #pragma unroll
     for (int e = 0; e < V; ++e) {
       const float D = d[e] + g[e];
-      dx[e] = b[i][e] * D;
-      const float own = as_new(b[i][e]);     // (as above: the product that follows)
-      df[e] = D * gap[i][e] * fmaf(-own, own, own);
-      g[e] = D - dx[e];
+      const float own = as_new(s[i][e]), rest = where_positive(own, D);     // (as above: the product that follows)
+      dx[e] = fmaf(own, D, D - rest);      // b D
+      df[e] = D * gap[i][e] * fmaf(-own, own, fabsf(own));
+      g[e] = fmaf(-own, D, rest);          // a D
     }
     if (!mine || !(q.inside >> i & 1)) return;
     const size_t t = as_new_scalar(t0 + i);

@@ -88,6 +88,63 @@ def scan_bounds(f, x, starts, h0=None, dh=None, dh_last=None):
     return out
 
 
+def scan_shares(f):
+    """(a, b), the shares of the old state and of the input: each by itself, so that the smaller one keeps all its bits"""
+    f = np.asarray(f, np.float64)
+    with np.errstate(over="ignore"):
+        return 1.0 / (1.0 + np.exp(-f)), 1.0 / (1.0 + np.exp(f))
+
+
+def scan_by_shares(f, x, starts, h0=None, dh=None, dh_last=None):
+    """(results, bounds), each a dict of h, h_last and, with dh, dgate, dx and dh0: the recurrence as h_t = a_t h_{t-1} + b_t x_t, and
+    what fp32 arithmetic may add where no bit is lost to cancellation.
+    M_t = a_t M_{t-1} + b_t |x_t| is what the terms of h_t amount to: it falls where a gate lets go of the state.  The smaller share is
+    off by d U of itself, d = 1.25 |f| + 8 (the exponential's argument and its constant, the exponential, the sum, the reciprocal and the
+    product), and by 2^-125 where the exponential has no more bits; the larger by less.  A step adds d U M_t, half a step of the difference of
+    input and state, which the smaller share weighs, of the result, and of the carried product: 4 U M_t.  Back it is the same with N, what the
+    terms of D amount to.  Twice the sum of it all, propagated like the state."""
+    a, b = scan_shares(f)
+    f, x = np.asarray(f, np.float64), np.asarray(x, np.float64)
+    n, c = len(starts) - 1, f.shape[1]
+    d = (1.25 * np.abs(f) + 8) * U
+    tiny = 2.0 ** -125
+    zero = lambda: np.zeros_like(x)
+    h, before, ebefore, mbefore, eh = zero(), zero(), zero(), zero(), zero()
+    last, elast = np.zeros((n, c)), np.zeros((n, c))
+    for j in range(n):
+        now = np.zeros(c) if h0 is None else np.asarray(h0[j], np.float64)
+        M, e = np.abs(now), np.zeros(c)
+        for t in range(starts[j], starts[j + 1]):
+            before[t], ebefore[t], mbefore[t] = now, e, M
+            most = M + np.abs(x[t])
+            now = a[t] * now + b[t] * x[t]
+            M = a[t] * M + b[t] * np.abs(x[t])
+            e = a[t] * e + (d[t] + 4 * U) * M + tiny * most
+            h[t], eh[t] = now, e
+        last[j], elast[j] = now, e
+    results, bounds = dict(h=h, h_last=last), dict(h=2 * eh, h_last=2 * elast)
+    if dh is None:
+        return results, bounds
+    dh = np.asarray(dh, np.float64)
+    D, N, eD = zero(), zero(), zero()
+    first, efirst = np.zeros((n, c)), np.zeros((n, c))
+    for j in range(n):
+        g = np.zeros(c) if dh_last is None else np.asarray(dh_last[j], np.float64)
+        G, e = np.abs(g), np.zeros(c)
+        for t in range(starts[j + 1] - 1, starts[j] - 1, -1):
+            D[t], N[t] = dh[t] + g, np.abs(dh[t]) + G
+            eD[t] = e + 2 * U * N[t]
+            g, G = a[t] * D[t], a[t] * N[t]
+            e = a[t] * eD[t] + (d[t] + 2 * U) * G + tiny * N[t]
+        first[j], efirst[j] = g, e
+    ab, gap = a * b, mbefore + np.abs(x)
+    results.update(dgate=D * (before - x) * ab, dx=D * b, dh0=first)
+    # a b is off by both, and by the roundings of a square and a difference; the gap by that of the state and its own
+    bounds.update(dx=2 * (b * eD + (d + 2 * U) * b * N + tiny * N), dh0=2 * efirst,
+                  dgate=2 * (ab * (gap * eD + N * (ebefore + U * gap) + N * gap * (2 * d + 5 * U)) + tiny * N * gap))
+    return results, bounds
+
+
 # ------------------------------------------------------------------------------------------ log probabilities
 def logprob_forward(z, tokens, scale, top=0):
     """dict of logprob, entropy, stats, top_id, top_logprob, and q, p"""

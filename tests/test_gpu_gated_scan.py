@@ -361,3 +361,52 @@ def test_nothing_where_nothing_is_needed(torch):
     e.backward(gate=None, x=None, marks=None, dh=None, dgate=None, dx=None)
     torch.cuda.synchronize()
     assert torch.equal(e.h_last, e.h0) and torch.equal(e.dh0, e.dh_last)
+
+
+def check_closely(p):
+    """Every output within the bounds that hold where no bit is lost to cancellation."""
+    h2 = lambda t: t.float().cpu().numpy().astype(np.float64)
+    p.torch.cuda.synchronize()
+    starts, n = F.starts_of(p.tokens, p.sequences, p.starts), F.starts_of(p.tokens, p.sequences, p.starts)[-1]
+    h0, dl = (None if t is None else h2(t) for t in (p.h0, p.dh_last))
+    want, bound = F.scan_by_shares(h2(p.gate), h2(p.x), starts, h0, h2(p.dh), dl)
+    for name in want:
+        rows = n if name in ("h", "dgate", "dx") else None
+        got, w, e = h2(getattr(p, name))[:rows], want[name][:rows], bound[name][:rows]
+        if p.bf16 and rows is not None:
+            e = e + BF16_HALF * (np.abs(w) + e) + 1e-38
+        far = np.abs(got - w) - e
+        assert (far <= 0).all(), (name, np.unravel_index(far.argmax(), far.shape), far.max())
+
+
+SHAPES = [(700, 2, None), (1600, 4, [0, 300, 300, 301, 1590]), (48, 48, None), (5, 1, None)]
+
+
+@pytest.mark.parametrize("bf16", [True, False])
+@pytest.mark.parametrize("bias", [-30.0, -16.0, -10.0, -3.0, 0.0, 6.0])
+@pytest.mark.parametrize("tokens,sequences,starts", SHAPES)
+def test_no_bits_are_lost_on_either_side_of_the_gate(torch, tokens, sequences, starts, bias, bf16):
+    p = Problem(torch, 30, tokens, 68, sequences, starts, bf16=bf16, bias=bias)
+    p.forward()
+    p.backward()
+    check_closely(p)
+
+
+@pytest.mark.parametrize("tokens,sequences,starts", SHAPES)
+def test_large_states_that_a_gate_lets_go_of(torch, tokens, sequences, starts):
+    """States of 1e8, and inputs of 3e4 on the way, that a gate of -30, -10 or minus infinity replaces by inputs of a thousandth."""
+    p = Problem(torch, 31, tokens, 68, sequences, starts, bf16=False, bias=1.0)
+    rng = np.random.default_rng(32)
+    p.h0.mul_(1e8)
+    p.x.mul_(1e-3)
+    at = torch.from_numpy(rng.integers(0, tokens, tokens // 8)).cuda()
+    p.x[at] = 3e4
+    for k, gate in enumerate((-30.0, -10.0, float("-inf"))):
+        p.gate[k::7] = gate
+    p.forward()
+    p.backward()
+    # (minus infinity: an exponential of nothing, the input itself)
+    p.gate.clamp_(min=-200.0)
+    check_closely(p)
+    if tokens == 48:
+        assert torch.equal(p.h[2::7], p.x[2::7])

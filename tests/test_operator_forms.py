@@ -41,6 +41,65 @@ def test_scan_closed_forms():
     assert np.allclose(h[:, 0], 3.0 * (1 - a ** np.arange(1, 201)), rtol=0, atol=1e-13)
 
 
+def scan_in_fp32(f, x, dh, h0, dh_last, by_sign):
+    """One sequence in fp32, step by step: the share b rounded by itself and 1 - b taken from it, or (by_sign) the smaller share of the two."""
+    w = np.float32
+    f, x, dh = (np.asarray(a, w) for a in (f, x, dh))
+    E = np.exp(-np.abs(f) if by_sign else f)
+    small = E / (w(1) + E)
+    neg = f < 0
+    b = w(1) / (w(1) + E)
+    h, states, g, out = np.asarray(h0, w), [], np.asarray(dh_last, w), dict(h=[], dgate=[], dx=[])
+    for t in range(len(f)):
+        states.append(h)
+        if by_sign:
+            h = np.where(neg[t], x[t] + small[t] * (h - x[t]), h + small[t] * (x[t] - h))
+        else:
+            h = h + b[t] * (x[t] - h)
+        out["h"].append(h)
+    last = h
+    for t in range(len(f) - 1, -1, -1):
+        D, gap = dh[t] + g, states[t] - x[t]
+        if by_sign:
+            s = small[t]
+            ab, dx, g = s - s * s, np.where(neg[t], D - s * D, s * D), np.where(neg[t], s * D, D - s * D)
+        else:
+            ab, dx = b[t] - b[t] * b[t], b[t] * D
+            g = D - dx
+        out["dgate"].insert(0, D * gap * ab)
+        out["dx"].insert(0, dx)
+    return {**{k: np.array(v) for k, v in out.items()}, "h_last": last[None], "dh0": g[None]}
+
+
+@pytest.mark.parametrize("bias", [-30.0, -16.0, -10.0, 0.0, 3.0, 12.0])
+def test_scan_bounds_tell_where_bits_are_lost(bias):
+    """fp32 arithmetic with the smaller of the two shares stays within the bounds whatever the gates; with one minus the other share it does
+    not where gates are clearly negative."""
+    rng = np.random.default_rng(int(bias) + 100)
+    f, x, dh = (rng.standard_normal((400, 6)).astype(np.float32) for _ in range(3))
+    f += np.float32(bias)
+    h0, dl = (rng.standard_normal((1, 6)).astype(np.float32) for _ in range(2))
+    h0[0, :3] *= 1e8
+    want, bound = F.scan_by_shares(f, x, [0, 400], h0, dh, dl)
+    far = lambda got: {k: float((np.abs(got[k].astype(np.float64) - want[k]) / (bound[k] + 1e-300)).max()) for k in want}
+    assert max(far(scan_in_fp32(f, x, dh, h0[0], dl[0], True)).values()) <= 1
+    by_b = far(scan_in_fp32(f, x, dh, h0[0], dl[0], False))
+    if bias <= -10:
+        assert by_b["dgate"] > 10 and by_b["dh0"] > 10 and by_b["h"] > 10
+
+
+def test_scan_by_shares_is_the_scan():
+    rng = np.random.default_rng(4)
+    starts = [0, 3, 3, 9]
+    f, x, dh = (rng.standard_normal((9, 2)) for _ in range(3))
+    h0, dl = rng.standard_normal((3, 2)), rng.standard_normal((3, 2))
+    got, _ = F.scan_by_shares(f, x, starts, h0, dh, dl)
+    h, _, last = F.scan_forward(f, x, starts, h0)
+    dgate, dx, dh0, _ = F.scan_backward(f, x, starts, dh, h0, dl)
+    for k, want in dict(h=h, h_last=last, dgate=dgate, dx=dx, dh0=dh0).items():
+        assert np.abs(got[k] - want).max() < 1e-14, k
+
+
 def test_logprob_gradients_against_differences():
     rng = np.random.default_rng(2)
     z, tokens = rng.standard_normal((4, 7)), np.array([3, -1, 0, 6])
