@@ -158,114 +158,115 @@ __device__ __forceinline__ Part part_of(const Spans& p, int t0, unsigned long lo
 
 // ---- the chain of workgroups ------------------------------------------------------------------------------------
 // A chunk of KARMA_SCAN_MARK tokens and some channels belongs to a workgroup.  What it does to the state that comes in is
-// out = A in + H; it publishes both at once (8 bytes a channel; A below 0: out = H, a sequence began in it) and waits for the state
-// behind the chunk before it, which one wavefront per block of channels carries through all chunks in their order: the same sums in
-// the same order every time, without a trip to memory between one chunk and the next.  Workgroups take their work by counters, the
-// carriers first, so whoever is waited for is already running.  A word of all ones is not there yet.  A wait that never ends (a
-// workspace that another call is using) is given up, and the states become NaN.
-// 65536 tokens of 2048 channels: 175 us a call, of which 6 to clear the words; 171 in the kernel if nobody waited (what a copy of the same
-// bytes takes is 169); chunks of 128 tokens 225 in the kernel, of 64 373 (a chunk costs the chain 0.35 us), of 512 378 (one workgroup
-// on a compute unit: nothing hides its waits).
+// out = A in + H; it publishes both at once (8 bytes a channel; A below 0: out = H, a sequence began in it).  Chunks in their order of
+// work are in groups of as many as a workgroup has wavefronts: a workgroup looks at all effects of its group before its own at once, a
+// wavefront at each, and at the state that the group begins with, which the group before's last workgroup publishes, and runs through
+// them in their order: the same sums in the same order every time, and a trip to memory a group, not a chunk.
+// Workgroups take their chunks by counters, in the order of work, and wait only for what comes before theirs: for workgroups that have
+// begun, whose effects wait for nobody and whose states wait for earlier ones.  So every wait ends, whatever else is on the device and
+// however many workgroups find room at once.  A word of all ones is not there yet.  Where a word does not come for a second or so (a
+// workspace that another call is using), the states become NaN.
 struct Chain {
   unsigned* tickets;            // one for every block of channels, CHAIN_APART numbers from one to the next
-  unsigned long long* effect;   // [chunk][channel]
-  unsigned* state;              // behind the chunk
+  unsigned long long* effect;   // [place in the order of work][block of channels][channel of a lane][lane]
+  unsigned* state;              // [group][as above]; the first group begins with zeros
   int chunks, blocks, width;    // blocks of channels, channels of all blocks; chunks == 1: no chain
 };
 constexpr int CHAIN_APART = 32;         // 128 bytes: counters of their own cache lines
 constexpr int CHAIN_LIMIT = 1 << 20;    // looks at a word, a microsecond or so each
+constexpr int CHAIN_GROUP = 8;          // chunks of the smallest groups
 
-__device__ __forceinline__ unsigned long long effect_word(float A, float H, bool cut) {
-  const unsigned long long w = (unsigned long long)__float_as_uint(H) << 32 | __float_as_uint(cut ? -1.f : A);
-  return w == ~0ull ? 0x7fc000007fc00000ull : w;
-}
 template <int V>
-__device__ __forceinline__ void publish(const Chain& c, int chunk, int channel, const float (&A)[V], const float (&H)[V], bool cut) {
+__device__ __forceinline__ void publish(const Chain& c, int place, int first, const float (&A)[V], const float (&H)[V], bool cut) {
 #pragma unroll
-  for (int e = 0; e < V; ++e)
-    __hip_atomic_store(c.effect + (size_t)chunk * c.width + channel + e, effect_word(A[e], H[e], cut), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  for (int e = 0; e < V; ++e) {
+    const unsigned long long w = (unsigned long long)__float_as_uint(H[e]) << 32 | __float_as_uint(cut ? -1.f : A[e]);
+    __hip_atomic_store(c.effect + (size_t)place * c.width + first + e * 64, w == ~0ull ? 0x7fc000007fc00000ull : w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
 }
-template <int V>
-__device__ __forceinline__ void await(const Chain& c, int chunk, int channel, float (&in)[V]) {
-  unsigned w[V];
+// V words from `at` on, 64 apart; those that did not come are all ones, a NaN
+template <int V, typename W>
+__device__ __forceinline__ void await(const W* at, W (&w)[V]) {
   for (int n = 0; n < CHAIN_LIMIT; ++n) {
     bool missing = false;
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-      w[e] = __hip_atomic_load(c.state + (size_t)chunk * c.width + channel + e, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      missing |= w[e] == ~0u;
+      w[e] = __hip_atomic_load(at + e * 64, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      missing |= w[e] == (W)~(W)0;
     }
     if (!__ballot(missing)) break;
     __builtin_amdgcn_s_sleep(1);
   }
-#pragma unroll
-  for (int e = 0; e < V; ++e) in[e] = __uint_as_float(w[e]);    // all ones are a NaN
 }
-// from chunk 0 up, or from the last one down
-template <int V>
-__device__ __forceinline__ void carry(const Chain& c, int channel, bool up) {
-  constexpr int AHEAD = 8;
-  float s[V] = {};
-  int n = 0;
-  for (int done = 0; done < c.chunks - 1;) {
-    unsigned long long w[AHEAD][V];
+// what comes before a chunk in its group, in LDS
+template <int V, int W>
+struct Before {
+  float A[W - 1][64 * V], H[W - 1][64 * V], state[64 * V];
+};
+// Wavefront w's part of it.
+template <int V, int W>
+__device__ __forceinline__ void look_back(const Chain& c, int place, int first, int w, Before<V, W>& b) {
+  const int lane = threadIdx.x & 63, group = place / W;
+  if (w < place % W) {
+    unsigned long long word[V];
+    await<V>(c.effect + (size_t)(group * W + w) * c.width + first, word);
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) {
-      const int k = min(done + i, c.chunks - 1);
-#pragma unroll
-      for (int e = 0; e < V; ++e)
-        w[i][e] = __hip_atomic_load(c.effect + (size_t)(up ? k : c.chunks - 1 - k) * c.width + channel + e, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    for (int e = 0; e < V; ++e) {
+      b.A[w][e * 64 + lane] = __uint_as_float((unsigned)word[e]);
+      b.H[w][e * 64 + lane] = __uint_as_float((unsigned)(word[e] >> 32));
     }
-    if (++n > CHAIN_LIMIT) return;
-    const int before = done;
+  } else if (w == W - 1) {
+    unsigned word[V] = {};
+    if (group) await<V>(c.state + (size_t)group * c.width + first, word);
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) {
-      bool missing = false;
-#pragma unroll
-      for (int e = 0; e < V; ++e) missing |= w[i][e] == ~0ull;
-      if (done != before + i || done >= c.chunks - 1 || __ballot(missing)) continue;
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        const float A = __uint_as_float((unsigned)w[i][e]), H = __uint_as_float((unsigned)(w[i][e] >> 32));
-        s[e] = A < 0.f ? H : fmaf(A, s[e], H);
-        const unsigned u = __float_as_uint(s[e]);
-        __hip_atomic_store(c.state + (size_t)(up ? done : c.chunks - 1 - done) * c.width + channel + e, u == ~0u ? 0x7fc00000u : u, __ATOMIC_RELAXED,
-                           __HIP_MEMORY_SCOPE_AGENT);
-      }
-      ++done;
-    }
-    if (done != before) n = 0;
+    for (int e = 0; e < V; ++e) b.state[e * 64 + lane] = __uint_as_float(word[e]);
   }
 }
-// all words behind the counters, 12 bytes a chunk and channel, widths being multiples of 128
+// The state that comes in, when all wavefronts have looked.
+template <int V, int W>
+__device__ __forceinline__ void run_through(int place, const Before<V, W>& b, float (&in)[V]) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int e = 0; e < V; ++e) in[e] = b.state[e * 64 + lane];
+  for (int k = 0; k < place % W; ++k)
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      const float A = b.A[k][e * 64 + lane], H = b.H[k][e * 64 + lane];
+      in[e] = A < 0.f ? H : fmaf(A, in[e], H);
+    }
+}
+// The last workgroup of a group: the state that the next group begins with.
+template <int V, int W>
+__device__ __forceinline__ void hand_on(const Chain& c, int place, int first, const float (&out)[V]) {
+  if (place % W != W - 1 || place + 1 >= c.chunks) return;
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+    const unsigned u = __float_as_uint(out[e]);
+    __hip_atomic_store(c.state + (size_t)(place / W + 1) * c.width + first + e * 64, u == ~0u ? 0x7fc00000u : u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+}
+// all words behind the counters, widths being multiples of 128
 __global__ __launch_bounds__(256) void chain_clear_kernel(Chain c, size_t pieces) {
   const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
   if (i < (size_t)c.blocks) c.tickets[i * CHAIN_APART] = 0;
   if (i < pieces) ((u32x4*)c.effect)[i] = u32x4{~0u, ~0u, ~0u, ~0u};
 }
 
-// The work of this workgroup: a chunk and a block of channels, or false for a carrier, which has then done its work.  Forward, each block of
+// The work of this workgroup: a block of channels, and a chunk by its place in the order of work; false: none.  Forward, each block of
 // channels has a counter: 512 workgroups that begin at once wait up to 6 us for one (packed prompts 53 us in the kernel instead of
 // 57, 65536 x 2048 180 instead of 187).  Backward they share one: its workgroups gain by not loading all at the same time (86 us, 91 with
-// counters of their own).  Carriers of eight blocks in one workgroup look slower than they save places: 64 us instead of 53.
-template <int V>
-__device__ __forceinline__ bool take_work(const Chain& c, bool up, int& chunk, int& block) {
+// counters of their own).
+__device__ __forceinline__ bool take_work(const Chain& c, bool up, int& place, int& block) {
   __shared__ unsigned ticket;
   const unsigned own = blockIdx.x % c.blocks, first = up ? own : 0, sharing = up ? 1 : c.blocks;    // blocks that share the counter
-  chunk = 0;
+  place = 0;
   block = own;
   if (c.chunks == 1) return true;
   if (threadIdx.x == 0) ticket = atomicAdd(c.tickets + (size_t)first * CHAIN_APART, 1u);
   __syncthreads();
-  unsigned unit = __builtin_amdgcn_readfirstlane((int)ticket);
-  if (unit < sharing) {
-    if (threadIdx.x < 64) carry<V>(c, (first + unit) * 64 * V + threadIdx.x * V, up);
-    return false;
-  }
-  unit -= sharing;
+  const unsigned unit = __builtin_amdgcn_readfirstlane((int)ticket);
   if (unit >= sharing * c.chunks) return false;     // (the counter is another call's too)
-  chunk = unit / sharing;
-  if (!up) chunk = c.chunks - 1 - chunk;
+  place = unit / sharing;
   block = first + unit % sharing;
   return true;
 }
@@ -279,13 +280,13 @@ __device__ __forceinline__ bool take_work(const Chain& c, bool up, int& chunk, i
 template <typename T, int V, int L, int W>
 __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(4))) void scan_fwd_kernel(ScanFwd a, Spans p, Chain chain) {
   typedef Lane<T, V> Ln;
-  static_assert(L * W == KARMA_SCAN_MARK, "a chunk is what lies between two marks");
+  static_assert(L * W == KARMA_SCAN_MARK && W >= CHAIN_GROUP, "a chunk is what lies between two marks; room for the groups' states");
   __shared__ float effects[W][2][64 * V];
-  __shared__ float incoming[64 * V];
+  __shared__ Before<V, W> before;
   __shared__ unsigned long long words[W];
-  __shared__ int cuts[W];
+  __shared__ int cuts[W];       // 1: a sequence begins in the part, 2: with its first token
   int chunk, block;
-  if (!take_work<V>(chain, true, chunk, block)) return;
+  if (!take_work(chain, true, chunk, block)) return;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), C = (int)a.s.channels;
   const int channel = block * 64 * V + lane * V, c = channel < C ? channel : C - V;     // (lanes without a channel repeat the last one)
   const bool mine = channel < C;
@@ -341,7 +342,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(4))) voi
   }
 #pragma unroll
   for (int e = 0; e < V; ++e) { effects[w][0][lane * V + e] = A[e]; effects[w][1][lane * V + e] = h[e]; }
-  if (lane == 0) cuts[w] = q.begins != 0;
+  if (lane == 0) cuts[w] = (q.begins ? 1 : 0) | (q.begins & 1 ? 2 : 0);
   __syncthreads();
   // what the wavefronts before this one do together; the first wavefront has the whole chunk's
   float PA[V], PH[V];
@@ -349,7 +350,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(4))) voi
 #pragma unroll
   for (int e = 0; e < V; ++e) { PA[e] = 1.f; PH[e] = 0.f; }
   for (int k = 0; k < (w == 0 ? W : w); ++k) {
-    const bool fresh = cuts[k];
+    const bool fresh = cuts[k] & 1;
     cut |= fresh;
 #pragma unroll
     for (int e = 0; e < V; ++e) {
@@ -358,19 +359,21 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(4))) voi
       PA[e] *= Ak;
     }
   }
-  const bool wants = chain.chunks > 1 && chunk > 0;
-  if (w == 0 && chain.chunks > 1) {
-    float in[V] = {};
-    publish<V>(chain, chunk, channel, PA, PH, cut);
-    if (wants && !(q.begins & 1)) await<V>(chain, chunk - 1, channel, in);
-#pragma unroll
-    for (int e = 0; e < V; ++e) incoming[lane * V + e] = in[e];
+  float in[V] = {};
+  const int words_at = block * 64 * V + lane;
+  if (chain.chunks > 1) {
+    const bool wants = !(cuts[0] & 2);
+    if (w == 0) publish<V>(chain, chunk, words_at, PA, PH, cut);
+    if (wants) look_back<V, W>(chain, chunk, words_at, w, before);
+    __syncthreads();
+    if (wants) run_through<V, W>(chunk, before, in);
   }
-  if (chain.chunks > 1) __syncthreads();
 #pragma unroll
-  for (int e = 0; e < V; ++e) {
-    const float in = chain.chunks > 1 ? incoming[lane * V + e] : 0.f;
-    h[e] = w == 0 ? in : cut ? PH[e] : fmaf(PA[e], in, PH[e]);
+  for (int e = 0; e < V; ++e) h[e] = cut ? PH[e] : fmaf(PA[e], in[e], PH[e]);
+  if (w == 0) {
+    if (chain.chunks > 1) hand_on<V, W>(chain, chunk, words_at, h);
+#pragma unroll
+    for (int e = 0; e < V; ++e) h[e] = in[e];
   }
   if (w == 0 && a.marks && mine) {
 #pragma unroll
@@ -504,13 +507,15 @@ __global__ __launch_bounds__(256) void scan_fwd_short_kernel(ScanFwd a, Spans p,
 template <typename T, int V, int L, int W, bool STATES>
 __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(5))) void scan_bwd_kernel(ScanBwd a, Spans p, Chain chain) {
   typedef Lane<T, V> Ln;
-  static_assert(L * W == KARMA_SCAN_MARK, "a chunk is what lies between two marks");
+  static_assert(L * W == KARMA_SCAN_MARK && W >= CHAIN_GROUP, "a chunk is what lies between two marks; room for the groups' states");
   __shared__ float effects[W][3][64 * V];
-  __shared__ float incoming[64 * V], marks[64 * V];
+  __shared__ Before<V, W> before;
+  __shared__ float marks[64 * V];
   __shared__ unsigned long long words[W];
-  __shared__ int cuts[W];       // 1: a sequence begins in the part, 2: one ends in it
-  int chunk, block;
-  if (!take_work<V>(chain, false, chunk, block)) return;
+  __shared__ int cuts[W];       // 1: a sequence begins in the part, 2: one ends in it, 4: with its last token
+  int place, block;
+  if (!take_work(chain, false, place, block)) return;
+  const int chunk = chain.chunks - 1 - place;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), C = (int)a.s.channels;
   const int channel = block * 64 * V + lane * V, c = channel < C ? channel : C - V;
   const bool mine = channel < C;
@@ -579,7 +584,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(5))) voi
     effects[w][1][lane * V + e] = h[e];
     effects[w][2][lane * V + e] = g[e];
   }
-  if (lane == 0) cuts[w] = (q.begins ? 1 : 0) | (q.ends ? 2 : 0);
+  if (lane == 0) cuts[w] = (q.begins ? 1 : 0) | (q.ends ? 2 : 0) | (q.ends >> (L - 1) & 1 ? 4 : 0);
   __syncthreads();
 #pragma unroll
   for (int e = 0; e < V; ++e) h[e] = marks[lane * V + e];
@@ -606,18 +611,21 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(5))) voi
       PA[e] *= Ak;
     }
   }
-  if (w == W - 1 && chain.chunks > 1) {
-    float in[V] = {};
-    publish<V>(chain, chunk, channel, PA, PR, cut);
-    if (chunk < chain.chunks - 1 && !(q.ends >> (L - 1) & 1)) await<V>(chain, chunk + 1, channel, in);
-#pragma unroll
-    for (int e = 0; e < V; ++e) incoming[lane * V + e] = in[e];
+  float in[V] = {};
+  const int words_at = block * 64 * V + lane;
+  if (chain.chunks > 1) {
+    const bool wants = !(cuts[W - 1] & 4);
+    if (w == W - 1) publish<V>(chain, place, words_at, PA, PR, cut);
+    if (wants) look_back<V, W>(chain, place, words_at, w, before);
+    __syncthreads();
+    if (wants) run_through<V, W>(place, before, in);
   }
-  if (chain.chunks > 1) __syncthreads();
 #pragma unroll
-  for (int e = 0; e < V; ++e) {
-    const float in = chain.chunks > 1 ? incoming[lane * V + e] : 0.f;
-    g[e] = w == W - 1 ? in : cut ? PR[e] : fmaf(PA[e], in, PR[e]);
+  for (int e = 0; e < V; ++e) g[e] = cut ? PR[e] : fmaf(PA[e], in[e], PR[e]);
+  if (w == W - 1) {
+    if (chain.chunks > 1) hand_on<V, W>(chain, place, words_at, g);
+#pragma unroll
+    for (int e = 0; e < V; ++e) g[e] = in[e];
   }
   float gap[L][V];      // h_{t-1} - x_t
   auto part_from = [&](int i) {
@@ -713,13 +721,15 @@ bool aligned_to(const void* p, size_t n) { return (uintptr_t)p % n == 0; }
 
 // the counters of blocks of 64 channels, which are the more
 static size_t chain_head(uint64_t width) { return width / 64 * CHAIN_APART * sizeof(unsigned); }
+// effects, and states of the smallest groups
+static size_t chain_words(uint64_t chunks, uint64_t width) { return (chunks * 8 + (chunks + CHAIN_GROUP - 1) / CHAIN_GROUP * 4) * width; }
 
 size_t gated_scan_ws_bytes(const karma_scan_shape& given) {
   karma_scan_shape shape = given;
   const int any = 0;      // (whether all sequences have one length does not matter here)
   if (check_scan(shape, &any)) return 0;
   const uint64_t chunks = scan_chunks(shape.tokens), width = scan_width(shape.channels);
-  return chunks > 1 ? chain_head(width) + chunks * width * 12 : 0;
+  return chunks > 1 ? chain_head(width) + chain_words(chunks, width) : 0;
 }
 
 static Spans spans_of(const karma_scan_shape& s, const int* starts) {
@@ -730,11 +740,11 @@ static Chain chain_of(const karma_scan_shape& s, int V, void* ws, hipStream_t st
   const uint64_t chunks = scan_chunks(s.tokens), width = scan_width(s.channels);
   unsigned long long* effect = (unsigned long long*)((char*)ws + chain_head(width));
   const Chain c{(unsigned*)ws, effect, (unsigned*)(effect + chunks * width), (int)chunks, (int)((s.channels + 64 * V - 1) / (64 * V)), (int)width};
-  const size_t pieces = chunks * width * 12 / 16;
+  const size_t pieces = chain_words(chunks, width) / 16;
   if (chunks > 1) hipLaunchKernelGGL(chain_clear_kernel, dim3((unsigned)((pieces + 255) / 256)), dim3(256), 0, stream, c, pieces);
   return c;
 }
-static unsigned chain_grid(const Chain& c) { return (unsigned)c.blocks * (unsigned)(c.chunks > 1 ? c.chunks + 1 : 1); }
+static unsigned chain_grid(const Chain& c) { return (unsigned)c.blocks * (unsigned)c.chunks; }
 
 int gated_scan_fwd(ScanFwd a, bool bf16, hipStream_t s) {
   const size_t e = bf16 ? 2 : 4;

@@ -410,3 +410,79 @@ def test_large_states_that_a_gate_lets_go_of(torch, tokens, sequences, starts):
     check_closely(p)
     if tokens == 48:
         assert torch.equal(p.h[2::7], p.x[2::7])
+
+
+@pytest.mark.parametrize("starts", [None, [0, 100, 357]])
+@pytest.mark.parametrize("bf16", [True, False])
+def test_more_blocks_of_channels_than_workgroups_that_run_at_once(torch, bf16, starts):
+    """300 000 channels of some chunks: workgroups of all blocks can never be there together.  The same bits as calls on a part of the
+    channels, and within bounds."""
+    tokens, channels = 600, 300_032
+    t = torch.bfloat16 if bf16 else torch.float32
+    gen = torch.Generator(device="cuda").manual_seed(40)
+    make = lambda rows=tokens, dtype=t, mean=0.0: torch.empty((rows, channels), device="cuda", dtype=dtype).normal_(mean, 1.0, generator=gen)
+    S = 1 if starts is None else len(starts) - 1
+    gate, x, dh, h0, dh_last = make(mean=3.0), make(), make(), make(S, torch.float32), make(S, torch.float32)
+    st = torch.tensor(starts, dtype=torch.int32, device="cuda") if starts else None
+    n = starts[-1] if starts else tokens
+    fwd, bwd = ((K.lib().karma_k_gated_scan_fwd_bf16, K.lib().karma_k_gated_scan_bwd_bf16) if bf16 else
+                (K.lib().karma_k_gated_scan_fwd_f32, K.lib().karma_k_gated_scan_bwd_f32))
+    q = C.c_void_p(torch.cuda.current_stream().cuda_stream)
+
+    def call(first, count):
+        cut = lambda a: a[:, first:first + count]
+        a, b, d, s, l = cut(gate), cut(x), cut(dh), cut(h0).contiguous(), cut(dh_last).contiguous()
+        out = lambda rows=tokens, dtype=t: torch.zeros((rows, count), device="cuda", dtype=dtype)
+        h, dgate, dx, last, first_g, marks = out(), out(), out(), out(S, torch.float32), out(S, torch.float32), out(3, torch.float32)
+        shape = K.ScanShape(tokens=tokens, channels=count, sequences=S, ld_gate=channels, ld_x=channels, ld_h=count)
+        ws = torch.empty(K.gated_scan_ws_bytes(shape), dtype=torch.uint8, device="cuda")
+        assert fwd(ptr(a), ptr(b), ptr(s), ptr(st), ptr(h), ptr(last), ptr(marks), C.byref(shape), ptr(ws), C.c_uint64(ws.numel()), q) == K.OK
+        if count < channels:
+            d = d.contiguous()
+        assert bwd(ptr(a), ptr(b), ptr(s), ptr(st), ptr(marks), ptr(d), ptr(l), ptr(dgate), ptr(dx), ptr(first_g), C.byref(shape), ptr(ws),
+                   C.c_uint64(ws.numel()), q) == K.OK
+        torch.cuda.synchronize()
+        return dict(h=h, dgate=dgate, dx=dx, h_last=last, dh0=first_g)
+
+    whole = call(0, channels)
+    for first in (0, 131_072, channels - 2048):
+        part = call(first, 2048)
+        for k in part:
+            assert torch.equal(whole[k][:, first:first + 2048], part[k]), (k, first)
+    some = torch.arange(7, channels, channels // 40, device="cuda")
+    h2 = lambda a: a[:, some].float().cpu().numpy().astype(np.float64)
+    want, bound = F.scan_by_shares(h2(gate), h2(x), F.starts_of(tokens, S, starts), h2(h0), h2(dh), h2(dh_last))
+    for k in want:
+        rows = n if k in ("h", "dgate", "dx") else None
+        got, w, e = h2(whole[k])[:rows], want[k][:rows], bound[k][:rows]
+        if bf16 and rows:
+            e = e + BF16_HALF * (np.abs(w) + e) + 1e-38
+        assert (np.abs(got - w) <= e).all(), k
+
+
+@pytest.mark.parametrize("bf16,tokens,channels,sequences", [(True, 256 * 100 + 3, 260, 1), (False, 256 * 17, 130, 2), (True, 256 * 9, 64, 1), (True, 256 * 8 + 1, 64, 1),
+                                                            (True, 256 * 16 + 1, 64, 1), (True, 256 * 33, 65, 3)])
+def test_groups_of_chunks(torch, bf16, tokens, channels, sequences):
+    """Chunks that fill their groups, end one, and begin the next."""
+    p = Problem(torch, 41, tokens, channels, sequences, bf16=bf16, bias=7.0)     # states live for a thousand tokens
+    p.forward()
+    p.backward()
+    check_closely(p)
+
+
+def test_beside_work_that_fills_the_device(torch):
+    p = Problem(torch, 42, 20000, 512, 1, bias=6.0)
+    both(p)
+    want = [t.clone() for t in (p.h, p.dgate, p.dx, p.h_last, p.dh0)]
+    a = torch.randn(8192, 8192, device="cuda", dtype=torch.bfloat16)
+    side, other = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(5):
+        with torch.cuda.stream(side):
+            for _ in range(4):
+                b = a @ a
+        p.forward(stream=other)
+        p.backward(stream=other)
+    torch.cuda.synchronize()
+    assert torch.isfinite(b).all()
+    assert all(torch.equal(t, w) for t, w in zip((p.h, p.dgate, p.dx, p.h_last, p.dh0), want))
