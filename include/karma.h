@@ -603,7 +603,10 @@ int karma_k_attention_bwd_bf16(const void* qkv_dev, const void* ctx_dev, const v
  * that the backward pass needs beside gate and x (undefined where that row starts a sequence or belongs to none).
  * h_dev may be gate_dev or x_dev where the strides are equal; no other overlap.
  * ws_dev: karma_k_gated_scan_ws_bytes(shape) bytes (0 for a wrong shape), 16-byte aligned, for one call at a time: calls that may run at the same
- * time (graphs replayed on two streams among them) need a workspace each.  The call clears what it needs cleared.
+ * time (graphs replayed on two streams among them) need a workspace each.  The call clears what it needs cleared.  Where another call uses the
+ * workspace at the same time, results are wrong: wherever a word of it does not come for some 2^20 looks, a second or so, states and
+ * gradients become NaN, after the call has returned KARMA_OK.  A call that has its workspace to itself waits for as long as it takes
+ * its own earlier workgroups, whatever else is on the device.
  * Errors: KARMA_E_INVAL, KARMA_E_OOM (ws_bytes too small). */
 #define KARMA_SCAN_MARK 256u
 typedef struct {
