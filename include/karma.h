@@ -607,7 +607,7 @@ int karma_k_attention_bwd_bf16(const void* qkv_dev, const void* ctx_dev, const v
  * workspace at the same time, results are wrong: wherever a word of it does not come for some 2^20 looks, a second or so, states and
  * gradients become NaN, after the call has returned KARMA_OK.  A call that has its workspace to itself waits for as long as it takes
  * its own earlier workgroups, whatever else is on the device.
- * Errors: KARMA_E_INVAL, KARMA_E_OOM (ws_bytes too small). */
+ * Errors: KARMA_E_INVAL (operands off their elements' boundaries among them), KARMA_E_OOM (ws_bytes too small). */
 #define KARMA_SCAN_MARK 256u
 typedef struct {
   uint64_t tokens;              /* rows of the tensors, < 2^31 - 1024 */
@@ -644,7 +644,8 @@ int karma_k_gated_scan_bwd_f32(const float* gate_dev, const float* x_dev, const 
  * A logit of -inf is not allowed: its probability is 0.  A row of nothing else has q = -inf, entropy 0 and gradient 0.  +inf
  * or NaN in a row makes its results NaN (NaN is no alternative; where too few are left the index is -1).
  * ws_dev: karma_k_token_logprob_ws_bytes(rows, cols, top) bytes, 16-byte aligned, for one call at a time (0 bytes: may be NULL).
- * rows < 2^24, and rows x (cols / 1024, rounded up) <= 2^26 - 4 in the backward pass.  Errors: KARMA_E_INVAL, KARMA_E_OOM. */
+ * rows < 2^24, and rows x (cols / 1024, rounded up) <= 2^26 - 4 in the backward pass.  Errors: KARMA_E_INVAL (operands off their
+ * elements' boundaries among them), KARMA_E_OOM. */
 #define KARMA_TOP_MAX 64u
 uint64_t karma_k_token_logprob_ws_bytes(uint32_t rows, uint32_t cols, uint32_t top);
 int karma_k_token_logprob_fwd_bf16(const void* logits_dev, uint64_t ld, const int32_t* tokens_dev, float* logprob_dev, float* entropy_dev,

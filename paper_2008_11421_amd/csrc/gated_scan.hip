@@ -751,6 +751,7 @@ int gated_scan_fwd(ScanFwd a, bool bf16, hipStream_t s) {
   if (int st = check_scan(a.s, a.starts)) return st;
   if (a.s.tokens && (!a.gate || !a.x || !a.h)) return KARMA_E_INVAL;
   if (!aligned_to(a.gate, e) || !aligned_to(a.x, e) || !aligned_to(a.h, e) || !aligned_to(a.ws, 16)) return KARMA_E_INVAL;
+  if (!aligned_to(a.h0, 4) || !aligned_to(a.starts, 4) || !aligned_to(a.h_last, 4) || !aligned_to(a.marks, 4)) return KARMA_E_INVAL;
   if (a.ws_bytes < gated_scan_ws_bytes(a.s)) return KARMA_E_OOM;
   const bool pairs = bf16 && a.s.channels % 2 == 0 && (a.s.ld_gate | a.s.ld_x | a.s.ld_h) % 2 == 0 && aligned_to(a.gate, 4) && aligned_to(a.x, 4) &&
                      aligned_to(a.h, 4);
@@ -777,6 +778,7 @@ int gated_scan_bwd(ScanBwd a, bool bf16, hipStream_t s) {
   if (a.s.tokens && (!a.gate || !a.x || !a.marks || !a.dh || !a.dgate || !a.dx)) return KARMA_E_INVAL;
   if (!aligned_to(a.gate, e) || !aligned_to(a.x, e) || !aligned_to(a.dh, e) || !aligned_to(a.dgate, e) || !aligned_to(a.dx, e) ||
       !aligned_to(a.ws, 16)) return KARMA_E_INVAL;
+  if (!aligned_to(a.h0, 4) || !aligned_to(a.starts, 4) || !aligned_to(a.marks, 4) || !aligned_to(a.dh_last, 4) || !aligned_to(a.dh0, 4)) return KARMA_E_INVAL;
   if (a.ws_bytes < gated_scan_ws_bytes(a.s)) return KARMA_E_OOM;
   if (!a.s.tokens) {      // the gradient of a state that no token changed
     if (!a.dh0) return KARMA_OK;

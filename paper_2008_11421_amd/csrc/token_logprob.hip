@@ -570,6 +570,8 @@ int token_logprob_fwd(LogprobFwd a, bool bf16, hipStream_t s) {
   if (!good_rows(a.rows, a.cols, a.ld) || !(a.scale >= 1e-20f && a.scale <= 1e20f)) return KARMA_E_INVAL;
   if (a.top > KARMA_TOP_MAX || a.top > a.cols || (a.top && (!a.top_logprob || !a.top_id))) return KARMA_E_INVAL;
   if ((a.logprob && !a.tokens) || (!a.logprob && !a.entropy && !a.stats && !a.top)) return KARMA_E_INVAL;
+  for (const void* p : {(const void*)a.tokens, (const void*)a.logprob, (const void*)a.entropy, (const void*)a.stats, (const void*)a.top_logprob, (const void*)a.top_id})
+    if (!aligned_to(p, 4)) return KARMA_E_INVAL;
   if (!a.rows) return KARMA_OK;
   if (!a.logits || !aligned_to(a.logits, bf16 ? 2 : 4)) return KARMA_E_INVAL;
   if (a.ws_bytes < token_logprob_ws_bytes(a.rows, a.cols, a.top)) return KARMA_E_OOM;
@@ -597,6 +599,8 @@ int token_logprob_bwd(LogprobBwd a, bool bf16, hipStream_t s) {
   if (!a.ld_d) a.ld_d = a.cols;
   if (!good_rows(a.rows, a.cols, a.ld) || !good_rows(a.rows, a.cols, a.ld_d) || !(a.scale >= 1e-20f && a.scale <= 1e20f)) return KARMA_E_INVAL;
   if ((a.dlogprob && !a.tokens) || (a.dentropy && !a.entropy) || (!a.dlogprob && !a.dentropy)) return KARMA_E_INVAL;
+  for (const void* p : {(const void*)a.tokens, (const void*)a.stats, (const void*)a.entropy, (const void*)a.dlogprob, (const void*)a.dentropy})
+    if (!aligned_to(p, 4)) return KARMA_E_INVAL;
   if (!a.rows) return KARMA_OK;
   if (!a.logits || !a.stats || !a.dlogits || !aligned_to(a.logits, bf16 ? 2 : 4) || !aligned_to(a.dlogits, bf16 ? 2 : 4)) return KARMA_E_INVAL;
   const unsigned vectors = a.cols / (bf16 ? 8 : 4), units = std::max(1u, (vectors + 64 * LP_BATCH - 1) / (64 * LP_BATCH));

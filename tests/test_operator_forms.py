@@ -234,3 +234,30 @@ def test_sizes_beyond_a_launch_are_refused():
     step = K.AdamwStep(lr=1e-3, beta1=0.9, beta2=0.95, eps=1e-8, grad_scale=1.0, seed=1, step=1)
     t = (K.AdamwTensor * 1)(K.AdamwTensor(w=4096, m=4096, v=4096, grad=4096, n=1 << 34, flags=0))
     assert K.lib().karma_k_adamw(t, 1, C.byref(step), None, None) == K.E_INVAL
+
+
+@pytest.mark.parametrize("odd", [1, 2, 3])
+def test_operands_of_32_bits_off_their_boundaries_are_refused(odd):
+    """The starts and states of a scan, the tokens, statistics and results of log probabilities: a scalar load drops an address's lowest bits."""
+    Q = C.c_void_p(4096 + odd)
+    lib, shape = K.lib(), K.ScanShape(tokens=512, channels=8, sequences=2)
+    big = C.c_uint64(1 << 40)
+    for f in ("bf16", "f32"):
+        for which in range(4):
+            o = [None] * 4
+            o[which] = Q
+            h0, starts, h_last, marks = o
+            assert getattr(lib, "karma_k_gated_scan_fwd_" + f)(P, P, h0, starts, P, h_last, marks, C.byref(shape), P, big, None) == K.E_INVAL, (f, which)
+        for which in range(5):
+            o = [None, None, P, None, None]
+            o[which] = Q
+            h0, starts, marks, dh_last, dh0 = o
+            assert getattr(lib, "karma_k_gated_scan_bwd_" + f)(P, P, h0, starts, marks, P, dh_last, P, P, dh0, C.byref(shape), P, big, None) == K.E_INVAL, (f, which)
+        for name in ("tokens", "logprob", "entropy", "stats", "top_lp", "top_id"):
+            assert logprob_fwd(**{**dict(fn=f, top=2, entropy=P, stats=P, top_lp=P, top_id=P), name: Q}) == K.E_INVAL, (f, name)
+        for name in ("tokens", "stats", "entropy", "dl", "de"):
+            assert logprob_bwd(**{**dict(fn=f), name: Q}) == K.E_INVAL, (f, name)
+    ptrs = (C.c_void_p * 1)(4096 + odd)
+    good = (C.c_void_p * 1)(4096)
+    t = (K.AdamwTensor * 1)(K.AdamwTensor(w=4096, m=4096, v=4096, m_scale=4096, v_scale=4096, grad=4096, n=10, flags=4))
+    assert lib.karma_k_adamw_states(t, 1, ptrs, good, None) == K.E_INVAL and lib.karma_k_adamw_states(t, 1, good, ptrs, None) == K.E_INVAL
