@@ -83,6 +83,10 @@ class AdamwStep(C.Structure):
                 ("seed", C.c_uint32), ("step", C.c_uint64)]
 
 
+class AdamwLive(C.Structure):
+    _fields_ = [("lr", C.c_float), ("grad_scale", C.c_float), ("step", C.c_uint32), ("seed", C.c_uint32)]
+
+
 class ProductPart(C.Structure):
     _fields_ = [("kernel", C.c_uint32), ("m", C.c_uint32), ("n", C.c_uint32), ("splits", C.c_uint32)]
 

@@ -261,3 +261,24 @@ def test_operands_of_32_bits_off_their_boundaries_are_refused(odd):
     good = (C.c_void_p * 1)(4096)
     t = (K.AdamwTensor * 1)(K.AdamwTensor(w=4096, m=4096, v=4096, m_scale=4096, v_scale=4096, grad=4096, n=10, flags=4))
     assert lib.karma_k_adamw_states(t, 1, ptrs, good, None) == K.E_INVAL and lib.karma_k_adamw_states(t, 1, good, ptrs, None) == K.E_INVAL
+
+
+def test_structures_are_laid_out_as_in_the_header(tmp_path):
+    """The operators' structures, field by field, as a C compiler lays them out."""
+    import os
+    import shutil
+    import subprocess
+    cc = shutil.which("gcc") or shutil.which("cc")
+    if not cc:
+        pytest.skip("no C compiler")
+    structures = dict(karma_scan_shape=K.ScanShape, karma_adamw_tensor=K.AdamwTensor, karma_adamw_step=K.AdamwStep, karma_adamw_live=K.AdamwLive)
+    lines = ["#include <stddef.h>", "#include <stdio.h>", '#include "karma.h"', "int main(void) {"]
+    for name, s in structures.items():
+        lines.append('printf("%%zu", sizeof(%s));' % name)
+        lines += ['printf(" %%zu", offsetof(%s, %s));' % (name, f[0]) for f in s._fields_] + ['printf("\\n");']
+    (tmp_path / "l.c").write_text("\n".join(lines + ["return 0;", "}"]))
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    subprocess.run([cc, "-I", os.path.join(root, "include"), "-o", str(tmp_path / "l"), str(tmp_path / "l.c")], check=True)
+    out = subprocess.run([str(tmp_path / "l")], check=True, capture_output=True, text=True).stdout.split("\n")
+    for line, (name, s) in zip(out, structures.items()):
+        assert [int(v) for v in line.split()] == [C.sizeof(s)] + [getattr(s, f[0]).offset for f in s._fields_], name
