@@ -486,3 +486,25 @@ def test_beside_work_that_fills_the_device(torch):
     torch.cuda.synchronize()
     assert torch.isfinite(b).all()
     assert all(torch.equal(t, w) for t, w in zip((p.h, p.dgate, p.dx, p.h_last, p.dh0), want))
+
+
+@pytest.mark.parametrize("tokens,sequences,starts", SHAPES)
+@pytest.mark.parametrize("states", [(False, False), (True, False), (False, True), (True, True)])
+def test_any_of_the_states_may_be_missing(torch, tokens, sequences, starts, states):
+    """h0 and dh_last, each with and without; and neither last states nor their gradients asked for: the rest is the same, from outputs that
+    held something else."""
+    p = Problem(torch, 50, tokens, 70, sequences, starts, state=True)
+    if not states[0]:
+        p.h0 = None
+    if not states[1]:
+        p.dh_last = None
+    both(p)
+    want = [t.clone() for t in (p.h, p.dgate, p.dx)]
+    for t in (p.h, p.dgate, p.dx, p.h_last, p.dh0):
+        t.fill_(7)
+    p.forward(h_last=None)
+    p.backward(dh0=None)
+    torch.cuda.synchronize()
+    for t, w in zip((p.h, p.dgate, p.dx), want):
+        assert torch.equal(t, w) and not (t == 7).all()
+    assert (p.h_last == 7).all() and (p.dh0 == 7).all()

@@ -282,3 +282,20 @@ def test_structures_are_laid_out_as_in_the_header(tmp_path):
     out = subprocess.run([str(tmp_path / "l")], check=True, capture_output=True, text=True).stdout.split("\n")
     for line, (name, s) in zip(out, structures.items()):
         assert [int(v) for v in line.split()] == [C.sizeof(s)] + [getattr(s, f[0]).offset for f in s._fields_], name
+
+
+def test_a_workspace_that_is_too_small_is_refused():
+    lib = K.lib()
+    shape = K.ScanShape(tokens=4096, channels=64, sequences=1)
+    need = K.gated_scan_ws_bytes(shape)
+    assert need > 0
+    for f in ("bf16", "f32"):
+        for ws, size in ((P, need - 1), (P, 0), (None, need), (None, 1 << 40)):
+            assert getattr(lib, "karma_k_gated_scan_fwd_" + f)(P, P, None, None, P, None, None, C.byref(shape), ws, C.c_uint64(size), None) == K.E_OOM
+            assert getattr(lib, "karma_k_gated_scan_bwd_" + f)(P, P, None, None, P, P, None, P, P, None, C.byref(shape), ws, C.c_uint64(size),
+                                                               None) == K.E_OOM
+    need = K.token_logprob_ws_bytes(2, 100000, 20)
+    assert need > 0
+    for f in ("bf16", "f32"):
+        for ws, size in ((P, need - 1), (P, 0), (None, need), (None, 1 << 40)):
+            assert logprob_fwd(rows=2, cols=100000, top=20, top_lp=P, top_id=P, fn=f, ws=ws, ws_bytes=size) == K.E_OOM
