@@ -45,9 +45,8 @@ __device__ __forceinline__ float share_of(float f) {
   const float E = __builtin_amdgcn_exp2f(fabsf(f) * -1.44269504f);
   return copysignf(E * __builtin_amdgcn_rcpf(1.f + E), f);
 }
-__device__ __forceinline__ float step_of(float s, float x, float h) { return fmaf(s, x - h, __builtin_signbitf(s) ? x : h); }
-// The choice by the sign, where a part is run through more than once: a mask of the sign and a merge of bits, in assembly, as the compiler
-// would make comparisons of them and keep all those for the later runs, 64 pairs of scalar registers (and spill a hundred of them).
+// The choice by the sign: a mask of it and a merge of bits, in assembly, as the compiler would make a comparison of them (three places
+// more: nothing may read it in the two behind it) and keep all those for a part's later runs, 64 pairs of scalar registers.
 __device__ __forceinline__ float by_sign(float s, float positive, float negative) {
   float r;
   asm("v_ashrrev_i32 %0, 31, %1\n\tv_bfi_b32 %0, %0, %3, %2" : "=&v"(r) : "v"(s), "v"(positive), "v"(negative));
@@ -58,6 +57,7 @@ __device__ __forceinline__ float where_positive(float s, float v) {
   asm("v_ashrrev_i32 %0, 31, %1\n\tv_bfi_b32 %0, %0, 0, %2" : "=&v"(r) : "v"(s), "v"(v));
   return r;
 }
+__device__ __forceinline__ float step_of(float s, float x, float h) { return fmaf(s, x - h, by_sign(s, h, x)); }
 __device__ __forceinline__ float kept(float s, float v) { return fmaf(-s, v, where_positive(s, v)); }      // a v
 // a step of the state h and of the decay A of all steps so far
 __device__ __forceinline__ void effect_of(float s, float x, float& h, float& A) {
@@ -171,6 +171,7 @@ struct Chain {
   unsigned long long* effect;   // [place in the order of work][block of channels][channel of a lane][lane]
   unsigned* state;              // [group][as above]; the first group begins with zeros
   int chunks, blocks, width;    // blocks of channels, channels of all blocks; chunks == 1: no chain
+  int sharing;                  // blocks that share a counter: all or one
 };
 constexpr int CHAIN_APART = 32;         // 128 bytes: counters of their own cache lines
 constexpr int CHAIN_LIMIT = 1 << 20;    // looks at a word, a microsecond or so each
@@ -252,31 +253,28 @@ __global__ __launch_bounds__(256) void chain_clear_kernel(Chain c, size_t pieces
   if (i < pieces) ((u32x4*)c.effect)[i] = u32x4{~0u, ~0u, ~0u, ~0u};
 }
 
-// The work of this workgroup: a block of channels, and a chunk by its place in the order of work; false: none.  Forward, each block of
-// channels has a counter: 512 workgroups that begin at once wait up to 6 us for one (packed prompts 53 us in the kernel instead of
-// 57, 65536 x 2048 180 instead of 187).  Backward they share one: its workgroups gain by not loading all at the same time (86 us, 91 with
-// counters of their own).
-__device__ __forceinline__ bool take_work(const Chain& c, bool up, int& place, int& block) {
+// The work of this workgroup: a block of channels, and a chunk by its place in the order of work; false: none.
+__device__ __forceinline__ bool take_work(const Chain& c, int& place, int& block) {
   __shared__ unsigned ticket;
-  const unsigned own = blockIdx.x % c.blocks, first = up ? own : 0, sharing = up ? 1 : c.blocks;    // blocks that share the counter
+  const unsigned own = blockIdx.x % c.blocks, first = c.sharing > 1 ? 0 : own;
   place = 0;
   block = own;
   if (c.chunks == 1) return true;
   if (threadIdx.x == 0) ticket = atomicAdd(c.tickets + (size_t)first * CHAIN_APART, 1u);
   __syncthreads();
   const unsigned unit = __builtin_amdgcn_readfirstlane((int)ticket);
-  if (unit >= sharing * c.chunks) return false;     // (the counter is another call's too)
-  place = unit / sharing;
-  block = first + unit % sharing;
+  if (unit >= (unsigned)c.sharing * c.chunks) return false;     // (the counter is another call's too)
+  place = unit / c.sharing;
+  block = first + unit % c.sharing;
   return true;
 }
 
 // ---- forward ----------------------------------------------------------------------------------------------------
 // W wavefronts have the chunk's tokens one part behind the other, L each, a lane V channels, everything in registers: one pass over
-// memory, which bounds it (6 bytes an element in bf16 against some 20 vector operations, of which the exponential and the reciprocal are
-// eight).  Each wavefront runs through its part once for A and H, and, when the state before it is known, again for the states.  120
-// registers: two workgroups on a compute unit, so that one loads while the other waits.  One channel a lane takes 220 us instead of 191
-// for 65536 x 2048.
+// memory, which bounds it where calls are long (6 bytes an element in bf16 against vector operations of some 27 places, of which the
+// exponential and the reciprocal are eight).  Each wavefront runs through its part once for A and H, and, when the state before it is known, again for the states.  120
+// registers: two workgroups on a compute unit, so that one loads while the other waits.  One channel a lane takes 67 us instead of 58
+// for packed prompts.
 template <typename T, int V, int L, int W>
 __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(4))) void scan_fwd_kernel(ScanFwd a, Spans p, Chain chain) {
   typedef Lane<T, V> Ln;
@@ -286,7 +284,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(4))) voi
   __shared__ unsigned long long words[W];
   __shared__ int cuts[W];       // 1: a sequence begins in the part, 2: with its first token
   int chunk, block;
-  if (!take_work(chain, true, chunk, block)) return;
+  if (!take_work(chain, chunk, block)) return;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), C = (int)a.s.channels;
   const int channel = block * 64 * V + lane * V, c = channel < C ? channel : C - V;     // (lanes without a channel repeat the last one)
   const bool mine = channel < C;
@@ -388,7 +386,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(4))) voi
       float x[V];
       Ln::get(as_new(rx[i]), x);
 #pragma unroll
-      for (int e = 0; e < V; ++e) h[e] = fmaf(s[i][e], x[e] - h[e], by_sign(s[i][e], h[e], x[e]));
+      for (int e = 0; e < V; ++e) h[e] = step_of(s[i][e], x[e], h[e]);
       store(i);
     }
   } else {
@@ -411,7 +409,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(4))) voi
         float x[V];
         Ln::get(as_new(rx[i]), x);
 #pragma unroll
-        for (int e = 0; e < V; ++e) h[e] = fmaf(s[i][e], x[e] - h[e], by_sign(s[i][e], h[e], x[e]));
+        for (int e = 0; e < V; ++e) h[e] = step_of(s[i][e], x[e], h[e]);
         store(i);
       }
       if ((q.ends & run) && a.h_last && mine) {
@@ -469,10 +467,8 @@ __device__ __forceinline__ void short_part(const ScanFwd& a, int t0, int n, unsi
     for (int i = 0; i < L; ++i) step(i);
   } else {
 #pragma unroll
-    for (int i = 0; i < L - 1; ++i) {
-      if (i >= n) break;
-      step(i);
-    }
+    for (int i = 0; i < L - 1; ++i)
+      if (i < n) step(i);
   }
 }
 template <typename T, int V>
@@ -502,8 +498,8 @@ __global__ __launch_bounds__(256) void scan_fwd_short_kernel(ScanFwd a, Spans p,
 // As forward, with the chain from the last chunk to the first: the gradient g of the state behind a part goes in, that of the state
 // before it comes out, out = A g + R.  The states are run through again from the chunk's mark: 10 bytes an element in bf16 where reading
 // h would make 12, and exact.  Three inputs, the shares and the gaps leave room for 16 tokens a wavefront, so the chunk takes 16
-// wavefronts; without states (STATES) 90 registers, so that wavefronts of the next chunk begin while the last of this one end: with 32 x
-// 1024 tokens of 1024 channels 87 us, 106 with 128 registers, 173 with spills.  One channel a lane: 120.
+// wavefronts; 90 registers, 94 with states (STATES), so that wavefronts of the next chunk begin while the last of this one end: with 32 x
+// 1024 tokens of 1024 channels 92 us a call, 94 with room for 128 registers; with states 101, 103.  One channel a lane: 117 and 136.
 template <typename T, int V, int L, int W, bool STATES>
 __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(5))) void scan_bwd_kernel(ScanBwd a, Spans p, Chain chain) {
   typedef Lane<T, V> Ln;
@@ -514,7 +510,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(5))) voi
   __shared__ unsigned long long words[W];
   __shared__ int cuts[W];       // 1: a sequence begins in the part, 2: one ends in it, 4: with its last token
   int place, block;
-  if (!take_work(chain, false, place, block)) return;
+  if (!take_work(chain, place, block)) return;
   const int chunk = chain.chunks - 1 - place;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), C = (int)a.s.channels;
   const int channel = block * 64 * V + lane * V, c = channel < C ? channel : C - V;
@@ -688,14 +684,15 @@ __global__ void copy_or_zero_kernel(const float* x, float* y, size_t n) {
   if (i < n) y[i] = x ? x[i] : 0.f;
 }
 
-// Whether wavefronts take whole sequences (`units` of them), at 0.09 us a token where they are few.  Sequences of one length, 1024 channels
-// in bf16, us by whole sequences / in chunks: 4096 x 1 token 13.6 / 58.8, 1 x 64 7.0 / 10.5, 16 x 128 12.4 / 15.3, 16 x 256 22.9 / 16.5;
-// where there are 512 units (8 a sequence here) 64 x 256 30.2 / 35.4, 64 x 512 52.7 / 58.2, with fewer 32 x 256 27.4 / 23.2.  Of packed
-// ones nobody here knows the longest: up to 512 tokens more than sequences, of which it can have 513 at most.  64 x 8 4.7 / 18.9,
-// 64 x 16 5.1 / 16.8, 63 x 1 and one of 512 43.6 / 36.2, 20 x 1 and one of 1024 84 / 28, 63 x 1 and one of 1900 180 / 36.7.
+// Whether wavefronts take whole sequences (`units` of them), at 0.11 us a token where they are few.  Sequences of one length, 1024 channels
+// in bf16, us a call by whole sequences / in chunks: 4096 x 1 token 13.8 / 38.9; in a single chunk 1 x 96 11.3 / 12.1, 1 x 128 14.7 / 12.1;
+// 16 x 128 15.0 / 16.3, 16 x 160 18.5 / 18.1; with 512 units (8 a sequence here) 64 x 192 23.0 / 27.0, 64 x 256 29.4 / 26.8; with 1024
+// 128 x 256 34.5 / 49.3, 128 x 512 86 / 103.  Of packed ones nobody here knows the longest: up to 512 tokens more than sequences, of which it
+// can have 513 at most.  64 x 8 5.3 / 19.9, 63 x 1 and one of 300 32.3 / 37.1, of 512 53.4 / 36.8, of 1900 189 / 37.3.
 bool whole_sequences(const karma_scan_shape& s, bool packed, uint64_t units) {
   if (packed) return s.tokens <= s.sequences + 512ull && s.tokens <= 128ull * s.sequences;
-  return s.tokens <= (units >= 512 ? 512ull : 128ull) * s.sequences;
+  const uint64_t most = units >= 1024 ? 512 : units >= 512 ? 192 : s.tokens > KARMA_SCAN_MARK ? 128 : 96;
+  return s.tokens <= most * s.sequences;
 }
 
 // chunks of a call; channels of all blocks whatever a lane has
@@ -735,11 +732,16 @@ size_t gated_scan_ws_bytes(const karma_scan_shape& given) {
 static Spans spans_of(const karma_scan_shape& s, const int* starts) {
   return Spans{starts, (int)s.tokens, (int)s.sequences, starts ? 0 : (int)(s.tokens / s.sequences)};
 }
-// V channels a lane; the chain is cleared by a kernel ahead (a call that is captured has kernels alone)
-static Chain chain_of(const karma_scan_shape& s, int V, void* ws, hipStream_t stream) {
-  const uint64_t chunks = scan_chunks(s.tokens), width = scan_width(s.channels);
+// V channels a lane; the chain is cleared by a kernel ahead (a call that is captured has kernels alone).  One counter for all blocks of
+// channels, or one each?  512 workgroups that begin at once wait some microseconds for one counter; from then on workgroups
+// gain by not loading all at the same time, which one counter sees to.  So forward from 2048 workgroups on, four times what runs at
+// once (one / each, us a call: 65536 x 2048 163 / 181, 32768 x 2048 95 / 97, 16384 x 2048 60 / 56, packed prompts 60 / 58; fp32
+// 65536 x 2048 297 / 326, 32768 x 1024 90 / 92, 65536 x 256 64 / 59), and backward always (32 x 1024 x 1024 92 / 94, 32768 x 2048 164 / 171).
+static Chain chain_of(const karma_scan_shape& s, int V, bool forward, void* ws, hipStream_t stream) {
+  const uint64_t chunks = scan_chunks(s.tokens), width = scan_width(s.channels), blocks = ((uint64_t)s.channels + 64 * V - 1) / (64 * V);
   unsigned long long* effect = (unsigned long long*)((char*)ws + chain_head(width));
-  const Chain c{(unsigned*)ws, effect, (unsigned*)(effect + chunks * width), (int)chunks, (int)((s.channels + 64 * V - 1) / (64 * V)), (int)width};
+  const Chain c{(unsigned*)ws, effect, (unsigned*)(effect + chunks * width), (int)chunks, (int)blocks, (int)width,
+                forward && blocks * chunks < 2048 ? 1 : (int)blocks};
   const size_t pieces = chain_words(chunks, width) / 16;
   if (chunks > 1) hipLaunchKernelGGL(chain_clear_kernel, dim3((unsigned)((pieces + 255) / 256)), dim3(256), 0, stream, c, pieces);
   return c;
@@ -763,7 +765,7 @@ int gated_scan_fwd(ScanFwd a, bool bf16, hipStream_t s) {
     else if (bf16) hipLaunchKernelGGL((scan_fwd_short_kernel<bf16_t, 1>), grid, dim3(256), 0, s, a, p, blocks, units);
     else hipLaunchKernelGGL((scan_fwd_short_kernel<float, 1>), grid, dim3(256), 0, s, a, p, blocks, units);
   } else {
-    const Chain c = chain_of(a.s, pairs ? 2 : 1, a.ws, s);
+    const Chain c = chain_of(a.s, pairs ? 2 : 1, true, a.ws, s);
     const dim3 grid(chain_grid(c));
     if (pairs) hipLaunchKernelGGL((scan_fwd_kernel<bf16_t, 2, 32, 8>), grid, dim3(512), 0, s, a, p, c);
     else if (bf16) hipLaunchKernelGGL((scan_fwd_kernel<bf16_t, 1, 32, 8>), grid, dim3(512), 0, s, a, p, c);
@@ -789,7 +791,7 @@ int gated_scan_bwd(ScanBwd a, bool bf16, hipStream_t s) {
   const bool pairs = bf16 && a.s.channels % 2 == 0 && (a.s.ld_gate | a.s.ld_x | a.s.ld_h | a.s.ld_dgate | a.s.ld_dx) % 2 == 0 &&
                      aligned_to(a.gate, 4) && aligned_to(a.x, 4) && aligned_to(a.dh, 4) && aligned_to(a.dgate, 4) && aligned_to(a.dx, 4);
   const Spans p = spans_of(a.s, a.starts);
-  const Chain c = chain_of(a.s, pairs ? 2 : 1, a.ws, s);
+  const Chain c = chain_of(a.s, pairs ? 2 : 1, false, a.ws, s);
   const dim3 grid(chain_grid(c));
 #define KARMA_SCAN_BWD(T, V)                                                                                           \
   do {                                                                                                                 \
