@@ -508,3 +508,39 @@ def test_any_of_the_states_may_be_missing(torch, tokens, sequences, starts, stat
     for t, w in zip((p.h, p.dgate, p.dx), want):
         assert torch.equal(t, w) and not (t == 7).all()
     assert (p.h_last == 7).all() and (p.dh0 == 7).all()
+
+
+@pytest.mark.parametrize("bf16,each,sequences,channels", [(True, 300, 1030, 64), (False, 512, 520, 66), (True, 192, 520, 60), (False, 97, 2, 33), (True, 96, 2, 70),
+                                                          (True, 128, 3, 70)])
+def test_many_whole_sequences(torch, bf16, each, sequences, channels):
+    """Sequences that are taken whole although marks lie inside them, and lengths next to the borders of that rule: some of the sequences
+    against the plain form, forward and, from the marks, backward."""
+    t = torch.bfloat16 if bf16 else torch.float32
+    gen = torch.Generator(device="cuda").manual_seed(60)
+    tokens = each * sequences
+    make = lambda rows, mean=0.0, dtype=t: torch.empty((rows, channels), device="cuda", dtype=dtype).normal_(mean, 1.0, generator=gen)
+    p = Problem(torch, 61, 1, channels, bf16=bf16)
+    p.tokens, p.sequences = tokens, sequences
+    p.gate, p.x, p.dh, p.h0, p.dh_last = make(tokens, 3.0), make(tokens), make(tokens), make(sequences, dtype=torch.float32), make(sequences, dtype=torch.float32)
+    p.h, p.dgate, p.dx, p.h_last, p.dh0 = (torch.zeros_like(a) for a in (p.gate, p.gate, p.gate, p.h0, p.h0))
+    p.marks = torch.zeros((-(-tokens // K.SCAN_MARK), channels), device="cuda")
+    p.shape = K.ScanShape(tokens=tokens, channels=channels, sequences=sequences)
+    p.ws_bytes = K.gated_scan_ws_bytes(p.shape)
+    p.ws = torch.full((max(16, p.ws_bytes),), 0x5A, dtype=torch.uint8, device="cuda")
+    p.forward()
+    p.backward()
+    torch.cuda.synchronize()
+    h2 = lambda a: a.float().cpu().numpy().astype(np.float64)
+    for j in {0, 1, sequences // 2, sequences - 1}:
+        rows = slice(j * each, (j + 1) * each)
+        want, bound = F.scan_by_shares(h2(p.gate[rows]), h2(p.x[rows]), [0, each], h2(p.h0[j:j + 1]), h2(p.dh[rows]), h2(p.dh_last[j:j + 1]))
+        for k in want:
+            wide = k in ("h", "dgate", "dx")
+            got, e = h2(getattr(p, k)[rows] if wide else getattr(p, k)[j:j + 1]), bound[k]
+            if bf16 and wide:
+                e = e + BF16_HALF * (np.abs(want[k]) + e) + 1e-38
+            assert (np.abs(got - want[k]) <= e).all(), (k, j)
+        for r in range(-(-rows.start // K.SCAN_MARK) * K.SCAN_MARK, rows.stop, K.SCAN_MARK):
+            if r > rows.start:
+                at = r - rows.start - 1
+                assert (np.abs(h2(p.marks[r // K.SCAN_MARK]) - want["h"][at]) <= bound["h"][at]).all(), (j, r)
