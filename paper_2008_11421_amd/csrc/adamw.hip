@@ -187,8 +187,8 @@ __device__ __forceinline__ Codes quantised_step(const Codes& c, const f32x4& g, 
 }
 
 // A workgroup has 1024 consecutive values, a lane four of them: 16-byte accesses of the fp32 buffers.  Reads and writes 28 bytes a
-// value (bf16 gradient and weight), 16.25 with 8-bit moments: bound by memory.  217 M values in 8 bits take 711 us, 5.0 TB/s, 63 M in
-// 609 tensors 376 us; four groups of 1024 a workgroup, loaded ahead, take 813 and 430 (more registers, fewer wavefronts).
+// value (bf16 gradient and weight), 16.25 with 8-bit moments: bound by memory.  217 M values in 8 bits take 721 us, 4.9 TB/s, 63 M in
+// 609 tensors 373 us, 4.7 TB/s; four groups of 1024 a workgroup, loaded ahead, take 14 % longer (more registers, fewer wavefronts).
 constexpr unsigned ADAMW_SPAN = 1024;
 constexpr unsigned ADAMW_GRID = (1u << 24) - 1;     // workgroups of 256 lanes in a launch, which has less than 2^32
 template <bool EIGHT>
@@ -238,7 +238,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamwSet<EIGHT> u, AdamwNow 
   }
 }
 
-// The moments that 8-bit states stand for: four values a lane; 2.1 bytes in, 8 out (217 M values 391 us, 5.7 TB/s).
+// The moments that 8-bit states stand for: four values a lane; 2.1 bytes in, 8 out (217 M values 365 us, 6.0 TB/s).
 struct StatesTensor {
   const uint8_t* m; const uint8_t* v;
   const float* m_scale; const float* v_scale;

@@ -303,9 +303,9 @@ __device__ __forceinline__ void finish_row(const LogprobFwd& a, size_t r, Runnin
 }
 
 // W wavefronts share a part of a row (`parts` parts a row, W = 1: the whole row), lanes side by side on vectors.  One pass: every
-// vector goes into the running sums and past the list of alternatives.  Bound by memory: 4096 x 32000 in bf16 54 us, 4.8 TB/s (eight
-// vectors under way instead of four: 62); with 5 alternatives 67, with 20 73, with 64 92, which is the work on keys (inserting them one by
-// one into a list in registers took 72, 94 and 127; comparing all candidates with each other 87 with 5).
+// vector goes into the running sums and past the list of alternatives.  Bound by memory: 4096 x 32000 in bf16 55 us a call, 4.7
+// TB/s (eight vectors under way instead of four: 62); with 5 alternatives 63, with 20 68, with 64 85, which is the work on keys (inserting
+// them one by one into a list in registers took 72, 94 and 127; comparing all candidates with each other 87 with 5).
 template <typename T, int W, bool TOP>
 __global__ __launch_bounds__(LP_THREADS) void logprob_fwd_kernel(LogprobFwd a, unsigned parts, LogprobPart* sums, uint64_t* lists) {
   constexpr int N = Vec<T>::N;
@@ -479,8 +479,8 @@ __global__ __launch_bounds__(LP_THREADS) void logprob_join_kernel(LogprobFwd a, 
 }
 
 // ---- backward ------------------------------------------------------------------------------------------------
-// A wavefront has LP_BATCH vectors of each lane of one row; `units` wavefronts a row.  Bound by memory: 4096 x 51200 in bf16 143 us,
-// 5.9 TB/s.
+// A wavefront has LP_BATCH vectors of each lane of one row; `units` wavefronts a row.  Bound by memory: 4096 x 51200 in bf16 144 us
+// a call, 5.8 TB/s.
 template <typename T>
 __global__ __launch_bounds__(LP_THREADS) void logprob_bwd_kernel(LogprobBwd a, unsigned units) {
   constexpr int N = Vec<T>::N, SPAN = 64 * LP_BATCH;
