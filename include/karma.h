@@ -605,8 +605,8 @@ int karma_k_attention_bwd_bf16(const void* qkv_dev, const void* ctx_dev, const v
  * ws_dev: karma_k_gated_scan_ws_bytes(shape) bytes (0 for a wrong shape), 16-byte aligned, for one call at a time: calls that may run at the same
  * time (graphs replayed on two streams among them) need a workspace each.  The call clears what it needs cleared.  Where another call uses the
  * workspace at the same time, results are wrong: wherever a word of it does not come for some 2^20 looks, a second or so, states and
- * gradients become NaN, after the call has returned KARMA_OK.  A call that has its workspace to itself waits for as long as it takes
- * its own earlier workgroups, whatever else is on the device.
+ * gradients become NaN, after the call has returned KARMA_OK.  A call that has its workspace to itself waits only for workgroups of its
+ * own that have begun, whatever else is on the device.
  * Errors: KARMA_E_INVAL (operands off their elements' boundaries among them), KARMA_E_OOM (ws_bytes too small). */
 #define KARMA_SCAN_MARK 256u
 typedef struct {

@@ -271,10 +271,10 @@ __device__ __forceinline__ bool take_work(const Chain& c, int& place, int& block
 
 // ---- forward ----------------------------------------------------------------------------------------------------
 // W wavefronts have the chunk's tokens one part behind the other, L each, a lane V channels, everything in registers: one pass over
-// memory, which bounds it where calls are long (6 bytes an element in bf16 against vector operations of some 27 places, of which the
-// exponential and the reciprocal are eight).  Each wavefront runs through its part once for A and H, and, when the state before it is known, again for the states.  120
-// registers: two workgroups on a compute unit, so that one loads while the other waits.  One channel a lane takes 67 us instead of 58
-// for packed prompts.
+// memory, which bounds long calls (6 bytes an element in bf16 against some 27 issue slots of vector operations, of which the exponential and
+// the reciprocal take eight).  Each wavefront runs through its part once for A and H, and, when the state before it is known, again for
+// the states.  121 registers: two workgroups on a compute unit, so that one loads while the other waits.  One channel a lane takes 67 us
+// instead of 58 for packed prompts.
 template <typename T, int V, int L, int W>
 __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(4))) void scan_fwd_kernel(ScanFwd a, Spans p, Chain chain) {
   typedef Lane<T, V> Ln;
