@@ -706,6 +706,106 @@ int karma_k_adamw(const karma_adamw_tensor* tensors, uint32_t n, const karma_ada
  * arrays of n device pointers, to as many values as the tensor has.  All tensors need the flag; w, grad and out are not looked at. */
 int karma_k_adamw_states(const karma_adamw_tensor* tensors, uint32_t n, float* const* m_out, float* const* v_out, void* stream);
 
+/* ---- queries and keys on their way to attention: a norm for each head and the rotation by position, in one pass --------
+ * q_dev [tokens][heads_q * d] and k_dev [tokens][heads_k * d] (rows ld_q and ld_k elements apart; 0: one behind the other) become
+ * yq_dev and yk_dev (ld_yq, ld_yk); all may be parts of one buffer, such as a projection's thirds, and an output may be its input
+ * where their strides are equal; no other overlap.  For every head's x of d columns (even, up to KARMA_QK_D_MAX):
+ *   KARMA_QK_NORM: n = x gamma / sqrt(mean(x^2) + eps), gamma [d] of the operands' type (NULL: ones); else n = x, and gamma is NULL;
+ *   the first `rot` columns (even; 0: none, which needs the norm) are turned in pairs: (a, b) -> (a cos - b sin, b cos + a sin) by the
+ *   angle position * freq_dev[i], pair i being columns i and i + rot / 2, or with KARMA_QK_PAIRS columns 2 i and 2 i + 1.
+ * freq_dev fp64 [rot / 2], radians from one position to the next; positions_dev int32 [tokens], or NULL: token % seq (seq 0: tokens).
+ * Angles are computed in 64 bits, everything else in 32, rounded once.  |x| up to 1e18: its square has to fit 32 bits.
+ * v_dev [tokens][heads_v * d] goes to yv_dev unchanged (heads_v 0, or yv_dev == v_dev: nothing is moved), so that the three parts
+ * of a projection's output become those that attention reads.
+ * tokens up to KARMA_QK_TOKENS_MAX, heads of a kind up to KARMA_QK_HEADS_MAX.  Errors: KARMA_E_INVAL (operands off their elements'
+ * boundaries among them). */
+#define KARMA_QK_NORM 1u
+#define KARMA_QK_PAIRS 2u
+#define KARMA_QK_D_MAX 256u
+#define KARMA_QK_TOKENS_MAX ((1u << 26) - 8)
+#define KARMA_QK_HEADS_MAX (1u << 14)
+typedef struct {
+  uint64_t tokens, seq;
+  uint32_t heads_q, heads_k, heads_v; /* one of the first two may be 0 */
+  uint32_t d, rot, flags;
+  float eps; /* above 0 with the norm */
+  uint64_t ld_q, ld_k, ld_v, ld_yq, ld_yk, ld_yv, ld_dq, ld_dk, ld_dv; /* ld_y*: of y and of dy */
+} karma_qk_shape;
+int karma_k_qk_rotary_fwd_bf16(const void* q_dev, const void* k_dev, const void* v_dev, const void* gamma_q_dev, const void* gamma_k_dev,
+                               const int32_t* positions_dev, const double* freq_dev, void* yq_dev, void* yk_dev, void* yv_dev,
+                               const karma_qk_shape* shape, void* stream);
+int karma_k_qk_rotary_fwd_f32(const float* q_dev, const float* k_dev, const float* v_dev, const float* gamma_q_dev, const float* gamma_k_dev,
+                              const int32_t* positions_dev, const double* freq_dev, float* yq_dev, float* yk_dev, float* yv_dev,
+                              const karma_qk_shape* shape, void* stream);
+/* Its backward: dq_dev and dk_dev from the gradients dyq_dev and dyk_dev of its results and from its inputs (q_dev and k_dev are not
+ * looked at without the norm); dgamma_q_dev and dgamma_k_dev fp32 [d] (each may be NULL; with the norm only), summed in a fixed order.  dyv_dev goes to
+ * dv_dev as v_dev does.  An output may be dy or the input of its part where the strides are equal; no other overlap.
+ * ws_dev: karma_k_qk_rotary_ws_bytes(shape) bytes (0 for a wrong shape and without the norm), 16-byte aligned, for one call at a
+ * time; not looked at where no dgamma is asked for.  Errors: KARMA_E_INVAL, KARMA_E_OOM. */
+uint64_t karma_k_qk_rotary_ws_bytes(const karma_qk_shape* shape);
+int karma_k_qk_rotary_bwd_bf16(const void* dyq_dev, const void* dyk_dev, const void* dyv_dev, const void* q_dev, const void* k_dev,
+                               const void* gamma_q_dev, const void* gamma_k_dev, const int32_t* positions_dev, const double* freq_dev,
+                               void* dq_dev, void* dk_dev, void* dv_dev, float* dgamma_q_dev, float* dgamma_k_dev,
+                               const karma_qk_shape* shape, void* ws_dev, uint64_t ws_bytes, void* stream);
+int karma_k_qk_rotary_bwd_f32(const float* dyq_dev, const float* dyk_dev, const float* dyv_dev, const float* q_dev, const float* k_dev,
+                              const float* gamma_q_dev, const float* gamma_k_dev, const int32_t* positions_dev, const double* freq_dev,
+                              float* dq_dev, float* dk_dev, float* dv_dev, float* dgamma_q_dev, float* dgamma_k_dev,
+                              const karma_qk_shape* shape, void* ws_dev, uint64_t ws_bytes, void* stream);
+
+/* ---- a row's next token, drawn by a given random number ---------------------------------------------
+ * logits_dev [rows][ld], cols <= ld used (ld 0: cols).  With the rule of the row (rules_dev holds `rules` of them: one for all rows, or
+ * one for each) and m the largest logit, token j has the weight
+ *   w_j = 2^40 e^((z_j - m) / temperature), rounded to a whole number: a row's sums are exact, in whatever order they are taken.
+ * In the order of falling logits, equal ones by rising index, there stay: the first top_k tokens (0: all); of these the shortest
+ * beginning whose weights reach top_p times theirs (at least one; top_p 1 or more: all); of these the tokens with w_j >= min_p 2^40
+ * (at least the first), and of these those with w_j > 0.  Their weights, summed up by rising index, first exceed uniform_dev[row] times their sum,
+ * rounded down, at the token drawn; uniform fp32 in [0, 1) (less counts as 0, more as the last token).  temperature 0: the first of the largest.
+ * (The products with top_p and uniform are rounded to 64-bit floating point.)
+ * Outputs, each NULL where it is not wanted (not all of them): token_dev int32 [rows]; logprob_dev fp32 [rows], the logarithm of the token's share of
+ * what stays; kept_dev int32 [rows], how many tokens stay.
+ * A logit of -inf has no weight.  A row without answer (NaN or +inf in it, nothing but -inf; a rule with a temperature that is negative, infinite or
+ * NaN, or a NaN in top_p or min_p) gives token -1, logprob NaN and kept 0.
+ * ws_dev: karma_k_sample_ws_bytes(rows, cols) bytes, 16-byte aligned, for one call at a time (0 bytes: may be NULL).
+ * cols up to KARMA_SAMPLE_COLS_MAX, rows < 2^20.  Errors: KARMA_E_INVAL (operands off their elements' boundaries among them), KARMA_E_OOM. */
+#define KARMA_SAMPLE_COLS_MAX ((1u << 22) - 1)
+typedef struct {
+  float temperature, top_p, min_p;
+  uint32_t top_k;
+} karma_sample_rule;
+uint64_t karma_k_sample_ws_bytes(uint32_t rows, uint32_t cols);
+int karma_k_sample_bf16(const void* logits_dev, uint64_t ld, const karma_sample_rule* rules_dev, uint32_t rules, const float* uniform_dev,
+                        int32_t* token_dev, float* logprob_dev, int32_t* kept_dev, uint32_t rows, uint32_t cols, void* ws_dev,
+                        uint64_t ws_bytes, void* stream);
+int karma_k_sample_f32(const float* logits_dev, uint64_t ld, const karma_sample_rule* rules_dev, uint32_t rules, const float* uniform_dev,
+                       int32_t* token_dev, float* logprob_dev, int32_t* kept_dev, uint32_t rows, uint32_t cols, void* ws_dev,
+                       uint64_t ws_bytes, void* stream);
+
+/* ---- the global norm of many gradients, and clipping ------------------------------------------------
+ * With s = grad_scale (above 0), over all values of all tensors: norm = s sqrt(sum g^2), factor = s min(1, max_norm / norm): what a step with clipped
+ * gradients multiplies them by.  norm_dev, factor_dev fp32 [1] and tensor_norms_dev fp32 [n] (s times the norm of each) may be NULL, not
+ * all of them; factor_dev may be the grad_scale of a karma_adamw_live, whose update then clips without another pass.  max_norm above 0,
+ * INFINITY: no bound.  Sums are taken in 64 bits in a fixed order.  An infinite gradient makes the norm infinite and the factor 0 (with no bound: s), NaN
+ * makes both NaN.  Tensors hold n values, bf16 with KARMA_GRAD_BF16, else fp32, on boundaries of their elements; n may be 0 (grad NULL);
+ * all together up to KARMA_GRAD_VALUES_MAX, at most KARMA_GRAD_TENSORS_MAX tensors.  `out` is not looked at.
+ * tensors is a host array, read during the call.  ws_dev: karma_k_grad_norm_ws_bytes(tensors, n) bytes (0 for a wrong list), 16-byte aligned, for
+ * one call at a time.  Errors: KARMA_E_INVAL, KARMA_E_OOM. */
+#define KARMA_GRAD_BF16 1u
+#define KARMA_GRAD_OUT_BF16 2u
+#define KARMA_GRAD_VALUES_MAX (1ull << 35)
+#define KARMA_GRAD_TENSORS_MAX (1u << 20)
+typedef struct {
+  const void* grad;
+  void* out; /* bf16 with KARMA_GRAD_OUT_BF16, else fp32 */
+  uint64_t n;
+  uint32_t flags;
+} karma_grad_tensor;
+uint64_t karma_k_grad_norm_ws_bytes(const karma_grad_tensor* tensors, uint32_t n);
+int karma_k_grad_norm(const karma_grad_tensor* tensors, uint32_t n, float max_norm, float grad_scale, float* norm_dev,
+                      float* tensor_norms_dev, float* factor_dev, void* ws_dev, uint64_t ws_bytes, void* stream);
+/* out = factor_dev[0] * grad for every tensor (out may be grad where both have one type: a factor of 1 then touches nothing; no other overlap,
+ * other tensors of the list included).  Errors: KARMA_E_INVAL. */
+int karma_k_grad_clip(const karma_grad_tensor* tensors, uint32_t n, const float* factor_dev, void* stream);
+
 /* ---- convolutional workload (Sec. III-C: convolution, batch normalisation, ReLU and
  * pooling layers).  Tensors are NHWC bf16, convolution weights [c_out][r][s][c_in]; c_in and
  * c_out must be multiples of 8 (an image with 3 channels is stored with 8, the rest zero).

@@ -22,6 +22,9 @@ GEMM_GELU_FWD, GEMM_GELU_BWD = 1, 2
 PRODUCT_STAGED_SMALL, PRODUCT_STAGED_LARGE, PRODUCT_SMALL, PRODUCT_LARGE, PRODUCT_NARROW = range(5)
 PRODUCT_SLICES, PRODUCT_BROAD, PRODUCT_FLAT, PLAN_TILES = 5, 6, 7, 1 << 31
 SCAN_MARK, TOP_MAX = 256, 64
+QK_NORM, QK_PAIRS, QK_D_MAX = 1, 2, 256
+SAMPLE_COLS_MAX = (1 << 22) - 1
+GRAD_BF16, GRAD_OUT_BF16 = 1, 2
 ADAMW_GRAD_BF16, ADAMW_OUT_BF16, ADAMW_STATES_8BIT, ADAMW_BLOCK = 1, 2, 4, 64
 CONV_FWD, CONV_DGRAD, CONV_WGRAD, CONV_KEEP_SUMS = 0, 1, 2, 4
 
@@ -71,6 +74,21 @@ class ConvShape(C.Structure):
 class ScanShape(C.Structure):
     _fields_ = [("tokens", C.c_uint64), ("channels", C.c_uint32), ("sequences", C.c_uint32), ("ld_gate", C.c_uint64), ("ld_x", C.c_uint64),
                 ("ld_h", C.c_uint64), ("ld_dgate", C.c_uint64), ("ld_dx", C.c_uint64)]
+
+
+class QkShape(C.Structure):
+    _fields_ = [("tokens", C.c_uint64), ("seq", C.c_uint64), ("heads_q", C.c_uint32), ("heads_k", C.c_uint32), ("heads_v", C.c_uint32),
+                ("d", C.c_uint32), ("rot", C.c_uint32), ("flags", C.c_uint32), ("eps", C.c_float), ("ld_q", C.c_uint64), ("ld_k", C.c_uint64),
+                ("ld_v", C.c_uint64), ("ld_yq", C.c_uint64), ("ld_yk", C.c_uint64), ("ld_yv", C.c_uint64), ("ld_dq", C.c_uint64),
+                ("ld_dk", C.c_uint64), ("ld_dv", C.c_uint64)]
+
+
+class SampleRule(C.Structure):
+    _fields_ = [("temperature", C.c_float), ("top_p", C.c_float), ("min_p", C.c_float), ("top_k", C.c_uint32)]
+
+
+class GradTensor(C.Structure):
+    _fields_ = [("grad", C.c_void_p), ("out", C.c_void_p), ("n", C.c_uint64), ("flags", C.c_uint32)]
 
 
 class AdamwTensor(C.Structure):
@@ -131,6 +149,9 @@ def lib():
         _lib.karma_destroy.argtypes = [C.c_void_p]
         _lib.karma_k_gated_scan_ws_bytes.restype = C.c_uint64
         _lib.karma_k_token_logprob_ws_bytes.restype = C.c_uint64
+        _lib.karma_k_qk_rotary_ws_bytes.restype = C.c_uint64
+        _lib.karma_k_sample_ws_bytes.restype = C.c_uint64
+        _lib.karma_k_grad_norm_ws_bytes.restype = C.c_uint64
     return _lib
 
 
@@ -165,6 +186,19 @@ def gated_scan_ws_bytes(shape):
 
 def token_logprob_ws_bytes(rows, cols, top=0):
     return lib().karma_k_token_logprob_ws_bytes(rows, cols, top)
+
+
+def qk_rotary_ws_bytes(shape):
+    return lib().karma_k_qk_rotary_ws_bytes(C.byref(shape))
+
+
+def sample_ws_bytes(rows, cols):
+    return lib().karma_k_sample_ws_bytes(C.c_uint32(rows), C.c_uint32(cols))
+
+
+def grad_norm_ws_bytes(tensors):
+    """tensors: a ctypes array of GradTensor"""
+    return lib().karma_k_grad_norm_ws_bytes(tensors, len(tensors))
 
 
 def _layers_array(layers):

@@ -208,6 +208,31 @@ int token_logprob_bwd(LogprobBwd a, bool bf16, hipStream_t s);
 int adamw(const karma_adamw_tensor* tensors, uint32_t n, const karma_adamw_step& now, const karma_adamw_live* live, hipStream_t s);
 int adamw_states(const karma_adamw_tensor* tensors, uint32_t n, float* const* m_out, float* const* v_out, hipStream_t s);
 
+// ---- norms of queries and keys with the rotation by position (qk_rotary.hip); three pointers: queries, keys, values
+size_t qk_rotary_ws_bytes(const karma_qk_shape& s);
+int qk_rotary_fwd(const void* const* x, const void* const* gamma, const int* positions, const double* freq, void* const* y, const karma_qk_shape& s,
+                  bool bf16, hipStream_t stream);
+int qk_rotary_bwd(const void* const* dy, const void* const* x, const void* const* gamma, const int* positions, const double* freq, void* const* dx,
+                  float* const* dgamma, const karma_qk_shape& s, void* ws, size_t ws_bytes, bool bf16, hipStream_t stream);
+
+// ---- drawing of tokens (sample.hip); strides of 0 become cols
+struct SampleArgs {
+  const void* logits; uint64_t ld;
+  const karma_sample_rule* rules; uint32_t n_rules;
+  const float* uniform;
+  int* token; float* logprob; int* kept;
+  uint32_t rows, cols;
+  void* ws; size_t ws_bytes;
+};
+size_t sample_ws_bytes(uint32_t rows, uint32_t cols);
+int sample_rows(SampleArgs a, bool bf16, hipStream_t s);
+
+// ---- the global norm of gradients, clipping (grad_norm.hip)
+size_t grad_norm_ws_bytes(const karma_grad_tensor* tensors, uint32_t n);
+int grad_norm(const karma_grad_tensor* tensors, uint32_t n, float max_norm, float scale, float* norm, float* each, float* factor, void* ws,
+              size_t ws_bytes, hipStream_t s);
+int grad_clip(const karma_grad_tensor* tensors, uint32_t n, const float* factor, hipStream_t s);
+
 // ---- fused causal attention (attention.hip); seq multiple of 128, d in {64, 128, 152}
 int attention_fwd(const bf16_t* qkv, bf16_t* ctx, float* lse, int batch, int seq, int heads, int d, hipStream_t s);
 int attention_bwd(const bf16_t* qkv, const bf16_t* ctx, const bf16_t* dctx, const float* lse, float* delta,
