@@ -1,11 +1,10 @@
 // Draws a token from every row of logits: temperature, top-k, top-p, min-p, one uniform number a row.
 // With m the row's largest logit, token j weighs w_j = rint(2^40 e^((z_j - m) / T)).  Whole numbers: their sums are exact and the
 // same in whatever order lanes, wavefronts and passes take them, so which token stays and which is drawn hangs on no order.
-// Tokens are ordered by falling logit, equal ones by rising index; what top-k and top-p leave is a beginning of that order, "all before
-// the pair (logit, index)", and min-p cuts its end off by weight.  The pair is found without sorting: the row is counted (or weighed)
-// into 2048 bins of equal width in (m - z) / T, the bin that the border falls into is cut again by the bits of its logits, until a bin is a single
-// value; of its tokens, which weigh the same, the first ones by index stay.
-// A workgroup has a row and goes over it several times: the first time from memory, then from the L2.
+// Tokens are ordered by falling logit, equal ones by rising index; what top-k, top-p and min-p leave is a beginning of that order: all tokens
+// above a logit, the border, and the first `ties` of those that equal it.  The border is found by counting and weighing the row, without sorting,
+// and the draw by sums over runs of columns: of the wavefronts, of tiles, of lanes.
+// A workgroup has a row and goes over it a few times: the first time from memory, then from the L2.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -31,7 +30,15 @@ template <>
 struct RowVec<bf16_t> {
   static constexpr int N = 8;
   static __device__ __forceinline__ void unpack(const u32x4& v, float* f) { unpack8(v, f); }
-  static __device__ __forceinline__ float one(const bf16_t* p) { return bf2f(*p); }
+  static __device__ __forceinline__ float nth(const u32x4& v, int e) {
+    const unsigned d = e & 4 ? (e & 2 ? v[3] : v[2]) : e & 2 ? v[1] : v[0];
+    return __uint_as_float(e & 1 ? d & 0xffff0000u : d << 16);
+  }
+  static __device__ __forceinline__ u32x4 nothing() { return u32x4{0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u}; }
+  static __device__ __forceinline__ void put(u32x4& v, unsigned at, bf16_t x) {
+#pragma unroll
+    for (unsigned i = 0; i < 4; ++i) v[i] = at / 2 != i ? v[i] : at % 2 ? (v[i] & 0xffff) | (unsigned)x << 16 : (v[i] & 0xffff0000u) | x;
+  }
   // the order of logits as whole numbers
   static __device__ __forceinline__ unsigned key(float z) {
     const unsigned u = __float_as_uint(z + 0.f);
@@ -49,7 +56,12 @@ struct RowVec<float> {
 #pragma unroll
     for (int e = 0; e < 4; ++e) f[e] = __uint_as_float(v[e]);
   }
-  static __device__ __forceinline__ float one(const float* p) { return *p; }
+  static __device__ __forceinline__ float nth(const u32x4& v, int e) { return __uint_as_float(e & 2 ? (e & 1 ? v[3] : v[2]) : e & 1 ? v[1] : v[0]); }
+  static __device__ __forceinline__ u32x4 nothing() { return u32x4{0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u}; }
+  static __device__ __forceinline__ void put(u32x4& v, unsigned at, float x) {
+#pragma unroll
+    for (unsigned i = 0; i < 4; ++i) v[i] = at == i ? __float_as_uint(x) : v[i];
+  }
   static __device__ __forceinline__ unsigned key(float z) {
     const unsigned u = __float_as_uint(z + 0.f);
     return (int)u < 0 ? ~u : u | 0x80000000u;
@@ -57,10 +69,12 @@ struct RowVec<float> {
   static __device__ __forceinline__ float value(unsigned key) { return __uint_as_float((int)key < 0 ? key & 0x7fffffffu : ~key); }
 };
 
-// rint(2^40 2^y), y <= 0: 2^f on [-1/2, 1/2] as 1 + f q(f), q through the Chebyshev nodes, off by 2^-50 of itself; 2^0 is 1
-__device__ __forceinline__ double weight_of(double y) {
-  y = fmax(y, -64.0);
-  const double n = rint(y), f = y - n;
+// rint(2^40 2^(d c)), d <= 0: 2^f on [-1/2, 1/2] as 1 + f q(f), q through the Chebyshev nodes, off by 2^-50 of itself; d = 0 gives 2^40.
+// Rounding to whole numbers is done by adding and subtracting 1.5 2^52 and 2^52, and the power of two goes into the exponent's bits: 64-bit
+// additions and products run at the rate of 32-bit ones.
+__device__ __forceinline__ double weight_of(double d, double c) {
+  constexpr double WHOLE = 0x1.8p52, POSITIVE = 0x1p52;
+  const double y = fmax(fma(d, c, 40.0), -24.0), t = y + WHOLE, f = y - (t - WHOLE);
   double q = 0x1.e5e9f548e5726p-28;
   q = fma(q, f, 0x1.b6571de2f2351p-24);
   q = fma(q, f, 0x1.62bfe46117445p-20);
@@ -71,231 +85,363 @@ __device__ __forceinline__ double weight_of(double y) {
   q = fma(q, f, 0x1.c6b08d7044119p-5);
   q = fma(q, f, 0x1.ebfbdff82c590p-3);
   q = fma(q, f, 0x1.62e42fefa39f7p-1);
-  return rint(ldexp(fma(q, f, 1.0), (int)n + 40));
+  q = fma(q, f, 1.0);
+  const double w = __hiloint2double(__double2hiint(q) + (__double2loint(t) << 20), __double2loint(q));
+  return (w + POSITIVE) - POSITIVE;
 }
 
-__device__ __forceinline__ u64 wave_sum_u64(u64 v) {
-#pragma unroll
-  for (int m = 1; m < 64; m *= 2) v += (u64)__shfl_xor((long long)v, m, 64);
+// 64-bit sums over a wavefront by data-parallel-primitive moves (six reads through the LDS crossbar, twice over, take 700 cycles)
+template <int CTRL, int ROW_MASK>
+__device__ __forceinline__ u64 dpp_u64(u64 v) {
+  const int lo = __builtin_amdgcn_update_dpp(0, (int)(unsigned)v, CTRL, ROW_MASK, 0xf, false);
+  const int hi = __builtin_amdgcn_update_dpp(0, (int)(unsigned)(v >> 32), CTRL, ROW_MASK, 0xf, false);
+  return (u64)(unsigned)hi << 32 | (unsigned)lo;
+}
+__device__ __forceinline__ u64 row_scan_u64(u64 v) {      // inclusive, of each 16 lanes
+  v += dpp_u64<0x111, 0xf>(v);    // row_shr 1, 2, 4, 8
+  v += dpp_u64<0x112, 0xf>(v);
+  v += dpp_u64<0x114, 0xf>(v);
+  v += dpp_u64<0x118, 0xf>(v);
   return v;
 }
 __device__ __forceinline__ u64 wave_scan_u64(u64 v) {      // inclusive
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int m = 1; m < 64; m *= 2) {
-    const u64 o = (u64)__shfl_up((long long)v, m, 64);
-    if (lane >= m) v += o;
-  }
+  v = row_scan_u64(v);
+  v += dpp_u64<0x142, 0xa>(v);    // row_bcast:15 into rows 1 and 3
+  v += dpp_u64<0x143, 0xc>(v);    // row_bcast:31 into rows 2 and 3
   return v;
 }
+__device__ __forceinline__ u64 read_lane_u64(u64 v, int lane) {
+  return (u64)(unsigned)__builtin_amdgcn_readlane((int)(unsigned)(v >> 32), lane) << 32 | (unsigned)__builtin_amdgcn_readlane((int)(unsigned)v, lane);
+}
+__device__ __forceinline__ u64 wave_sum_u64(u64 v) { return read_lane_u64(wave_scan_u64(v), 63); }
 
-template <int THREADS>
-struct SampleShared {
+struct Bins {
   u64 mass[BINS];
-  u64 total[THREADS / 64];
-  u64 found_before;
   unsigned count[BINS];
-  unsigned lo[THREADS / 64], hi[THREADS / 64];
-  float top[THREADS / 64];
-  unsigned found, found_in;
+};
+
+// What stays of a row: the tokens of a logit above `logit`, and of its own the first `ties`, which weigh `weight` each.
+struct Border {
+  float logit;
+  unsigned ties;
+  u64 weight;
+};
+// Where a sum over columns in rising order first exceeds `target`, if of the ties only the first `ties` count.
+struct Search {
+  u64 target;
+  unsigned ties;
+};
+
+// What a workgroup's wavefronts tell each other.
+struct SampleShared {
+  u64 total[16], before;
+  unsigned number[16];
+  Search left;
+  int run;
+  float top[16];
+  unsigned found, token;
+  float logit;
   int bad;
 };
-
-// The tokens that stay: those of a key above `key`, and of `key` itself those with an index up to `last`.
-struct Border {
-  unsigned key;
-  unsigned last;
-  __device__ __forceinline__ bool stays(unsigned k, unsigned index) const { return k > key || (k == key && index <= last); }
-};
-
+// A row and how a workgroup goes over it: a wavefront has a run of tiles of 64 vectors, so that its sums are those of a run of columns.
 template <typename T, int THREADS>
 struct Sampler {
-  static constexpr int N = RowVec<T>::N, WAVES = THREADS / 64, BATCH = 4, TILE = 64 * N;
+  static constexpr int N = RowVec<T>::N, WAVES = THREADS / 64, TILE = 64 * N;
+  // vectors under way: where a logit is a few operations, and where it is a weight
+  static constexpr int LIGHT = THREADS == 1024 ? 8 : 4, HEAVY = 16 / N;
   typedef RowVec<T> R;
   const T* row;
-  unsigned cols, skip;
-  unsigned begin, end;      // tiles of this wavefront
-  SampleShared<THREADS>& sh;
+  unsigned cols, skip, tiles, per;
+  SampleShared& sh;
   int lane, wave;
-  float m, s;               // largest logit; bins per logit
+  float m;                  // the largest logit
   double c;                 // log2 e / temperature
 
-  __device__ __forceinline__ Sampler(SampleShared<THREADS>& shared) : sh(shared) {}
-
-  __device__ __forceinline__ void read(unsigned tile, float* z) const {
-    const unsigned at = tile * TILE + lane * N;      // column + skip
-    if (at >= skip && at + N <= cols + skip) {
-      R::unpack(*(const u32x4*)(row + at - skip), z);
+  __device__ __forceinline__ Sampler(SampleShared& shared, const SampleArgs& a) : sh(shared) {
+    row = (const T*)a.logits + (size_t)blockIdx.x * a.ld;
+    cols = a.cols;
+    skip = (unsigned)((uintptr_t)row % 16 / sizeof(T));
+    tiles = (cols + skip + TILE - 1) / TILE;
+    per = (tiles + WAVES - 1) / WAVES;
+    lane = threadIdx.x & 63;
+    wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  }
+  // the vectors of the tiles t .. t + B - 1, of those before `end`; columns outside the row are -inf.  All loads are under way at once; where the
+  // row begins or ends within a tile, its vectors that the row fills only in part are seen to afterwards.
+  template <int B>
+  __device__ __forceinline__ void read(u32x4 (&v)[B], unsigned t, unsigned end) const {
+    const unsigned past = min(t + B, end);
+    // (with 80 registers the second way serves both: 4096 x 32000 in 167 us instead of 184)
+    if (THREADS != 512 && (t || !skip) && past * TILE <= cols + skip) {
+      const T* from = row + (size_t)t * TILE - skip;
+#pragma unroll
+      for (int b = 0; b < B; ++b)
+        if (t + b < past) v[b] = ((const u32x4*)from)[b * 64 + lane];
       return;
     }
 #pragma unroll
-    for (int e = 0; e < N; ++e) z[e] = at + e >= skip && at + e < cols + skip ? R::one(row + at + e - skip) : -INFINITY;
+    for (int b = 0; b < B; ++b) {
+      const unsigned at = (t + b) * TILE + lane * N;      // column + skip
+      v[b] = R::nothing();
+      if (t + b < past && at >= skip && at + N <= cols + skip) v[b] = *(const u32x4*)(row + at - skip);
+    }
+#pragma unroll
+    for (int b = 0; b < B; ++b) {
+      const unsigned at = (t + b) * TILE + lane * N, to = min(at + N, cols + skip);
+      if (t + b < past && (at < skip || at + N > cols + skip))
+#pragma unroll 1
+        for (unsigned i = max(at, skip); i < to; ++i) R::put(v[b], i - at, row[i - skip]);
+    }
   }
-  // f(z, column of the first) for the tiles of this wavefront, in order
-  template <class F>
+  // f(vector, tile) for the tiles of this wavefront, BATCH of them under way
+  template <int BATCH, class F>
+  __device__ __forceinline__ void each_vector(F f) const {
+    const unsigned begin = min(wave * per, tiles), end = min(begin + per, tiles);
+    for (unsigned t = begin; t < end; t += BATCH) {
+      u32x4 v[BATCH];
+      read(v, t, end);
+#pragma unroll
+      for (int b = 0; b < BATCH; ++b)
+        if (t + b < end) f(v[b], t + b);
+    }
+  }
+  template <int BATCH = HEAVY, class F>
   __device__ __forceinline__ void each(F f) const {
-    unsigned t = begin;
-    for (; t + BATCH <= end; t += BATCH) {
-      float z[BATCH][N];
-#pragma unroll
-      for (int b = 0; b < BATCH; ++b) read(t + b, z[b]);
-#pragma unroll
-      for (int b = 0; b < BATCH; ++b) f(z[b], (t + b) * TILE + lane * N - skip);
-    }
-    for (; t < end; ++t) {
+    each_vector<BATCH>([&](const u32x4& v, unsigned) {
       float z[N];
-      read(t, z);
-      f(z, t * TILE + lane * N - skip);
-    }
+      R::unpack(v, z);
+#pragma unroll
+      for (int e = 0; e < N; ++e) f(z[e]);
+    });
   }
-  __device__ __forceinline__ int bin(float z) const { return (int)fminf((m - z) * s, (float)LAST); }
-  __device__ __forceinline__ double weight(float z) const { return weight_of(((double)z - (double)m) * c); }
+  __device__ __forceinline__ double weight(float z) const { return weight_of((double)z - (double)m, c); }
 
+  // sums over the wavefronts, which are in sh.total: those before this one, and all
+  __device__ __forceinline__ u64 totals(u64& all) const {
+    const u64 v = row_scan_u64(lane < WAVES ? sh.total[lane] : 0);
+    all = read_lane_u64(v, 15);
+    return wave ? read_lane_u64(v, wave - 1) : 0;
+  }
   __device__ __forceinline__ u64 block_sum(u64 v) const {
     v = wave_sum_u64(v);
     __syncthreads();
     if (lane == 0) sh.total[wave] = v;
     __syncthreads();
-    u64 all = 0;
-    for (int w = 0; w < WAVES; ++w) all += sh.total[w];
+    u64 all;
+    totals(all);
     return all;
   }
-  __device__ __forceinline__ void clear_bins() const {
+  // what the threads before this one have in all
+  __device__ __forceinline__ u64 block_before(u64 v, u64& all) const {
+    const u64 upto = wave_scan_u64(v);
     __syncthreads();
-    for (int i = threadIdx.x; i < BINS; i += THREADS) { sh.mass[i] = 0; sh.count[i] = 0; }
+    if (lane == 63) sh.total[wave] = upto;
+    __syncthreads();
+    return totals(all) + upto - v;
+  }
+
+  // Of the lanes (of the first 16, or all), which hold sums of consecutive runs of columns (the ties' number apart), the one in which the
+  // search ends, and what is left to search there; -1 and what is left behind them all if it is none.
+  template <bool ROW>
+  __device__ __forceinline__ int pick(Search& s, u64 sum, unsigned number, u64 tie_weight) const {
+    const unsigned upto = (unsigned)(ROW ? row_scan_u64(number) : wave_scan_u64(number)), before = upto - number;
+    const u64 own = sum + tie_weight * min(number, s.ties > before ? s.ties - before : 0), all = ROW ? row_scan_u64(own) : wave_scan_u64(own);
+    const u64 past = __ballot(all > s.target && (!ROW || lane < 16));
+    const int k = past ? __ffsll((unsigned long long)past) - 1 : ROW ? 15 : 63;
+    const unsigned ties = (unsigned)__builtin_amdgcn_readlane((int)(past ? before : upto), k);
+    s.target -= read_lane_u64(past ? all - own : all, k);
+    s.ties -= min(s.ties, ties);
+    return past ? k : -1;
+  }
+  // This thread's sum over its columns without ties, and their number: left for all wavefronts to see.
+  __device__ __forceinline__ void leave(u64 sum, unsigned number) const {
+    sum = wave_sum_u64(sum);
+    const unsigned n = (unsigned)wave_sum_u64(number);
+    __syncthreads();
+    if (lane == 0) { sh.total[wave] = sum; sh.number[wave] = n; }
+    __syncthreads();
+  }
+  // the first wavefront's pick among all wavefronts' sums
+  __device__ __forceinline__ int pick_wave(Search& s, u64 tie_weight) const {
+    if (wave == 0) {
+      const int k = pick<true>(s, lane < WAVES ? sh.total[lane] : 0, lane < WAVES ? sh.number[lane] : 0, tie_weight);
+      if (lane == 0) { sh.run = k; sh.left = s; }
+    }
+    __syncthreads();
+    s = sh.left;
+    return sh.run;
+  }
+  // The search's end, in sh.token and sh.logit: among the wavefronts' runs, as `leave` left them, then among the run's tiles, a wavefront
+  // each, and among its lanes.  f(logit, weight): whether it is a tie; its weight otherwise.
+  template <class F>
+  __device__ __forceinline__ void search(Search s, u64 tie_weight, F f) const {
+    const unsigned begin = min((unsigned)max(pick_wave(s, tie_weight), 0) * per, tiles), end = min(begin + per, tiles);
+    for (unsigned t = begin; t < end; t += WAVES) {
+      float z[N];
+      u64 own[N], sum = 0;
+      unsigned is = 0;
+      if (t + wave < end) {
+        u32x4 v[1];
+        read(v, t + wave, end);
+        R::unpack(v[0], z);
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+          own[e] = 0;
+          if (f(z[e], own[e])) is |= 1u << e;
+          else sum += own[e];
+        }
+        // 512 logits weigh 2^49 at most: their ties are counted above that, in the same sum
+        const u64 both = wave_sum_u64(sum + ((u64)__popc(is) << 50));
+        if (lane == 0) { sh.total[wave] = both & ((1ull << 50) - 1); sh.number[wave] = (unsigned)(both >> 50); }
+      } else if (lane == 0) {
+        sh.total[wave] = 0;
+        sh.number[wave] = 0;
+      }
+      __syncthreads();
+      const int tile = pick_wave(s, tie_weight);
+      if (tile < 0) continue;
+      if (tile == wave) {
+        const int k = pick<false>(s, sum, __popc(is), tie_weight);
+        if (lane == k) {
+          u64 upto = 0;
+          unsigned ties = s.ties;
+          int at = -1;
+#pragma unroll
+          for (int e = 0; e < N; ++e) {
+            const bool tie = is >> e & 1;
+            upto += tie ? (ties ? tie_weight : 0) : own[e];
+            if (tie && ties) --ties;
+            if (at < 0 && upto > s.target) { at = e; sh.logit = z[e]; }
+          }
+          sh.token = (t + wave) * TILE + lane * N - skip + max(at, 0);
+        }
+      }
+      break;
+    }
+    __syncthreads();
+  }
+
+  // the largest logit, and this thread's; false if the row has no answer
+  __device__ __forceinline__ bool largest(float& own) {
+    own = -INFINITY;
+    bool bad = false;
+    each<LIGHT>([&](float z) {
+      own = fmaxf(own, z);
+      bad |= !(z < INFINITY);
+    });
+    m = wave_max(own);
+    __syncthreads();
+    if (threadIdx.x == 0) sh.bad = 0;
+    __syncthreads();
+    if (lane == 0) sh.top[wave] = m;
+    if (bad) sh.bad = 1;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) m = fmaxf(m, sh.top[w]);
+    return !sh.bad && m > -INFINITY;
+  }
+};
+
+__device__ __forceinline__ u64 top_p_need(float top_p, u64 all) { return max((u64)ceil((double)top_p * (double)all), (u64)1); }
+__device__ __forceinline__ u64 draw_target(float uniform, u64 all) {
+  const double u = uniform;
+  return min((u64)floor((u > 0.0 ? fmin(u, 1.0) : 0.0) * (double)all), all - 1);
+}
+__device__ __forceinline__ void answer(const SampleArgs& a, int token, float logprob, int kept) {
+  if (threadIdx.x) return;
+  if (a.token) a.token[blockIdx.x] = token;
+  if (a.logprob) a.logprob[blockIdx.x] = logprob;
+  if (a.kept) a.kept[blockIdx.x] = kept;
+}
+__device__ __forceinline__ void no_answer(const SampleArgs& a) { answer(a, -1, __uint_as_float(0x7fc00000u), 0); }
+template <class S>
+__device__ __forceinline__ void drawn_answer(const SampleArgs& a, const S& p, float temperature, u64 all, unsigned kept) {
+  if (threadIdx.x) return;
+  answer(a, (int)p.sh.token, (float)(((double)p.sh.logit - (double)p.m) / (double)temperature - log((double)all / ONE)), (int)kept);
+}
+
+// ------------------------------------------------------------------------------------- by bins of the logits
+// The row is counted and weighed into 2048 bins of equal width in (m - z) / T; the bin that a border falls into is cut again by the bits of
+// its logits, until a bin is a single value.
+template <typename T, int THREADS>
+struct BinSampler : Sampler<T, THREADS> {
+  typedef Sampler<T, THREADS> S;
+  typedef RowVec<T> R;
+  Bins &coarse, &fine;
+  float s;                  // bins per logit
+  __device__ __forceinline__ BinSampler(const S& base, Bins* b) : S(base), coarse(b[0]), fine(b[1]) {}
+  __device__ __forceinline__ int bin(float z) const { return (int)fminf((this->m - z) * s, (float)LAST); }
+
+  __device__ __forceinline__ void clear(Bins& b) const {
+    __syncthreads();
+    for (int i = threadIdx.x; i < BINS; i += THREADS) { b.mass[i] = 0; b.count[i] = 0; }
     __syncthreads();
   }
   // The first bin up to which there are `need` (at least 1) in all, and what lies before it: true if there is one.
-  __device__ __forceinline__ bool find(bool by_mass, u64 need, unsigned& which, u64& before) const {
+  __device__ __forceinline__ bool find(const Bins& b, bool by_mass, u64 need, unsigned& which, u64& before) const {
     constexpr int PER = BINS / THREADS;
     u64 own[PER], sum = 0;
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      own[i] = by_mass ? sh.mass[threadIdx.x * PER + i] : sh.count[threadIdx.x * PER + i];
+      own[i] = by_mass ? b.mass[threadIdx.x * PER + i] : b.count[threadIdx.x * PER + i];
       sum += own[i];
     }
-    const u64 upto = wave_scan_u64(sum);
-    if (lane == 63) sh.total[wave] = upto;
-    if (threadIdx.x == 0) sh.found = BINS;
-    __syncthreads();
-    u64 at = upto - sum;
-    for (int w = 0; w < wave; ++w) at += sh.total[w];
+    if (threadIdx.x == 0) this->sh.found = BINS;
+    u64 all, at = this->block_before(sum, all);
     if (at < need && at + sum >= need) {
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
-        if (at < need && at + own[i] >= need) { sh.found = threadIdx.x * PER + i; sh.found_before = at; }
+        if (at < need && at + own[i] >= need) { this->sh.found = threadIdx.x * PER + i; this->sh.before = at; }
         at += own[i];
       }
     }
     __syncthreads();
-    which = sh.found;
-    before = sh.found_before;
+    which = this->sh.found;
+    before = this->sh.before;
     return which < BINS;
   }
-
-  // The column at which sum over columns of f (whole numbers) first exceeds `target`
-  template <class F>
-  __device__ __forceinline__ unsigned locate(F f, u64 target) const {
-    u64 mine = 0;
-    each([&](const float* z, unsigned col) {
-#pragma unroll
-      for (int e = 0; e < N; ++e) mine += f(z[e], col + e);
-    });
-    mine = wave_sum_u64(mine);
-    __syncthreads();
-    if (lane == 0) sh.total[wave] = mine;
-    __syncthreads();
-    return walk(f, target);
-  }
-  // ... where the sums of the wavefronts are in sh.total already
-  template <class F>
-  __device__ __forceinline__ unsigned walk(F f, u64 target) const {
-    u64 at = 0;
-    for (int w = 0; w < wave; ++w) at += sh.total[w];
-    if (at <= target && target < at + sh.total[wave]) {
-      for (unsigned t = begin; t < end; ++t) {
-        float z[N];
-        read(t, z);
-        const unsigned col = t * TILE + lane * N - skip;
-        u64 own[N], sum = 0;
-#pragma unroll
-        for (int e = 0; e < N; ++e) { own[e] = f(z[e], col + e); sum += own[e]; }
-        const u64 upto = wave_scan_u64(sum);
-        const u64 all = (u64)__shfl((long long)upto, 63, 64);
-        if (target < at + all) {
-          u64 to = at + upto - sum;
-          if (to <= target && target < to + sum) {
-#pragma unroll
-            for (int e = 0; e < N; ++e) {
-              if (to <= target && target < to + own[e]) sh.found_in = col + e;
-              to += own[e];
-            }
-          }
-          break;
-        }
-        at += all;
-      }
-    }
-    __syncthreads();
-    const unsigned r = sh.found_in;
-    __syncthreads();
-    return r;
+  // what the bins before `which` weigh
+  __device__ __forceinline__ u64 mass_before(const Bins& b, unsigned which) const {
+    u64 v = 0;
+    for (unsigned i = threadIdx.x; i < which; i += THREADS) v += b.mass[i];
+    return this->block_sum(v);
   }
 
-  // The border behind the token at which count (or mass) reaches `need`; `in` says which tokens count.  The bins of the row are in place.
-  template <class In>
-  __device__ __forceinline__ bool border(bool by_mass, u64 need, In in, Border& out) const {
+  // The border behind the token at which count (or mass) reaches `need`, and what stays up to it weighs (0 without `weigh`): false if all that
+  // weighs anything stays.
+  __device__ __forceinline__ bool border(bool by_mass, bool weigh, u64 need, Border& out, u64& stays) const {
     unsigned b;
     u64 before;
-    if (!find(by_mass, need, b, before) || b == LAST) return false;
+    if (!find(coarse, by_mass, need, b, before) || b == LAST) return false;
+    stays = weigh ? (by_mass ? before : mass_before(coarse, b)) : 0;
     need -= before;
-    // the keys of the bin
-    unsigned lo = 0xffffffffu, hi = 0;
-    each([&](const float* z, unsigned col) {
-#pragma unroll
-      for (int e = 0; e < N; ++e)
-        if (bin(z[e]) == (int)b && in(z[e], col + e)) {
-          const unsigned k = R::key(z[e]);
-          lo = min(lo, k);
-          hi = max(hi, k);
-        }
-    });
-    for (int x = 1; x < 64; x *= 2) {
-      lo = min(lo, (unsigned)__shfl_xor((int)lo, x, 64));
-      hi = max(hi, (unsigned)__shfl_xor((int)hi, x, 64));
-    }
-    __syncthreads();
-    if (lane == 0) { sh.lo[wave] = lo; sh.hi[wave] = hi; }
-    __syncthreads();
-    for (int w = 0; w < WAVES; ++w) { lo = min(lo, sh.lo[w]); hi = max(hi, sh.hi[w]); }
+    // the keys of the bin, and some beside them: roundings move a logit by less than `slack`
+    const float near = (float)b / s, far = (float)(b + 1) / s, slack = (fabsf(this->m) + far) * 0x1p-20f;
+    unsigned hi = R::key(fminf(this->m - near + slack, this->m)), lo = R::key(fmaxf(this->m - far - slack, -3.4028234e38f));
     for (;;) {
       const unsigned range = hi - lo, shift = range < BINS ? 0 : 32 - __clz(range) - 11;
-      clear_bins();
-      each([&](const float* z, unsigned col) {
-#pragma unroll
-        for (int e = 0; e < N; ++e)
-          if (bin(z[e]) == (int)b && in(z[e], col + e)) {
-            const unsigned k = R::key(z[e]);
-            if (k >= lo && k <= hi) {
-              const unsigned at = (hi - k) >> shift;
-              atomicAdd(&sh.count[at], 1u);
-              if (by_mass) atomicAdd(&sh.mass[at], (u64)weight(z[e]));
-            }
-          }
+      clear(fine);
+      this->each([&](float z) {
+        const unsigned k = R::key(z);
+        if (k >= lo && k <= hi && bin(z) == (int)b) {
+          const unsigned at = (hi - k) >> shift;
+          atomicAdd(&fine.count[at], 1u);
+          if (weigh) atomicAdd(&fine.mass[at], (u64)this->weight(z));
+        }
       });
       unsigned at;
-      if (!find(by_mass, need, at, before)) return false;      // (cannot be)
+      if (!find(fine, by_mass, need, at, before)) return false;      // (cannot be)
       need -= before;
+      if (weigh) stays += by_mass ? before : mass_before(fine, at);
       const unsigned top = hi - (at << shift);
       if (!shift) {
-        out.key = top;
         // `need` of the bin's tokens, which weigh the same
-        const unsigned all = sh.count[at];
-        const u64 each_one = by_mass ? sh.mass[at] / all : 1, some = (need + each_one - 1) / each_one;
+        out.logit = R::value(top);
+        out.weight = (u64)this->weight(out.logit);
+        out.ties = (unsigned)(by_mass ? (need + out.weight - 1) / out.weight : need);
+        stays += out.ties * out.weight;
         __syncthreads();
-        out.last = 0xffffffffu;
-        if (some < all) out.last = locate([&](float z, unsigned col) { return (u64)(R::key(z) == top && in(z, col)); }, some - 1);
         return true;
       }
       hi = top;
@@ -305,122 +451,534 @@ struct Sampler {
 };
 
 template <typename T, int THREADS>
-__global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
-  __shared__ SampleShared<THREADS> sh;
-  typedef Sampler<T, THREADS> S;
-  typedef RowVec<T> R;
-  S p(sh);
-  const size_t r = blockIdx.x;
-  p.row = (const T*)a.logits + r * a.ld;
-  p.cols = a.cols;
-  p.skip = (unsigned)((uintptr_t)p.row % 16 / sizeof(T));
-  p.lane = threadIdx.x & 63;
-  p.wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const unsigned tiles = (p.cols + p.skip + S::TILE - 1) / S::TILE, per = (tiles + S::WAVES - 1) / S::WAVES;
-  p.begin = min(p.wave * per, tiles);
-  p.end = min(p.begin + per, tiles);
-  const karma_sample_rule rule = a.rules[a.n_rules == 1 ? 0 : r];
-
-  // the largest logit, and whether the row has an answer
-  float m = -INFINITY;
-  bool bad = false;
-  p.each([&](const float* z, unsigned) {
-#pragma unroll
-    for (int e = 0; e < S::N; ++e) {
-      m = fmaxf(m, z[e]);
-      bad |= !(z[e] < INFINITY);
-    }
-  });
-  m = wave_max(m);
-  if (threadIdx.x == 0) sh.bad = 0;
-  __syncthreads();
-  if (p.lane == 0) sh.top[p.wave] = m;
-  if (bad) sh.bad = 1;
-  __syncthreads();
-  for (int w = 0; w < S::WAVES; ++w) m = fmaxf(m, sh.top[w]);
-  bad = sh.bad || m == -INFINITY || !(rule.temperature >= 0.f && rule.temperature < INFINITY) || rule.top_p != rule.top_p || rule.min_p != rule.min_p;
-  if (bad) {
-    if (threadIdx.x == 0) {
-      if (a.token) a.token[r] = -1;
-      if (a.logprob) a.logprob[r] = __uint_as_float(0x7fc00000u);
-      if (a.kept) a.kept[r] = 0;
-    }
-    return;
-  }
-  p.m = m;
-  if (rule.temperature == 0.f || rule.top_k == 1 || rule.top_p <= 0.f) {
-    const unsigned token = p.locate([&](float z, unsigned) { return (u64)(z == m); }, 0);
-    if (threadIdx.x == 0) {
-      if (a.token) a.token[r] = (int)token;
-      if (a.logprob) a.logprob[r] = 0.f;
-      if (a.kept) a.kept[r] = 1;
-    }
-    return;
-  }
-  p.c = 1.4426950408889634074 / (double)rule.temperature;
+__device__ __forceinline__ void sample_by_bins(const SampleArgs& a, const karma_sample_rule& rule, float uniform, double least, const Sampler<T, THREADS>& base,
+                                               Bins* bins) {
+  BinSampler<T, THREADS> p(base, bins);
+  float own;
+  if (!p.largest(own)) return no_answer(a);
   p.s = fminf((float)LAST / (REACH * rule.temperature), 1e30f);
-
-  Border border{0, 0xffffffffu};
-  if (rule.top_k && rule.top_k < a.cols) {
-    p.clear_bins();
-    p.each([&](const float* z, unsigned) {
-#pragma unroll
-      for (int e = 0; e < S::N; ++e) {
-        const int b = p.bin(z[e]);
-        if (b < LAST) atomicAdd(&sh.count[b], 1u);
-      }
-    });
-    // (none where all tokens that weigh anything stay)
-    p.border(false, rule.top_k, [&](float, unsigned) { return true; }, border);
-  }
-  if (rule.top_p < 1.f) {
-    p.clear_bins();
-    const Border k = border;
+  const bool by_count = rule.top_k && rule.top_k < a.cols, by_mass = rule.top_p < 1.f;
+  Border border{-INFINITY, 0, 0};
+  if (by_count || by_mass) {
+    p.clear(p.coarse);
     double mine = 0.0;
-    p.each([&](const float* z, unsigned col) {
-#pragma unroll
-      for (int e = 0; e < S::N; ++e) {
-        const int b = p.bin(z[e]);
-        if (b < LAST && k.stays(R::key(z[e]), col + e)) {
-          const double w = p.weight(z[e]);
+    p.each([&](float z) {
+      const int b = p.bin(z);
+      if (b < LAST) {
+        if (by_count) atomicAdd(&p.coarse.count[b], 1u);
+        if (by_mass) {
+          const double w = p.weight(z);
           mine += w;
-          atomicAdd(&sh.mass[b], (u64)w);
+          atomicAdd(&p.coarse.mass[b], (u64)w);
         }
       }
     });
-    const u64 all = p.block_sum((u64)mine);
-    const u64 need = max((u64)ceil((double)rule.top_p * (double)all), (u64)1);
-    p.border(true, need, [&](float z, unsigned col) { return k.stays(R::key(z), col); }, border);
-    if (border.key == k.key) border.last = min(border.last, k.last);
+    u64 all = by_mass ? p.block_sum((u64)mine) : 0, stays;
+    if (by_count && p.border(false, by_mass, rule.top_k, border, stays)) all = stays;
+    if (by_mass) p.border(true, true, top_p_need(rule.top_p, all), border, stays);
   }
-  const double least = rule.min_p > 0.f ? fmin((double)rule.min_p, 1.0) * ONE : 0.0;
-  auto drawn = [&](float z, unsigned col) {
-    if (!border.stays(R::key(z), col)) return (u64)0;
-    const double w = p.weight(z);
-    return w >= least ? (u64)w : 0;
+  // (the border's weight may be below min-p's: then none of its tokens stays)
+  if ((double)border.weight < least) border.ties = 0;
+  auto drawn = [&](float z, u64& w) {
+    if (z == border.logit) return true;
+    if (z > border.logit) {
+      const double v = p.weight(z);
+      w = v >= least ? (u64)v : 0;
+    }
+    return false;
   };
-  u64 mine = 0;
-  unsigned count = 0;
-  p.each([&](const float* z, unsigned col) {
-#pragma unroll
-    for (int e = 0; e < S::N; ++e) {
-      const u64 w = drawn(z[e], col + e);
+  double mine = 0.0;
+  unsigned count = 0, ties = 0;
+  if (border.logit == -INFINITY && least <= 0.0) {      // all stays
+    p.each([&](float z) {
+      const double w = p.weight(z);
       mine += w;
-      count += w != 0;
+      count += w > 0.0;
+    });
+  } else {
+    p.each([&](float z) {
+      if (z > border.logit) {
+        const double w = p.weight(z);
+        if (w >= least) { mine += w; count += w > 0.0; }
+      }
+      ties += z == border.logit;
+    });
+  }
+  unsigned kept = (unsigned)p.block_sum(count) + (border.weight ? border.ties : 0);
+  p.leave((u64)mine, ties);
+  u64 all;
+  p.totals(all);
+  all += border.ties * border.weight;
+  p.search(Search{draw_target(uniform, all), border.ties}, border.weight, drawn);
+  drawn_answer(a, p, rule.temperature, all, kept);
+}
+
+// ------------------------------------------------------------------------------------- by a list of the likeliest tokens
+// With a small top_k: there are at least top_k logits from the threads' top_k-th largest maximum on.  Those, few more than top_k, are put
+// into a list, and all else is sums over pairs of its tokens.  (1 x 128000 in fp32 with top_k 50 and top_p 0.9: 17 us, by bins 106.)
+constexpr unsigned LIST_MOST = 256, LIST_TOP_K = 128;
+struct List {
+  float logit[LIST_MOST];
+  unsigned column[LIST_MOST], rank[LIST_MOST];
+  u64 weight[LIST_MOST], before[LIST_MOST], drawn_before[LIST_MOST];
+  unsigned count[BINS], n;
+  float floor[16];
+};
+// false: the row has to go another way
+template <typename T, int THREADS>
+__device__ __forceinline__ bool sample_by_list(const SampleArgs& a, const karma_sample_rule& rule, float uniform, double least, Sampler<T, THREADS>& p, List& l) {
+  constexpr int N = RowVec<T>::N, WAVES = THREADS / 64;
+  const int tid = threadIdx.x;
+  for (int i = tid; i < BINS; i += THREADS) l.count[i] = 0;
+  if (tid == 0) { l.n = 0; p.sh.found = BINS; }
+  float own;
+  if (!p.largest(own)) {
+    no_answer(a);
+    return true;
+  }
+  // the bin of the top_k-th largest of the threads' maxima, and the smallest maximum that is not behind it
+  const float s = fminf((float)LAST / (REACH * rule.temperature), 1e30f);
+  const int bin = (int)fminf((p.m - own) * s, (float)LAST);
+  if (bin < LAST) atomicAdd(&l.count[bin], 1u);
+  __syncthreads();
+  constexpr int PER = BINS / THREADS;
+  unsigned upto = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) upto += l.count[tid * PER + i];
+  u64 all, at = p.block_before(upto, all);
+  if (at < rule.top_k && at + upto >= rule.top_k) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const unsigned n = l.count[tid * PER + i];
+      if (at < rule.top_k && at + n >= rule.top_k) p.sh.found = tid * PER + i;
+      at += n;
+    }
+  }
+  __syncthreads();
+  if (p.sh.found == BINS) return false;
+  float floor = -wave_max(bin <= (int)p.sh.found ? -own : -INFINITY);
+  if (p.lane == 0) l.floor[p.wave] = floor;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) floor = fminf(floor, l.floor[w]);
+  p.template each_vector<Sampler<T, THREADS>::LIGHT>([&](const u32x4& v, unsigned tile) {
+    float z[N];
+    RowVec<T>::unpack(v, z);
+    float most = z[0];
+#pragma unroll
+    for (int e = 1; e < N; ++e) most = fmaxf(most, z[e]);
+    if (most < floor) return;
+    unsigned in = 0;
+#pragma unroll
+    for (int e = 0; e < N; ++e) in |= z[e] >= floor ? 1u << e : 0;
+    for (; in; in &= in - 1) {
+      const int e = __ffs((int)in) - 1;
+      const unsigned i = atomicAdd(&l.n, 1u);
+      if (i < LIST_MOST) { l.logit[i] = RowVec<T>::nth(v, e); l.column[i] = tile * (64 * N) + p.lane * N - p.skip + e; }
     }
   });
-  const u64 kept = p.block_sum(count), all = p.block_sum(mine);      // (sh.total holds the wavefronts' shares of `all`)
-  const double u = a.uniform[r];
-  const u64 target = min((u64)floor((u > 0.0 ? fmin(u, 1.0) : 0.0) * (double)all), all - 1);
-  const unsigned token = p.walk(drawn, target);
-  if (threadIdx.x == 0) {
-    if (a.token) a.token[r] = (int)token;
-    if (a.kept) a.kept[r] = (int)kept;
-    if (a.logprob) {
-      const float z = R::one(p.row + token);
-      a.logprob[r] = (float)(((double)z - (double)m) / (double)rule.temperature - log((double)all / ONE));
+  __syncthreads();
+  const unsigned n = l.n;
+  if (n > LIST_MOST) return false;
+  const bool mine = tid < (int)n;
+  const u64 weight = mine ? (u64)p.weight(l.logit[tid]) : 0;
+  if (tid < (int)LIST_MOST) { l.weight[tid] = weight; l.rank[tid] = 0; l.before[tid] = 0; l.drawn_before[tid] = 0; }
+  __syncthreads();
+  // pairs: a token of the list for every thread of a group, and the groups share the others
+  const unsigned group = n <= 64 ? 64 : n <= 128 ? 128 : 256, me = tid % group;
+  const float z = l.logit[min(me, n - 1)];
+  const unsigned column = l.column[min(me, n - 1)];
+  unsigned rank = 0;
+  u64 before = 0;
+#pragma unroll 4
+  for (unsigned j = tid / group; j < n; j += THREADS / group) {
+    const float other = l.logit[j];
+    const unsigned c = l.column[j];
+    const u64 w = l.weight[j];
+    const bool first = other > z || (other == z && c < column);
+    rank += first;
+    before += first ? w : 0;
+  }
+  if (me < n && rank) { atomicAdd(&l.rank[me], rank); atomicAdd(&l.before[me], before); }
+  __syncthreads();
+  // (a token's own thread from here on)
+  rank = mine ? l.rank[tid] : n;
+  before = mine ? l.before[tid] : 0;
+  bool stays = rank < rule.top_k;
+  if (rule.top_p < 1.f) {
+    const u64 need = top_p_need(rule.top_p, p.block_sum(stays ? weight : 0));
+    stays = stays && before < need;
+  }
+  stays = stays && weight && (double)weight >= least;
+  // 256 tokens weigh 2^48 at most: their number above that, in the same sum
+  const u64 sums = p.block_sum(stays ? weight + (1ull << 52) : 0), total = sums & ((1ull << 52) - 1), target = draw_target(uniform, total);
+  if (tid < (int)LIST_MOST) l.weight[tid] = stays ? weight : 0;
+  __syncthreads();
+  before = 0;
+#pragma unroll 4
+  for (unsigned j = tid / group; j < n; j += THREADS / group) {
+    const unsigned c = l.column[j];
+    const u64 w = l.weight[j];
+    before += c < column ? w : 0;
+  }
+  if (me < n && before) atomicAdd(&l.drawn_before[me], before);
+  __syncthreads();
+  if (stays && l.drawn_before[tid] <= target && target < l.drawn_before[tid] + weight) {
+    p.sh.token = l.column[tid];
+    p.sh.logit = l.logit[tid];
+  }
+  __syncthreads();
+  drawn_answer(a, p, rule.temperature, total, (unsigned)(sums >> 52));
+  return true;
+}
+
+// ------------------------------------------------------------------------------------- by counters of bf16 logits
+typedef short short2_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ short2_t as_short2(unsigned v) { return __builtin_bit_cast(short2_t, v); }
+__device__ __forceinline__ short2_t max2(short2_t a, short2_t b) { return __builtin_elementwise_max(a, b); }
+// From 2^-14 to 2^18 there are 4096 bf16 numbers, and as many negative ones: the row is counted by its bits, and everything but the draw itself
+// follows from the counters, with one weight for every value that occurs.  Ranks rise as logits fall: the positive ones, a group of 64 for 0
+// alone, the negative ones.  The few numbers next to 0 are kept one by one; what lies below -2^18 is left out (masked logits) where it weighs
+// nothing.  A row that has other numbers, many next to 0, or its border among those goes by bins.
+constexpr unsigned CT_LOW = 0x3880, CT_SIDE = 4096;
+constexpr unsigned ZERO_GROUP = CT_SIDE / 64, CT_GROUPS = 2 * ZERO_GROUP + 1, RANK_ZERO = CT_SIDE, RANK_NEGATIVE = CT_SIDE + 64, CT_RANKS = RANK_NEGATIVE + CT_SIDE;
+constexpr unsigned CT_TINY = 64;
+constexpr float CT_FAR = 262144.f;
+struct Counted {
+  unsigned counter[2 * CT_SIDE];      // by bits: positive, negative
+  unsigned zeros, tiny;
+  unsigned short tiny_bits[CT_TINY];
+  u64 mass[CT_GROUPS];
+  unsigned count[CT_GROUPS];
+  unsigned short list[CT_GROUPS];     // groups that have any
+  // the group that a border falls into and what lies before it; the border found, what stays up to it, and the weight of its rank
+  u64 mass_before, stays, border_weight;
+  unsigned group, count_before, border, ties, count_stays, first;
+  int other, left_out;
+
+  __device__ __forceinline__ unsigned of(unsigned rank) const {
+    return rank < CT_SIDE ? counter[CT_SIDE - 1 - rank] : rank >= RANK_NEGATIVE ? counter[rank - RANK_NEGATIVE + CT_SIDE] : rank == RANK_ZERO ? zeros : 0;
+  }
+};
+__device__ __forceinline__ float rank_value(unsigned rank) {
+  const unsigned bits = rank < CT_SIDE ? CT_LOW + CT_SIDE - 1 - rank : rank >= RANK_NEGATIVE ? 0x8000 + CT_LOW + rank - RANK_NEGATIVE : 0;
+  return __uint_as_float(bits << 16);
+}
+// (numbers that have no rank: one behind all)
+__device__ __forceinline__ unsigned rank_of(unsigned u) {
+  const unsigned i = (u & 0x7fff) - CT_LOW;
+  if (i < CT_SIDE) return u & 0x8000 ? RANK_NEGATIVE + i : CT_SIDE - 1 - i;
+  return u & 0x7fff ? CT_RANKS : RANK_ZERO;
+}
+__device__ __forceinline__ bool next_to_zero(unsigned u) { return (u & 0x7fff) - 1 < CT_LOW - 1; }
+// the room of both ways, which later holds the weights by rank
+constexpr size_t SAMPLE_ROOM = sizeof(Counted) > 2 * sizeof(Bins) ? sizeof(Counted) : 2 * sizeof(Bins);
+constexpr unsigned CT_TABLE = SAMPLE_ROOM / sizeof(double);
+
+// false: the row has to go by bins
+template <int THREADS>
+__device__ __forceinline__ bool sample_by_counters(const SampleArgs& a, const karma_sample_rule& rule, float uniform, double least, Sampler<bf16_t, THREADS>& p,
+                                                   Counted& ct) {
+  typedef Sampler<bf16_t, THREADS> S;
+  constexpr int WAVES = S::WAVES, AHEAD = THREADS == 1024 ? 8 : 4;
+  const int lane = p.lane, wave = p.wave, tid = threadIdx.x;
+  // ---- count the row; its first vectors are under way while the counters are cleared
+  u32x4 ahead[AHEAD];
+  const unsigned begin = min(wave * p.per, p.tiles), end = min(begin + p.per, p.tiles);
+  p.read(ahead, begin, end);
+  for (int i = tid; i < (int)CT_SIDE / 2; i += THREADS) ((u32x4*)ct.counter)[i] = u32x4{0, 0, 0, 0};
+  for (int i = tid; i < (int)CT_GROUPS; i += THREADS) { ct.count[i] = 0; ct.mass[i] = 0; }
+  if (tid == 0) {
+    ct.zeros = 0; ct.tiny = 0; ct.other = 0; ct.left_out = 0; ct.first = CT_GROUPS; ct.group = CT_GROUPS; ct.border = CT_RANKS - 1; ct.ties = 0xffffffffu;
+    ct.border_weight = 0;
+  }
+  __syncthreads();
+  auto for_vectors = [&](auto f) {
+#pragma unroll
+    for (int b = 0; b < AHEAD; ++b)
+      if (begin + b < end) f(ahead[b]);
+    for (unsigned t = begin + AHEAD; t < end; t += AHEAD) {
+      u32x4 v[AHEAD];
+      p.read(v, t, end);
+#pragma unroll
+      for (int b = 0; b < AHEAD; ++b)
+        if (t + b < end) f(v[b]);
+    }
+  };
+  // f for each of a vector's logits for which `is` holds, in a loop that is not unrolled: few have any
+  auto for_some = [&](const u32x4& v, auto is, auto f) {
+#pragma unroll 1
+    for (int i = 0; i < 8; ++i) {
+      const unsigned d = i & 4 ? (i & 2 ? v[3] : v[2]) : i & 2 ? v[1] : v[0], u = i & 1 ? d >> 16 : d & 0xffff;
+      if (is(u)) f(u);
+    }
+  };
+  auto has_rank = [](unsigned u) { return (u & 0x7fff) - CT_LOW < CT_SIDE; };
+  auto count = [&](const u32x4& v) {
+    bool others = false;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const unsigned u = i % 2 ? v[i / 2] >> 16 : v[i / 2] & 0xffff, at = (u & 0x7fff) - CT_LOW;
+      if (at < CT_SIDE) atomicAdd(&ct.counter[at + __umul24(u >> 15, CT_SIDE)], 1u);
+      others |= at >= CT_SIDE;
+    }
+    if (!others) return;
+    for_some(v, [&](unsigned u) { return !has_rank(u); },
+             [&](unsigned u) {
+               if (!(u & 0x7fff)) atomicAdd(&ct.zeros, 1u);
+               else if (u >= 0x8000 + CT_LOW + CT_SIDE && u <= 0xff80) { if (u != 0xff80) ct.left_out = 1; }
+               else if (next_to_zero(u)) {
+                 const unsigned i = atomicAdd(&ct.tiny, 1u);
+                 if (i < CT_TINY) ct.tiny_bits[i] = (unsigned short)u;
+                 else ct.other = 1;
+               } else ct.other = 1;
+             });
+  };
+  // 64 counters are 16 lanes' vectors
+  auto count_groups = [&]() {
+    for (int at = tid; at < (int)CT_SIDE / 2; at += THREADS) {
+      const u32x4 v = ((const u32x4*)ct.counter)[at];
+      int n = (int)((v[0] + v[1]) + (v[2] + v[3]));
+      if (!__ballot(n != 0)) continue;
+      n += __builtin_amdgcn_update_dpp(0, n, 0xB1, 0xf, 0xf, false);     // quad_perm [1,0,3,2]
+      n += __builtin_amdgcn_update_dpp(0, n, 0x4E, 0xf, 0xf, false);     // quad_perm [2,3,0,1]
+      n += __builtin_amdgcn_update_dpp(0, n, 0x141, 0xf, 0xf, false);    // row_half_mirror
+      n += __builtin_amdgcn_update_dpp(0, n, 0x140, 0xf, 0xf, false);    // row_mirror
+      const int group = at / 16;
+      if (tid % 16 == 0) ct.count[group < (int)ZERO_GROUP ? ZERO_GROUP - 1 - group : group + 1] = n;
+    }
+  };
+  auto largest_of = [](const u32x4& v) {
+    // as whole numbers of 16 bits positive logits are ordered and negative ones lie below them
+    const short2_t x = max2(max2(as_short2(v[0]), as_short2(v[1])), max2(as_short2(v[2]), as_short2(v[3])));
+    return max(x[0], x[1]);
+  };
+  for_vectors(count);
+  __syncthreads();
+  if (ct.other) return false;
+  count_groups();
+  if (tid == 0) ct.count[ZERO_GROUP] = ct.zeros + ct.tiny;
+  __syncthreads();
+  // ---- the groups that have any, one behind the other, and the largest logit
+  const unsigned own_count = tid < (int)CT_GROUPS ? ct.count[tid] : 0;
+  u64 row_count;
+  // (counts and groups side by side in one sum)
+  const u64 before = p.block_before((u64)own_count << 32 | (own_count != 0), row_count);
+  const unsigned count_before = (unsigned)(before >> 32), lists = (unsigned)row_count;
+  const unsigned tiny = ct.tiny;
+  if (!lists) return false;
+  if (own_count) {
+    ct.list[(unsigned)before] = (unsigned short)tid;
+    if (!count_before) ct.first = tid;
+  }
+  __syncthreads();
+  if (tiny && ct.first == ZERO_GROUP) return false;
+  const unsigned first = ct.first * 64 + __ffsll((unsigned long long)__ballot(ct.of(ct.first * 64 + lane) != 0)) - 1;
+  p.m = rank_value(first);
+  if (ct.left_out && !(p.m + CT_FAR > REACH * rule.temperature)) return false;
+
+  // f(group, its ranks, their counts) with four ranks a lane and four groups a wavefront
+  auto sweep = [&](auto f) {
+    for (unsigned i = wave * 4 + lane / 16; i < lists; i += WAVES * 4) {
+      const unsigned g = ct.list[i], zero = ZERO_GROUP;
+      const u32x4 v = *(const u32x4*)&ct.counter[(g < zero ? zero - 1 - g : g == zero ? 0 : g - 1) * 64 + lane % 16 * 4];
+      unsigned n[4], r[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        n[j] = g == zero ? (lane % 16 || j ? 0 : ct.zeros) : v[j];
+        r[j] = g < zero ? g * 64 + 63 - (lane % 16 * 4 + j) : g * 64 + lane % 16 * 4 + j;
+      }
+      f(g, r, n);
+    }
+  };
+  // (ranks before the first one have no tokens)
+  auto rank_weight = [&](unsigned rank) { return (u64)p.weight(fminf(rank_value(rank), p.m)); };
+  sweep([&](unsigned g, const unsigned* r, const unsigned* n) {
+    u64 w = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w += n[j] * rank_weight(r[j]);
+    if (g == ZERO_GROUP)
+      for (unsigned i = lane % 16; i < tiny; i += 16) w += (u64)p.weight(bf2f(ct.tiny_bits[i]));
+    w += dpp_u64<0xB1, 0xf>(w);
+    w += dpp_u64<0x4E, 0xf>(w);
+    w += dpp_u64<0x141, 0xf>(w);
+    w += dpp_u64<0x140, 0xf>(w);
+    if (lane % 16 == 0) ct.mass[g] = w;
+  });
+  __syncthreads();
+  const u64 own_mass = tid < (int)CT_GROUPS ? ct.mass[tid] : 0;
+  u64 all;
+  const u64 mass_before = p.block_before(own_mass, all);
+
+  // ---- the tokens that stay: all of the ranks before `border`, and `ties` of its own.  One wavefront looks into the group.
+  auto into_group = [&](u64 need, bool by_mass) {
+    if (wave) return;
+    const unsigned g = ct.group, n = ct.of(g * 64 + lane);
+    const u64 w = n ? rank_weight(g * 64 + lane) : 0;
+    const u64 mass = ct.mass_before + wave_scan_u64(n * w), number = ct.count_before + wave_scan_u64(n);
+    const int at = __ffsll((unsigned long long)__ballot((by_mass ? mass : number) >= need)) - 1;
+    if (lane != at) return;
+    // as many of the rank's tokens, which weigh the same, as reach it
+    const unsigned some = by_mass ? (unsigned)((need - (mass - n * w) + w - 1) / w) : (unsigned)(need - (number - n));
+    ct.border = g * 64 + at;
+    ct.ties = some;
+    ct.border_weight = w;
+    ct.stays = mass - (n - some) * w;
+    ct.count_stays = (unsigned)number - (n - some);
+  };
+  auto from_here = [&]() { ct.group = tid; ct.mass_before = mass_before; ct.count_before = count_before; };
+  if (rule.top_k && rule.top_k < (row_count >> 32)) {
+    if (count_before < rule.top_k && count_before + own_count >= rule.top_k) from_here();
+    __syncthreads();
+    if (tiny && ct.group == ZERO_GROUP) return false;
+    into_group(rule.top_k, false);
+    __syncthreads();
+    all = ct.stays;
+  }
+  if (rule.top_p < 1.f) {
+    const u64 need = top_p_need(rule.top_p, all);
+    if (mass_before < need && mass_before + own_mass >= need) from_here();
+    __syncthreads();
+    if (tiny && ct.group == ZERO_GROUP) return false;
+    into_group(need, true);
+  }
+  __syncthreads();
+  const unsigned border = ct.border;
+  unsigned ties = ct.ties, kept = ct.count_stays;
+  if (ct.border_weight && least <= 0.0) all = ct.stays;
+  else {
+    u64 sum = 0;
+    unsigned number = 0;
+    sweep([&](unsigned g, const unsigned* r, const unsigned* n) {
+      if (g > border / 64) return;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const unsigned some = r[j] < border ? n[j] : r[j] == border ? min(n[j], ties) : 0;
+        const double w = p.weight(fminf(rank_value(r[j]), p.m));
+        if (w >= least && w > 0.0) { sum += some * (u64)w; number += some; }
+      }
+      if (g == ZERO_GROUP)
+        for (unsigned i = lane % 16; i < tiny; i += 16) {
+          const double w = p.weight(bf2f(ct.tiny_bits[i]));
+          if (w >= least && w > 0.0) { sum += (u64)w; ++number; }
+        }
+    });
+    kept = (unsigned)p.block_sum(number);
+    all = p.block_sum(sum);
+  }
+  const Search s{draw_target(uniform, all), ties};
+  const double limit = p.weight(rank_value(border));
+  const u64 tie_weight = limit >= least ? (u64)limit : 0;
+  const unsigned span = border - first;
+  const float z_border = rank_value(border);
+  auto weigh = [&](float z) {
+    const double w = p.weight(z);
+    return w >= least ? w : 0.0;
+  };
+  if (span + 2 <= CT_TABLE) {
+    // The weights of the ranks that stay, where the counters were; a mark for the border's; and a 0 behind them that all others read: a read
+    // without a branch can be under way with the next ones.  64 logits of a lane weigh 2^46 at most, and their marks lie above that.
+    constexpr double MARK = 0x1p47;
+    double* table = (double*)&ct;
+    __syncthreads();
+    for (unsigned i = tid; i <= span + 1; i += THREADS) table[i] = i < span ? weigh(rank_value(first + i)) : i == span ? MARK : 0.0;
+    __syncthreads();
+    u64 sum = 0;
+    unsigned number = 0;
+    // `none`: whether none of a vector's logits stays, at six operations for eight of them
+    auto pass = [&](auto none, auto add) {
+      for (unsigned t = begin; t < end; t += AHEAD) {
+        u32x4 v[AHEAD];
+        p.read(v, t, end);
+        double mine = 0.0;
+#pragma unroll
+        for (int b = 0; b < AHEAD; ++b)
+          if (t + b < end && !__all(none(v[b]))) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mine += add(v[b][i] & 0xffff) + add(v[b][i] >> 16);
+          }
+        const double marks = floor(mine * (1 / MARK));
+        number += (unsigned)marks;
+        sum += (u64)(mine - marks * MARK);
+      }
+    };
+    const unsigned top = __float_as_uint(p.m) >> 16;
+    // (the rank by one subtraction where all that stays has one sign)
+    if (border < RANK_ZERO || first > RANK_ZERO) {
+      const unsigned from = border < RANK_ZERO ? top : 0 - top, sign = border < RANK_ZERO ? 0xffffffffu : 0;      // top - u, or u - top
+      const unsigned add = from - sign;
+      const short least_bits = border < RANK_ZERO ? (short)(__float_as_uint(z_border) >> 16) : (short)-32768;
+      pass([&](const u32x4& v) { return largest_of(v) < least_bits; }, [&](unsigned u) { return table[min((u ^ sign) + add, span + 1)]; });
+      p.leave(sum, number);
+      p.search(s, tie_weight, [&](float z, u64& w) {
+        const unsigned i = min(((__float_as_uint(z) >> 16) ^ sign) + add, span + 1);
+        w = (u64)table[i];
+        return i == span;
+      });
+    } else {
+      auto of = [&](unsigned u) { return table[min(rank_of(u) - first, span + 1)]; };
+      auto stays = [&](unsigned u) { return next_to_zero(u) && __uint_as_float(u << 16) > z_border; };
+      pass([&](const u32x4& v) {
+             if (tiny) for_some(v, stays, [&](unsigned u) { sum += (u64)weigh(__uint_as_float(u << 16)); });
+             return false;
+           }, of);
+      p.leave(sum, number);
+      p.search(s, tie_weight, [&](float z, u64& w) {
+        const unsigned u = __float_as_uint(z) >> 16;
+        w = (u64)(tiny && stays(u) ? weigh(z) : of(u));
+        return z == z_border;
+      });
+    }
+  } else {
+    double mine = 0.0;
+    unsigned number = 0;
+    p.each([&](float z) {
+      if (z > z_border) mine += weigh(z);
+      number += z == z_border;
+    });
+    p.leave((u64)mine, number);
+    p.search(s, tie_weight, [&](float z, u64& w) {
+      w = z > z_border ? (u64)weigh(z) : 0;
+      return z == z_border;
+    });
+  }
+  drawn_answer(a, p, rule.temperature, all, kept);
+  return true;
+}
+
+template <typename T, int THREADS>
+__global__ __launch_bounds__(THREADS, THREADS == 512 ? 6 : THREADS == 256 ? 3 : 4) void sample_kernel(SampleArgs a) {
+  constexpr bool COUNTED = sizeof(T) == 2;
+  __shared__ SampleShared sh;
+  __shared__ __attribute__((aligned(16))) unsigned char room[SAMPLE_ROOM];
+  Sampler<T, THREADS> p(sh, a);
+  const karma_sample_rule rule = a.rules[a.n_rules == 1 ? 0 : blockIdx.x];
+  const float uniform = a.uniform[blockIdx.x];
+  if (!(rule.temperature >= 0.f && rule.temperature < INFINITY) || rule.top_p != rule.top_p || rule.min_p != rule.min_p) return no_answer(a);
+  if (rule.temperature == 0.f || rule.top_k == 1 || rule.top_p <= 0.f) {
+    // one token stays: the first of the largest
+    float own;
+    if (!p.largest(own)) return no_answer(a);
+    unsigned ties = 0;
+    p.template each<Sampler<T, THREADS>::LIGHT>([&](float z) { ties += z == p.m; });
+    p.leave(0, ties);
+    p.search(Search{0, 1}, 1, [&](float z, u64&) { return z == p.m; });
+    return answer(a, (int)sh.token, 0.f, 1);
+  }
+  p.c = 1.4426950408889634074 / (double)rule.temperature;
+  const double least = rule.min_p > 0.f ? fmin((double)rule.min_p, 1.0) * ONE : 0.0;
+  static_assert(sizeof(List) <= SAMPLE_ROOM, "room");
+  if (rule.top_k && rule.top_k <= LIST_TOP_K && rule.top_k < a.cols) {
+    if (sample_by_list<T, THREADS>(a, rule, uniform, least, p, *(List*)room)) return;
+    __syncthreads();
+  }
+  if constexpr (COUNTED) {
+    if ((rule.top_k && rule.top_k < a.cols) || rule.top_p < 1.f) {
+      if (sample_by_counters<THREADS>(a, rule, uniform, least, p, *(Counted*)room)) return;
+      __syncthreads();
     }
   }
+  sample_by_bins<T, THREADS>(a, rule, uniform, least, p, (Bins*)room);
 }
 
 bool aligned_to(const void* p, size_t n) { return (uintptr_t)p % n == 0; }
@@ -428,6 +986,13 @@ bool aligned_to(const void* p, size_t n) { return (uintptr_t)p % n == 0; }
 }  // namespace
 
 size_t sample_ws_bytes(uint32_t, uint32_t) { return 0; }
+// Threads of a row.  More of them shorten a row's way (1 x 51200 in bf16 with top_p: 256 / 512 / 1024 threads 58 / 38 / 29 us), fewer leave
+// room for more rows on a compute unit: three of 512 threads, one of 1024 (4096 x 8000: 98 / 102 / 224; 1024 x 16000: 49 / 44 / 70), and wait less
+// for each other where rows are short (64 x 1000 12.3 / 12.5 / 14.5).
+static int sample_threads(uint32_t rows, uint32_t cols) {
+  if (rows <= 256) return cols <= 4096 ? 256 : cols <= 12288 ? 512 : 1024;
+  return cols <= 12288 ? 256 : 512;
+}
 
 int sample_rows(SampleArgs a, bool bf16, hipStream_t s) {
   if (!a.ld) a.ld = a.cols;
@@ -438,8 +1003,11 @@ int sample_rows(SampleArgs a, bool bf16, hipStream_t s) {
     if (!aligned_to(p, 4)) return KARMA_E_INVAL;
   if (!a.rows) return KARMA_OK;
   if (!a.logits || !a.rules || !a.uniform || !aligned_to(a.logits, bf16 ? 2 : 4)) return KARMA_E_INVAL;
-  if (bf16) hipLaunchKernelGGL((sample_kernel<bf16_t, 1024>), dim3(a.rows), dim3(1024), 0, s, a);
-  else hipLaunchKernelGGL((sample_kernel<float, 1024>), dim3(a.rows), dim3(1024), 0, s, a);
+#define KARMA_SAMPLE_LAUNCH(T, THREADS) hipLaunchKernelGGL((sample_kernel<T, THREADS>), dim3(a.rows), dim3(THREADS), 0, s, a)
+  const int threads = sample_threads(a.rows, a.cols);
+  if (bf16) { if (threads == 256) KARMA_SAMPLE_LAUNCH(bf16_t, 256); else if (threads == 512) KARMA_SAMPLE_LAUNCH(bf16_t, 512); else KARMA_SAMPLE_LAUNCH(bf16_t, 1024); }
+  else { if (threads == 256) KARMA_SAMPLE_LAUNCH(float, 256); else if (threads == 512) KARMA_SAMPLE_LAUNCH(float, 512); else KARMA_SAMPLE_LAUNCH(float, 1024); }
+#undef KARMA_SAMPLE_LAUNCH
   return hipGetLastError() == hipSuccess ? KARMA_OK : KARMA_E_HIP;
 }
 

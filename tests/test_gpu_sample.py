@@ -128,6 +128,58 @@ def test_many_values_close_together(t):
 
 
 @pytest.mark.parametrize("t", ["bf16", "f32"])
+def test_numbers_of_every_size(t):
+    """Rows with a few logits next to 0, far below or far above the others, and of one sign."""
+    import torch
+    rng = np.random.default_rng(12)
+    rules = [(1.0, 0.9, 0.0, 0), (1.0, 1.0, 0.0, 300), (0.5, 0.5, 0.0, 0), (1.0, 0.999, 0.01, 0), (1e5, 0.7, 0.0, 0), (1e5, 1.0, 0.0, 600), (3.0, 0.99, 0.0, 700),
+             (1.0, 1.0, 0.0, 0), (20.0, 0.6, 0.0, 0), (1.0, 0.9, 0.0, 20)]
+    cols = 1200
+    base = rng.standard_normal((len(rules), cols)).astype(np.float32)
+    tiny = base.copy()
+    at = rng.integers(0, cols, 12)
+    tiny[:, at] = np.array([1e-5, -1e-5, 1e-6, -1e-6, 3e-5, -3e-5, 1e-20, -1e-20, 1e-40, 0.0, -0.0, 5e-5], np.float32)
+    flat = np.where(np.abs(base) > 1.5, -base ** 2, 0).astype(np.float32)       # mostly zeros, the largest
+    flat[:, at] = tiny[:, at]
+    far = base.copy()
+    far[:, ::5] = -1e6
+    far[:, 1::50] = -3e5
+    high = base.copy()
+    high[:, 700] = 1e6
+    high[:, 701] = 1e6
+    for z in (tiny, flat, far, high, base - 9, base + 9, 1e-3 * base - 300000, 40 * base):
+        z = torch.from_numpy(np.ascontiguousarray(z, np.float32)).to(types()[t]).cuda()
+        for u in (rng.random(len(rules)), np.full(len(rules), 0.9999999)):
+            check(z, rules, u.astype(np.float32))
+
+
+@pytest.mark.parametrize("t", ["bf16", "f32"])
+def test_rows_for_every_number_of_threads(t):
+    import torch
+    rng = np.random.default_rng(13)
+    for rows, cols in ((257, 13000), (257, 700), (3, 13000), (2, 9000), (2, 70001)):
+        z = torch.from_numpy((2 * rng.standard_normal((rows, cols))).astype(np.float32)).to(types()[t]).cuda()
+        rules = [RULES[r % len(RULES)] for r in range(rows)]
+        for u in (rng.random(rows), np.full(rows, 0.999)):
+            check(z, rules, u.astype(np.float32))
+    z = torch.from_numpy((2 * rng.standard_normal((8, 140001))).astype(np.float32)).to(types()[t]).cuda()
+    check(z, [(1.0, 0.9, 0.0, 0), (0.7, 0.95, 0.0, 40), (1.0, 1.0, 0.0, 0), (1.3, 0.97, 0.02, 0), (1.0, 0.9, 0.0, 128), (1.0, 0.9, 0.0, 129), (1.5, 1.0, 0.0, 5000),
+              (0.8, 1.0, 0.1, 0)], rng.random(8).astype(np.float32))
+
+
+@pytest.mark.parametrize("t", ["bf16", "f32"])
+def test_many_equal_logits_at_a_small_top_k(t):
+    """More tokens than a list of candidates holds, all of them equal."""
+    import torch
+    rng = np.random.default_rng(14)
+    z = torch.from_numpy((0.3 * rng.standard_normal((4, 6000))).astype(np.float32)).to(types()[t]).cuda()
+    for some in (100, 300, 5000):
+        z[:, rng.permutation(6000)[:some]] = 2.0
+        for k in (2, 50, 128):
+            check(z, [(1.0, 0.9, 0.0, k)], np.array([0.0, 0.3, 0.6, 0.99], np.float32))
+
+
+@pytest.mark.parametrize("t", ["bf16", "f32"])
 def test_masks_and_rows_without_answer(t):
     import torch
     rng = np.random.default_rng(6)
