@@ -17,7 +17,7 @@
 namespace karma {
 namespace {
 
-constexpr int QK_WAVES = 4, QK_THREADS = 64 * QK_WAVES;
+constexpr int QK_WAVES = 4, QK_BWD_WAVES = 8;
 
 
 // V elements between memory and fp32, one access
@@ -90,37 +90,51 @@ __device__ __forceinline__ float group_sum(float v, int lanes) {
 }
 
 // What a lane has of every head: NU units of 2 V columns, V of them (lo) and V others (hi) that they turn with.  Unit u of the
-// turned columns is u V .. and rot / 2 + u V .., or (PAIRS) 2 u V .. + 2 V; the columns behind `rot` are cut into runs of 2 V.
+// turned columns is u V .. and rot / 2 + u V .., or (PAIRS) 2 u V .. + 2 V, of which the second half may not turn; the columns behind
+// `rot` are cut into runs of 2 V.
+// Cosines and sines of a token's pairs are computed once by a wavefront, a pair a lane, and handed on through LDS.
+typedef float PairTurn[KARMA_QK_D_MAX / 2][2];
 template <int V, int NU, bool PAIRS>
 struct Units {
-  int lo[NU], hi[NU];
-  bool there[NU], turns[NU];
+  int lo[NU], hi[NU], unit[NU];
+  bool there[NU], turns[NU], turns_hi[NU];
   float c[NU][V], s[NU][V];
   __device__ __forceinline__ void place(const QkArgs& a, int lane) {
-    const int turned = a.rot / (2 * V), units = a.d / (2 * V);
+    const int units = a.d / (2 * V);
 #pragma unroll
     for (int k = 0; k < NU; ++k) {
       const int u = lane % a.lanes + k * a.lanes;
       there[k] = u < units;
-      turns[k] = u < turned;
+      turns[k] = 2 * u * V < a.rot;
+      turns_hi[k] = PAIRS && V > 1 ? (2 * u + 1) * V < a.rot : turns[k];
+      unit[k] = turns[k] ? u : 0;
       const bool pairs = PAIRS || !turns[k];
       lo[k] = pairs ? 2 * u * V : u * V;
       hi[k] = pairs ? 2 * u * V + V : a.rot / 2 + u * V;
       if (!there[k]) lo[k] = hi[k] = 0;
     }
   }
-  __device__ __forceinline__ void angles(const QkArgs& a, int lane, int token) {
+  __device__ __forceinline__ void angles(const QkArgs& a, int lane, int token, PairTurn& pairs) {
+    if (!a.rot) return;
     const double at = a.positions ? (double)a.positions[token] : (double)((unsigned)token % a.seq);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");      // (the last token's have been read)
+    __builtin_amdgcn_wave_barrier();
+    for (int i = lane; i < a.rot / 2; i += 64) {
+      const double turn = at * a.freq[i] * 0.15915494309189533577;
+      float s1, c1;
+      sincospif(2.f * (float)(turn - rint(turn)), &s1, &c1);
+      pairs[i][0] = c1;
+      pairs[i][1] = s1;
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
 #pragma unroll
-    for (int k = 0; k < NU; ++k) {
-      const int u = lane % a.lanes + k * a.lanes;
+    for (int k = 0; k < NU; ++k)
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        const double turn = turns[k] ? at * a.freq[u * V + e] * 0.15915494309189533577 : 0.0;
-        const float part = (float)(turn - rint(turn));
-        sincospif(2.f * part, &s[k][e], &c[k][e]);
+        c[k][e] = pairs[unit[k] * V + e][0];
+        s[k][e] = pairs[unit[k] * V + e][1];
       }
-    }
   }
   // in place; dir -1: back.  (Columns that do not turn are left alone, not turned by 0: the other one may be infinite.)
   __device__ __forceinline__ void turn(int k, float* x, float* y, float dir) const {
@@ -131,8 +145,9 @@ struct Units {
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         const float p = f[2 * e], q = f[2 * e + 1], t = dir * s[k][e];
-        f[2 * e] = turns[k] ? fmaf(p, c[k][e], -q * t) : p;
-        f[2 * e + 1] = turns[k] ? fmaf(q, c[k][e], p * t) : q;
+        const bool on = e < V / 2 ? turns[k] : turns_hi[k];
+        f[2 * e] = on ? fmaf(p, c[k][e], -q * t) : p;
+        f[2 * e + 1] = on ? fmaf(q, c[k][e], p * t) : q;
       }
 #pragma unroll
       for (int e = 0; e < V; ++e) { x[e] = f[e]; y[e] = f[V + e]; }
@@ -169,122 +184,146 @@ __device__ __forceinline__ void move_values(const QkArgs& a, const U& un, size_t
 
 template <typename T, int V, int NU>
 struct Gamma {
-  float lo[NU][V], hi[NU][V];
+  Piece<T, V> lo[NU], hi[NU];
   template <class U>
   __device__ __forceinline__ void load(const void* g, const U& un) {
+    if (!g) return;
 #pragma unroll
     for (int k = 0; k < NU; ++k) {
-      if (g) {
-        to_f32(load_piece<T, V>((const T*)g + un.lo[k]), lo[k]);
-        to_f32(load_piece<T, V>((const T*)g + un.hi[k]), hi[k]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < V; ++e) lo[k][e] = hi[k][e] = 1.f;
-      }
+      lo[k] = load_piece<T, V>((const T*)g + un.lo[k]);
+      hi[k] = load_piece<T, V>((const T*)g + un.hi[k]);
     }
   }
 };
+template <typename T, int V>
+__device__ __forceinline__ void to_gamma(bool given, const Piece<T, V>& p, float* f) {
+  to_f32(p, f);
+  if (!given)
+#pragma unroll
+    for (int e = 0; e < V; ++e) f[e] = 1.f;
+}
 
-// A wavefront has a token, or one part of its heads: 64 / lanes heads side by side, BATCH such groups under way.
+// A wavefront has a token, or one part of its heads: 64 / lanes heads side by side, BATCH such groups under way, the first ones while the
+// angles are computed.
 template <typename T, int V, int NU, bool PAIRS>
-__global__ __launch_bounds__(QK_THREADS) void qk_fwd_kernel(QkArgs a) {
+__global__ __launch_bounds__(64 * QK_WAVES) void qk_fwd_kernel(QkArgs a) {
   constexpr int BATCH = NU * V * sizeof(T) >= 16 ? 2 : 4;
-  const int lane = threadIdx.x & 63, per = 64 / a.lanes, sub = lane / a.lanes;
-  const unsigned wave = __builtin_amdgcn_readfirstlane(blockIdx.x * QK_WAVES + threadIdx.x / 64);
+  __shared__ PairTurn pairs[QK_WAVES];
+  const int lane = threadIdx.x & 63, per = 64 / a.lanes, sub = lane / a.lanes, wv = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const unsigned wave = blockIdx.x * QK_WAVES + wv;
   const unsigned token = wave / a.parts;
   if (token >= a.tokens) return;
-  int first = wave % a.parts;
+  const int first = wave % a.parts;
   Units<V, NU, PAIRS> un;
   un.place(a, lane);
-  un.angles(a, lane, token);
+  const int nq = (a.heads[0] + per - 1) / per, n = nq + (a.heads[1] + per - 1) / per;
   const float inv_d = 1.f / (float)a.d;
-#pragma unroll 1
-  for (int seg = 0; seg < 2; ++seg) {
-    const int heads = a.heads[seg], n = (heads + per - 1) / per;
-    const T* x = (const T*)a.x[seg] + (size_t)token * a.ld_x[seg];
-    T* y = (T*)a.out[seg] + (size_t)token * a.ld_out[seg];
-    Gamma<T, V, NU> gm;
-    gm.load(a.gamma[seg], un);
-    for (; first < n; first += BATCH * a.parts) {
-      Piece<T, V> lo[BATCH][NU], hi[BATCH][NU];
+  Piece<T, V> lo[BATCH][NU], hi[BATCH][NU];
+  auto fetch = [&](int at) {
 #pragma unroll
-      for (int b = 0; b < BATCH; ++b) {
-        const int head = (first + b * a.parts) * per + sub;
+    for (int b = 0; b < BATCH; ++b) {
+      const int it = at + b * a.parts, seg = it < nq ? 0 : 1, head = (seg ? it - nq : it) * per + sub;
+      const T* x = (const T*)a.x[seg] + (size_t)token * a.ld_x[seg] + (size_t)head * a.d;
 #pragma unroll
-        for (int k = 0; k < NU; ++k) {
-          const bool in = head < heads && un.there[k];
-          lo[b][k] = in ? load_piece<T, V>(x + (size_t)head * a.d + un.lo[k]) : no_piece<T, V>();
-          hi[b][k] = in ? load_piece<T, V>(x + (size_t)head * a.d + un.hi[k]) : no_piece<T, V>();
-        }
+      for (int k = 0; k < NU; ++k) {
+        const bool in = it < n && head < a.heads[seg] && un.there[k];
+        lo[b][k] = in ? load_piece<T, V>(x + un.lo[k]) : no_piece<T, V>();
+        hi[b][k] = in ? load_piece<T, V>(x + un.hi[k]) : no_piece<T, V>();
       }
+    }
+  };
+  Gamma<T, V, NU> gamma[2];
+  fetch(first);
+  gamma[0].load(a.gamma[0], un);
+  gamma[1].load(a.gamma[1], un);
+  un.angles(a, lane, token, pairs[wv]);
+  int it = first;
+  while (it < n) {
 #pragma unroll
-      for (int b = 0; b < BATCH; ++b) {
-        const int head = (first + b * a.parts) * per + sub;
-        float p[NU][V], q[NU][V], sum = 0.f;
+    for (int b = 0; b < BATCH; ++b) {
+      const int i = it + b * a.parts;
+      if (i >= n) break;
+      const int seg = i < nq ? 0 : 1, head = (seg ? i - nq : i) * per + sub;
+      T* y = (T*)a.out[seg] + (size_t)token * a.ld_out[seg] + (size_t)head * a.d;
+      float p[NU][V], q[NU][V], sum = 0.f;
 #pragma unroll
-        for (int k = 0; k < NU; ++k) {
-          to_f32(lo[b][k], p[k]);
-          to_f32(hi[b][k], q[k]);
+      for (int k = 0; k < NU; ++k) {
+        to_f32(lo[b][k], p[k]);
+        to_f32(hi[b][k], q[k]);
 #pragma unroll
-          for (int e = 0; e < V; ++e) sum = fmaf(p[k][e], p[k][e], fmaf(q[k][e], q[k][e], sum));
-        }
-        const float r = a.norm ? 1.f / sqrtf(fmaf(group_sum(sum, a.lanes), inv_d, a.eps)) : 1.f;
+        for (int e = 0; e < V; ++e) sum = fmaf(p[k][e], p[k][e], fmaf(q[k][e], q[k][e], sum));
+      }
+      const float r = a.norm ? 1.f / sqrtf(fmaf(group_sum(sum, a.lanes), inv_d, a.eps)) : 1.f;
 #pragma unroll
-        for (int k = 0; k < NU; ++k) {
+      for (int k = 0; k < NU; ++k) {
+        float gl[V], gh[V];
+        to_gamma(a.gamma[seg] != nullptr, seg ? gamma[1].lo[k] : gamma[0].lo[k], gl);
+        to_gamma(a.gamma[seg] != nullptr, seg ? gamma[1].hi[k] : gamma[0].hi[k], gh);
 #pragma unroll
-          for (int e = 0; e < V; ++e) { p[k][e] *= r * gm.lo[k][e]; q[k][e] *= r * gm.hi[k][e]; }
-          un.turn(k, p[k], q[k], 1.f);
-          if (head < heads && un.there[k]) {
-            store_piece(y + (size_t)head * a.d + un.lo[k], p[k], std::integral_constant<int, V>());
-            store_piece(y + (size_t)head * a.d + un.hi[k], q[k], std::integral_constant<int, V>());
-          }
+        for (int e = 0; e < V; ++e) { p[k][e] *= r * gl[e]; q[k][e] *= r * gh[e]; }
+        un.turn(k, p[k], q[k], 1.f);
+        if (head < a.heads[seg] && un.there[k]) {
+          store_piece(y + un.lo[k], p[k], std::integral_constant<int, V>());
+          store_piece(y + un.hi[k], q[k], std::integral_constant<int, V>());
         }
       }
     }
-    // the parts' turns go on through queries, keys and values
-    first = first >= n ? (first - n) % a.parts : first;
+    it += BATCH * a.parts;
+    if (it < n) fetch(it);
   }
-  move_values<T, V, NU>(a, un, token, lane, first, a.parts);
+  // the parts' turns go on through queries, keys and values
+  move_values<T, V, NU>(a, un, token, lane, (it - n) % a.parts, a.parts);
 }
 
-// A workgroup has the tokens blockIdx, blockIdx + gridDim, ... of a wavefront each, and adds up what they give to dgamma.
+// A workgroup's wavefronts have a token each, or a part of its heads, and then the next ones; first the queries of all, then the keys, as one sum for
+// dgamma takes half the registers of two.
 template <typename T, int V, int NU, bool PAIRS>
-__global__ __launch_bounds__(QK_THREADS) void qk_bwd_kernel(QkArgs a) {
-  const int lane = threadIdx.x & 63, per = 64 / a.lanes, sub = lane / a.lanes, wave = threadIdx.x / 64;
+__global__ __launch_bounds__(64 * QK_BWD_WAVES) void qk_bwd_kernel(QkArgs a) {
+  __shared__ PairTurn pairs[QK_BWD_WAVES];
+  __shared__ float sums[QK_BWD_WAVES][2 * KARMA_QK_D_MAX];
+  const int lane = threadIdx.x & 63, per = 64 / a.lanes, sub = lane / a.lanes, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   Units<V, NU, PAIRS> un;
   un.place(a, lane);
   const float inv_d = 1.f / (float)a.d;
-  float sum_lo[2][NU][V], sum_hi[2][NU][V];
+  const unsigned waves = gridDim.x * QK_BWD_WAVES, all = a.tokens * (unsigned)a.parts;
+  int before = 0;       // groups of heads of the segments before
+#pragma unroll 1
+  for (int seg = 0; seg < 2; ++seg) {
+    const int heads = a.heads[seg], n = (heads + per - 1) / per;
+    float sum_lo[NU][V], sum_hi[NU][V];
 #pragma unroll
-  for (int k = 0; k < NU; ++k)
+    for (int k = 0; k < NU; ++k)
 #pragma unroll
-    for (int e = 0; e < V; ++e) sum_lo[0][k][e] = sum_hi[0][k][e] = sum_lo[1][k][e] = sum_hi[1][k][e] = 0.f;
-
-  const unsigned waves = gridDim.x * QK_WAVES, all = a.tokens * (unsigned)a.parts;
-  for (unsigned w = __builtin_amdgcn_readfirstlane(blockIdx.x * QK_WAVES + wave); w < all; w += waves) {
-    const unsigned token = w / a.parts;
-    int first = w % a.parts;
-    un.angles(a, lane, token);
-#pragma unroll
-    for (int seg = 0; seg < 2; ++seg) {
-      const int heads = a.heads[seg], n = (heads + per - 1) / per;
+      for (int e = 0; e < V; ++e) sum_lo[k][e] = sum_hi[k][e] = 0.f;
+    Gamma<T, V, NU> gamma;
+    gamma.load(a.gamma[seg], un);
+    const bool given = a.gamma[seg] != nullptr;
+    for (unsigned w = blockIdx.x * QK_BWD_WAVES + wave; w < all; w += waves) {
+      const unsigned token = w / a.parts;
+      // the parts' turns go on through queries, keys and values
+      int it = (int)((w + (unsigned)a.parts * ((unsigned)before / a.parts + 1) - (unsigned)before) % a.parts);
+      if (it >= n) continue;
       const T* x = (const T*)a.x[seg] + (size_t)token * a.ld_x[seg];
       const T* dy = (const T*)a.dy[seg] + (size_t)token * a.ld_dy[seg];
       T* dx = (T*)a.out[seg] + (size_t)token * a.ld_out[seg];
-      Gamma<T, V, NU> gm;
-      gm.load(a.gamma[seg], un);
-      for (; first < n; first += a.parts) {
-        const int head = first * per + sub;
+      Piece<T, V> xl[NU], xh[NU], gl[NU], gh[NU];
+      auto fetch = [&](int i) {
+        const int head = i * per + sub;
         const size_t at = (size_t)head * a.d;
-        Piece<T, V> xl[NU], xh[NU], gl[NU], gh[NU];
 #pragma unroll
         for (int k = 0; k < NU; ++k) {
           const bool in = head < heads && un.there[k];
-          xl[k] = in && a.norm ? load_piece<T, V>(x + at + un.lo[k]) : no_piece<T, V>();
-          xh[k] = in && a.norm ? load_piece<T, V>(x + at + un.hi[k]) : no_piece<T, V>();
           gl[k] = in ? load_piece<T, V>(dy + at + un.lo[k]) : no_piece<T, V>();
           gh[k] = in ? load_piece<T, V>(dy + at + un.hi[k]) : no_piece<T, V>();
+          xl[k] = in && a.norm ? load_piece<T, V>(x + at + un.lo[k]) : no_piece<T, V>();
+          xh[k] = in && a.norm ? load_piece<T, V>(x + at + un.hi[k]) : no_piece<T, V>();
         }
+      };
+      fetch(it);
+      un.angles(a, lane, token, pairs[wave]);
+      while (it < n) {
+        const int head = it * per + sub;
+        const size_t at = (size_t)head * a.d;
         float p[NU][V], q[NU][V], f[NU][V], g[NU][V], sq = 0.f, dot = 0.f;
 #pragma unroll
         for (int k = 0; k < NU; ++k) {
@@ -292,11 +331,20 @@ __global__ __launch_bounds__(QK_THREADS) void qk_bwd_kernel(QkArgs a) {
           to_f32(xh[k], q[k]);
           to_f32(gl[k], f[k]);
           to_f32(gh[k], g[k]);
+        }
+        // the next group's vectors are on their way while this one is worked on
+        it += a.parts;
+        if (it < n) fetch(it);
+#pragma unroll
+        for (int k = 0; k < NU; ++k) {
+          float ml[V], mh[V];
+          to_gamma(given, gamma.lo[k], ml);
+          to_gamma(given, gamma.hi[k], mh);
           un.turn(k, f[k], g[k], -1.f);
 #pragma unroll
           for (int e = 0; e < V; ++e) {
             sq = fmaf(p[k][e], p[k][e], fmaf(q[k][e], q[k][e], sq));
-            dot = fmaf(f[k][e] * gm.lo[k][e], p[k][e], fmaf(g[k][e] * gm.hi[k][e], q[k][e], dot));
+            dot = fmaf(f[k][e] * ml[e], p[k][e], fmaf(g[k][e] * mh[e], q[k][e], dot));
           }
         }
         float r = 1.f, back = 0.f;
@@ -306,13 +354,16 @@ __global__ __launch_bounds__(QK_THREADS) void qk_bwd_kernel(QkArgs a) {
         }
 #pragma unroll
         for (int k = 0; k < NU; ++k) {
+          float ml[V], mh[V];
+          to_gamma(given, gamma.lo[k], ml);
+          to_gamma(given, gamma.hi[k], mh);
 #pragma unroll
           for (int e = 0; e < V; ++e) {
             const float u = r * p[k][e], v = r * q[k][e];
-            sum_lo[seg][k][e] = fmaf(f[k][e], u, sum_lo[seg][k][e]);
-            sum_hi[seg][k][e] = fmaf(g[k][e], v, sum_hi[seg][k][e]);
-            f[k][e] = fmaf(f[k][e] * gm.lo[k][e], r, -u * back);
-            g[k][e] = fmaf(g[k][e] * gm.hi[k][e], r, -v * back);
+            sum_lo[k][e] = fmaf(f[k][e], u, sum_lo[k][e]);
+            sum_hi[k][e] = fmaf(g[k][e], v, sum_hi[k][e]);
+            f[k][e] = fmaf(f[k][e] * ml[e], r, -u * back);
+            g[k][e] = fmaf(g[k][e] * mh[e], r, -v * back);
           }
           if (head < heads && un.there[k]) {
             store_piece(dx + at + un.lo[k], f[k], std::integral_constant<int, V>());
@@ -320,20 +371,15 @@ __global__ __launch_bounds__(QK_THREADS) void qk_bwd_kernel(QkArgs a) {
           }
         }
       }
-      first = first >= n ? (first - n) % a.parts : first;
     }
-    move_values<T, V, NU>(a, un, token, lane, first, a.parts);
-  }
-  if (!a.partial) return;
-  // the groups of lanes that have the same columns, then the wavefronts, in a fixed order
-  __shared__ float sums[QK_WAVES][2 * KARMA_QK_D_MAX];
-#pragma unroll
-  for (int seg = 0; seg < 2; ++seg)
+    before += n;
+    if (!a.partial) continue;
+    // the groups of lanes that have the same columns
 #pragma unroll
     for (int k = 0; k < NU; ++k)
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        float l = sum_lo[seg][k][e], h = sum_hi[seg][k][e];
+        float l = sum_lo[k][e], h = sum_hi[k][e];
         for (int m = a.lanes; m < 64; m *= 2) {
           l += __shfl_xor(l, m, 64);
           h += __shfl_xor(h, m, 64);
@@ -343,11 +389,16 @@ __global__ __launch_bounds__(QK_THREADS) void qk_bwd_kernel(QkArgs a) {
           sums[wave][seg * a.d + un.hi[k] + e] = h;
         }
       }
+  }
+  for (unsigned w = blockIdx.x * QK_BWD_WAVES + wave; w < all && a.heads[2]; w += waves)
+    move_values<T, V, NU>(a, un, w / a.parts, lane, (int)((w + (unsigned)a.parts * ((unsigned)before / a.parts + 1) - (unsigned)before) % a.parts), a.parts);
+  if (!a.partial) return;
+  // the wavefronts, in a fixed order
   __syncthreads();
-  for (int i = threadIdx.x; i < 2 * a.d; i += QK_THREADS) {
+  for (int i = threadIdx.x; i < 2 * a.d; i += 64 * QK_BWD_WAVES) {
     float v = 0.f;
 #pragma unroll
-    for (int w = 0; w < QK_WAVES; ++w) v += sums[w][i];
+    for (int w = 0; w < QK_BWD_WAVES; ++w) v += sums[w][i];
     a.partial[(size_t)blockIdx.x * 2 * a.d + i] = v;
   }
 }
@@ -376,8 +427,8 @@ __global__ __launch_bounds__(DG_COLS * DG_ROWS) void qk_dgamma_kernel(const floa
 bool aligned_to(const void* p, size_t n) { return (uintptr_t)p % n == 0; }
 
 // Workgroups of the backward pass: a row of sums for dgamma each.
-constexpr unsigned QK_BWD_GROUPS = 1024, QK_PLACES = 4096;
-unsigned bwd_groups(uint64_t waves) { return (unsigned)std::min<uint64_t>(QK_BWD_GROUPS, (waves + QK_WAVES - 1) / QK_WAVES); }
+constexpr unsigned QK_BWD_GROUPS = 512, QK_PLACES = 16384;
+unsigned bwd_groups(uint64_t waves) { return (unsigned)std::min<uint64_t>(QK_BWD_GROUPS, (waves + QK_BWD_WAVES - 1) / QK_BWD_WAVES); }
 
 bool good_shape(const karma_qk_shape& s) {
   if (s.tokens > KARMA_QK_TOKENS_MAX || s.seq > KARMA_QK_TOKENS_MAX || (s.flags & ~3u)) return false;
@@ -395,11 +446,12 @@ bool good_shape(const karma_qk_shape& s) {
 
 // How many elements an access has (all pointers, strides and the cut of a head's columns allow it), and how the lanes are dealt.
 struct QkCut { int v, nu; };
-QkCut cut(const QkArgs& a, bool bf16, bool backward) {
+// Backward a lane has eight columns at most: with sixteen it takes 154 registers (16384 tokens x 40 heads x 128: 132 us, with eight 99).
+QkCut cut(const QkArgs& a, bool bf16, bool pairs, bool backward) {
   const size_t e = bf16 ? 2 : 4;
-  int v = (int)(16 / e);
+  int v = bf16 && !backward ? 8 : 4;
   auto whole = [&](int v) {
-    if (a.rot % (2 * v) || (a.d - a.rot) % (2 * v)) return false;
+    if (pairs ? a.rot % v || a.d % (2 * v) : a.rot % (2 * v) || (a.d - a.rot) % (2 * v)) return false;
     for (int k = 0; k < 3; ++k) {
       if (!a.heads[k]) continue;
       const bool value = k == 2;
@@ -416,14 +468,15 @@ QkCut cut(const QkArgs& a, bool bf16, bool backward) {
 
 template <bool BWD, typename T, int V, int NU, bool PAIRS>
 void launch_one(const QkArgs& a, unsigned grid, hipStream_t s) {
-  if constexpr (BWD) hipLaunchKernelGGL((qk_bwd_kernel<T, V, NU, PAIRS>), dim3(grid), dim3(QK_THREADS), 0, s, a);
-  else hipLaunchKernelGGL((qk_fwd_kernel<T, V, NU, PAIRS>), dim3(grid), dim3(QK_THREADS), 0, s, a);
+  if constexpr (BWD) hipLaunchKernelGGL((qk_bwd_kernel<T, V, NU, PAIRS>), dim3(grid), dim3(64 * QK_BWD_WAVES), 0, s, a);
+  else hipLaunchKernelGGL((qk_fwd_kernel<T, V, NU, PAIRS>), dim3(grid), dim3(64 * QK_WAVES), 0, s, a);
 }
 template <bool BWD, bool PAIRS>
 void launch_cut(const QkArgs& a, QkCut c, bool bf16, unsigned grid, hipStream_t s) {
   if (bf16) {
-    if (c.v == 8) launch_one<BWD, bf16_t, 8, 1, PAIRS>(a, grid, s);
-    else if (c.v == 4) launch_one<BWD, bf16_t, 4, 1, PAIRS>(a, grid, s);
+    if (c.v == 8) {
+      if constexpr (!BWD) launch_one<BWD, bf16_t, 8, 1, PAIRS>(a, grid, s);
+    } else if (c.v == 4) launch_one<BWD, bf16_t, 4, 1, PAIRS>(a, grid, s);
     else if (c.v == 2) launch_one<BWD, bf16_t, 2, 1, PAIRS>(a, grid, s);
     else if (c.nu == 1) launch_one<BWD, bf16_t, 1, 1, PAIRS>(a, grid, s);
     else launch_one<BWD, bf16_t, 1, 2, PAIRS>(a, grid, s);
@@ -489,7 +542,7 @@ int qk_rotary_fwd(const void* const* x, const void* const* gamma, const int* pos
            {s.ld_q, s.ld_k, s.ld_v}, {1, 1}, {s.ld_yq, s.ld_yk, s.ld_yv}};
   const int st = qk_args(a, s, bf16, false);
   if (st != KARMA_OK || !s.tokens) return st;
-  const QkCut c = cut(a, bf16, false);
+  const QkCut c = cut(a, bf16, s.flags & KARMA_QK_PAIRS, false);
   deal(a, c);
   const unsigned grid = (unsigned)(((uint64_t)a.tokens * a.parts + QK_WAVES - 1) / QK_WAVES);
   if (s.flags & KARMA_QK_PAIRS) launch_cut<false, true>(a, c, bf16, grid, stream);
@@ -506,7 +559,7 @@ int qk_rotary_bwd(const void* const* dy, const void* const* x, const void* const
   if (st != KARMA_OK) return st;
   const bool sums = dgamma[0] || dgamma[1];
   if (sums && (!a.norm || !aligned_to(dgamma[0], 4) || !aligned_to(dgamma[1], 4))) return KARMA_E_INVAL;
-  const QkCut c = cut(a, bf16, true);
+  const QkCut c = cut(a, bf16, s.flags & KARMA_QK_PAIRS, true);
   deal(a, c);
   const unsigned grid = s.tokens ? bwd_groups((uint64_t)a.tokens * a.parts) : 0;
   if (sums) {
