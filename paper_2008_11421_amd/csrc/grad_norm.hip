@@ -16,30 +16,24 @@ namespace {
 
 constexpr int GN_THREADS = 256;
 constexpr unsigned GN_GRID = (1u << 24) - 1;        // workgroups of 256 lanes in a launch, which has less than 2^32
-// Elements of a workgroup (norm).
-constexpr unsigned GN_SPAN = 16384, GN_SPAN_FEW = 4096;
-constexpr uint64_t GN_FEW = 16u << 20;
-constexpr unsigned GC_SPAN = 4096;                  // (clipping)
+constexpr unsigned GC_SPAN = 4096;                  // elements of a workgroup (clipping)
 static_assert(KARMA_GRAD_VALUES_MAX / GC_SPAN + 1 <= GN_GRID, "a tensor fits a launch");
 
-struct NormTensor {
-  const void* grad;
-  size_t n;             // the highest bit: bf16
-};
-struct NormSet {        // the tensors of one launch, as kernel arguments
-  static constexpr int MOST = 200;
-  NormTensor t[MOST];
+// The tensors of one launch travel as kernel arguments, 4 KB in all: addresses of 48 bits with what is known of them above, the elements of a
+// tensor's last workgroup, and the workgroups before it.
+constexpr uint64_t BIT_BF16 = 1ull << 63, ADDRESS = (1ull << 48) - 1;
+struct NormSet {
+  static constexpr int MOST = 288;
+  uint64_t grad[MOST];
   unsigned first[MOST + 1];     // tensor k has workgroups [first[k], first[k + 1])
+  unsigned short last[MOST];    // elements of its last one, less one
   int n;
 };
-struct ClipTensor {
-  const void* grad; void* out;
-  size_t n;             // the highest bits: bf16, out in bf16
-};
 struct ClipSet {
-  static constexpr int MOST = 144;
-  ClipTensor t[MOST];
+  static constexpr int MOST = 184;
+  uint64_t grad[MOST], out[MOST];
   unsigned first[MOST + 1];
+  unsigned short last[MOST];
   int n;
 };
 struct EachSet {        // tensor k has the partial sums [first[k], first[k + 1])
@@ -48,7 +42,6 @@ struct EachSet {        // tensor k has the partial sums [first[k], first[k + 1]
   int n;
 };
 static_assert(sizeof(NormSet) + 16 <= 4096 && sizeof(ClipSet) + 16 <= 4096 && sizeof(EachSet) + 64 <= 4096, "kernel arguments");
-constexpr size_t BIT_BF16 = (size_t)1 << 63, BIT_OUT = (size_t)1 << 62, BITS = BIT_BF16 | BIT_OUT;
 
 template <typename Set>
 __device__ __forceinline__ int tensor_of(const Set& u, unsigned block) {
@@ -97,29 +90,26 @@ struct Vec16<float> {
   static __device__ __forceinline__ float one(const float* p) { return *p; }
 };
 
+// The elements [skip, n) of a span behind `base`, which lies on a 16-byte boundary.
 template <typename T>
-__device__ __forceinline__ double squares(const T* g, size_t n, size_t at, unsigned span) {
+__device__ __forceinline__ double squares(const T* base, unsigned skip, unsigned n) {
   constexpr int N = Vec16<T>::N, BATCH = 4;
-  const unsigned skip = (unsigned)((uintptr_t)g % 16 / sizeof(T));
   double sum = 0.0, sum2 = 0.0;
-  const T* base = g - skip;
-  for (unsigned v = threadIdx.x * N; v < span; v += GN_THREADS * N * BATCH) {
+  for (unsigned v = threadIdx.x * N; v < n; v += GN_THREADS * N * BATCH) {
     u32x4 raw[BATCH];
-    bool whole[BATCH];
 #pragma unroll
     for (int b = 0; b < BATCH; ++b) {
-      const size_t i = at + v + b * (GN_THREADS * N);
-      whole[b] = v + b * (GN_THREADS * N) < span && i >= skip && i + N <= n + skip;
-      raw[b] = whole[b] ? *(const u32x4*)(base + i) : u32x4{0, 0, 0, 0};
+      const unsigned i = v + b * (GN_THREADS * N);
+      raw[b] = i >= skip && i + N <= n ? *(const u32x4*)(base + i) : u32x4{0, 0, 0, 0};
     }
 #pragma unroll
     for (int b = 0; b < BATCH; ++b) {
-      const size_t i = at + v + b * (GN_THREADS * N);
+      const unsigned i = v + b * (GN_THREADS * N);
       float f[N];
       Vec16<T>::unpack(raw[b], f);
-      if (!whole[b] && v + b * (GN_THREADS * N) < span) {
+      if (i < n && (i < skip || i + N > n)) {
 #pragma unroll
-        for (int e = 0; e < N; ++e) f[e] = i + e >= skip && i + e < n + skip ? Vec16<T>::one(base + i + e) : 0.f;
+        for (int e = 0; e < N; ++e) f[e] = i + e >= skip && i + e < n ? Vec16<T>::one(base + i + e) : 0.f;
       }
 #pragma unroll
       for (int e = 0; e < N; e += 2) {
@@ -130,12 +120,31 @@ __device__ __forceinline__ double squares(const T* g, size_t n, size_t at, unsig
   }
   return sum + sum2;
 }
+// Workgroup `block` of tensor k: its elements [skip, n) behind *base.
+template <typename T, typename Set>
+__device__ __forceinline__ const T* span_of(const Set& u, int k, unsigned block, unsigned span, unsigned& skip, unsigned& n) {
+  const T* g = (const T*)(uintptr_t)(u.grad[k] & ADDRESS);
+  const unsigned before = (unsigned)((uintptr_t)g % 16 / sizeof(T)), at = block - u.first[k];
+  skip = at ? 0 : before;
+  n = block + 1 == u.first[k + 1] ? u.last[k] + 1u : span;
+  return g - before + (size_t)at * span;
+}
 
+// Reads every value once, with a conversion and a product-and-sum of 64 bits for each: bound by memory (217 M values in bf16 72 us, 6.0 TB/s) and, in
+// lists of many tensors, by launches of 288 tensors that drain one after the other (609 tensors of 63 M values 44 us).  A search of the workgroup's
+// tensor by all lanes at once instead of step by step made no difference.
 // partial[workgroup] = the sum of squares of `span` elements of one tensor
 __global__ __launch_bounds__(GN_THREADS) void grad_squares_kernel(NormSet u, unsigned span, double* partial) {
   const int k = tensor_of(u, blockIdx.x);
-  const size_t n = u.t[k].n & ~BITS, at = (size_t)(blockIdx.x - u.first[k]) * span;
-  double s = u.t[k].n & BIT_BF16 ? squares((const bf16_t*)u.t[k].grad, n, at, span) : squares((const float*)u.t[k].grad, n, at, span);
+  unsigned skip, n;
+  double s;
+  if (u.grad[k] & BIT_BF16) {
+    const bf16_t* g = span_of<bf16_t>(u, k, blockIdx.x, span, skip, n);
+    s = squares(g, skip, n);
+  } else {
+    const float* g = span_of<float>(u, k, blockIdx.x, span, skip, n);
+    s = squares(g, skip, n);
+  }
   s = block_sum64<GN_THREADS / 64>(s);
   if (threadIdx.x == 0) partial[blockIdx.x] = s;
 }
@@ -169,30 +178,32 @@ __global__ __launch_bounds__(FIN_THREADS) void grad_finish_kernel(EachSet u, con
   if (threadIdx.x % 64 == 0) o.each[k] = (float)((double)o.scale * sqrt(s));
 }
 
+// Reads and writes every value once: 5.0 to 5.3 TB/s (609 tensors of 63 M values in bf16 50 us in four launches, 15.8 M from fp32 to bf16 17.7 us).
+// Workgroups in falling order, which find more of what the norm has read last in the cache, took as long.
 template <typename T, typename O>
-__device__ __forceinline__ void clip_span(const T* g, O* out, size_t n, size_t at, float factor) {
+__device__ __forceinline__ void clip_span(const ClipSet& u, int k, unsigned block, float factor) {
   constexpr int N = Vec16<T>::N, BATCH = GC_SPAN / (GN_THREADS * N);
-  const unsigned skip = (unsigned)((uintptr_t)g % 16 / sizeof(T));
-  const T* base = g - skip;
-  O* to = out - skip;
+  unsigned skip, n;
+  const T* base = span_of<T>(u, k, block, GC_SPAN, skip, n);
+  O* to = (O*)(uintptr_t)(u.out[k] & ADDRESS) + (base - (const T*)(uintptr_t)(u.grad[k] & ADDRESS));
   constexpr size_t OUT_BYTES = N * sizeof(O) < 16 ? N * sizeof(O) : 16;
   const bool fits = (uintptr_t)to % OUT_BYTES == 0;
   u32x4 raw[BATCH];
 #pragma unroll
   for (int b = 0; b < BATCH; ++b) {
-    const size_t i = at + (threadIdx.x + b * GN_THREADS) * N;
-    raw[b] = i >= skip && i + N <= n + skip ? *(const u32x4*)(base + i) : u32x4{0, 0, 0, 0};
+    const unsigned i = (threadIdx.x + b * GN_THREADS) * N;
+    raw[b] = i >= skip && i + N <= n ? *(const u32x4*)(base + i) : u32x4{0, 0, 0, 0};
   }
 #pragma unroll
   for (int b = 0; b < BATCH; ++b) {
-    const size_t i = at + (threadIdx.x + b * GN_THREADS) * N;
-    if (i >= n + skip) continue;
-    const bool whole = i >= skip && i + N <= n + skip;
+    const unsigned i = (threadIdx.x + b * GN_THREADS) * N;
+    if (i >= n) continue;
+    const bool whole = i >= skip && i + N <= n;
     float f[N];
     Vec16<T>::unpack(raw[b], f);
     if (!whole) {
 #pragma unroll
-      for (int e = 0; e < N; ++e) f[e] = i + e >= skip && i + e < n + skip ? Vec16<T>::one(base + i + e) : 0.f;
+      for (int e = 0; e < N; ++e) f[e] = i + e >= skip && i + e < n ? Vec16<T>::one(base + i + e) : 0.f;
     }
 #pragma unroll
     for (int e = 0; e < N; ++e) f[e] *= factor;
@@ -208,7 +219,7 @@ __device__ __forceinline__ void clip_span(const T* g, O* out, size_t n, size_t a
     } else {
 #pragma unroll
       for (int e = 0; e < N; ++e)
-        if (i + e >= skip && i + e < n + skip) {
+        if (i + e >= skip && i + e < n) {
           if constexpr (sizeof(O) == 2) to[i + e] = f2bf(f[e]);
           else to[i + e] = f[e];
         }
@@ -217,19 +228,17 @@ __device__ __forceinline__ void clip_span(const T* g, O* out, size_t n, size_t a
 }
 
 __global__ __launch_bounds__(GN_THREADS) void grad_clip_kernel(ClipSet u, const float* factor) {
-  const int k = tensor_of(u, blockIdx.x);
-  const size_t bits = u.t[k].n, n = bits & ~BITS, at = (size_t)(blockIdx.x - u.first[k]) * GC_SPAN;
-  const void* g = u.t[k].grad;
-  void* out = u.t[k].out;
+  const unsigned block = blockIdx.x;
+  const int k = tensor_of(u, block);
   const float f = *factor;
-  const bool gbf = bits & BIT_BF16, obf = bits & BIT_OUT;
-  if (f == 1.f && g == out && gbf == obf) return;      // nothing changes
+  const bool gbf = u.grad[k] & BIT_BF16, obf = u.out[k] & BIT_BF16;
+  if (f == 1.f && u.grad[k] == u.out[k]) return;      // nothing changes
   if (gbf) {
-    if (obf) clip_span((const bf16_t*)g, (bf16_t*)out, n, at, f);
-    else clip_span((const bf16_t*)g, (float*)out, n, at, f);
+    if (obf) clip_span<bf16_t, bf16_t>(u, k, block, f);
+    else clip_span<bf16_t, float>(u, k, block, f);
   } else {
-    if (obf) clip_span((const float*)g, (bf16_t*)out, n, at, f);
-    else clip_span((const float*)g, (float*)out, n, at, f);
+    if (obf) clip_span<float, bf16_t>(u, k, block, f);
+    else clip_span<float, float>(u, k, block, f);
   }
 }
 
@@ -241,20 +250,22 @@ bool good_grads(const karma_grad_tensor* tensors, uint32_t n) {
   for (uint32_t k = 0; k < n; ++k) {
     const karma_grad_tensor& t = tensors[k];
     if ((t.flags & ~3u) || t.n > KARMA_GRAD_VALUES_MAX) return false;
-    if (t.n && (!t.grad || !aligned_to(t.grad, grad_size(t)))) return false;
+    if (t.n && (!t.grad || !aligned_to(t.grad, grad_size(t)) || (uintptr_t)t.grad > ADDRESS)) return false;
     all += t.n;
     if (all > KARMA_GRAD_VALUES_MAX) return false;
   }
   return true;
 }
 // vectors begin up to one vector before the tensor
-uint64_t spans(const karma_grad_tensor& t, unsigned span) {
-  return t.n ? (t.n + (uintptr_t)t.grad % 16 / grad_size(t) + span - 1) / span : 0;
-}
+uint64_t extent(const karma_grad_tensor& t) { return t.n ? t.n + (uintptr_t)t.grad % 16 / grad_size(t) : 0; }
+uint64_t spans(const karma_grad_tensor& t, unsigned span) { return (extent(t) + span - 1) / span; }
+uint64_t address(const void* p, bool bf16) { return ((uint64_t)(uintptr_t)p & ADDRESS) | (bf16 ? BIT_BF16 : 0); }
+// Elements of a workgroup: few where workgroups are few (16 tensors of 0.5 M values in all 4.2 us in the kernel), more in long lists, for
+// fewer sums to add up (one of 217 M in workgroups of 16384 / 32768: 76.6 / 78.7 us; 609 tensors of 63 M, clipped, of 8192 / 16384 / 32768: 99 / 100 / 101).
 unsigned norm_span(const karma_grad_tensor* tensors, uint32_t n) {
   uint64_t all = 0;
   for (uint32_t k = 0; k < n; ++k) all += tensors[k].n;
-  return all > GN_FEW ? GN_SPAN : GN_SPAN_FEW;
+  return all <= 16u << 20 ? 4096 : 16384;
 }
 
 }  // namespace
@@ -285,7 +296,8 @@ int grad_norm(const karma_grad_tensor* tensors, uint32_t n, float max_norm, floa
       const uint64_t more = spans(tensors[k], span);
       if (!more) continue;
       if (blocks + more > GN_GRID) break;
-      u.t[u.n] = NormTensor{tensors[k].grad, tensors[k].n | (tensors[k].flags & KARMA_GRAD_BF16 ? BIT_BF16 : 0)};
+      u.grad[u.n] = address(tensors[k].grad, tensors[k].flags & KARMA_GRAD_BF16);
+      u.last[u.n] = (unsigned short)((extent(tensors[k]) - 1) % span);
       blocks += more;
       u.first[++u.n] = (unsigned)blocks;
     }
@@ -317,7 +329,7 @@ int grad_norm(const karma_grad_tensor* tensors, uint32_t n, float max_norm, floa
 int grad_clip(const karma_grad_tensor* tensors, uint32_t n, const float* factor, hipStream_t s) {
   if (!good_grads(tensors, n) || !factor || !aligned_to(factor, 4)) return KARMA_E_INVAL;
   for (uint32_t k = 0; k < n; ++k)
-    if (tensors[k].n && (!tensors[k].out || !aligned_to(tensors[k].out, tensors[k].flags & KARMA_GRAD_OUT_BF16 ? 2 : 4))) return KARMA_E_INVAL;
+    if (tensors[k].n && (!tensors[k].out || (uintptr_t)tensors[k].out > ADDRESS || !aligned_to(tensors[k].out, tensors[k].flags & KARMA_GRAD_OUT_BF16 ? 2 : 4))) return KARMA_E_INVAL;
   bool launched = false;
   for (uint32_t k = 0; k < n;) {
     ClipSet u;
@@ -329,7 +341,9 @@ int grad_clip(const karma_grad_tensor* tensors, uint32_t n, const float* factor,
       const uint64_t more = spans(t, GC_SPAN);
       if (!more) continue;
       if (blocks + more > GN_GRID) break;
-      u.t[u.n] = ClipTensor{t.grad, t.out, t.n | (t.flags & KARMA_GRAD_BF16 ? BIT_BF16 : 0) | (t.flags & KARMA_GRAD_OUT_BF16 ? BIT_OUT : 0)};
+      u.grad[u.n] = address(t.grad, t.flags & KARMA_GRAD_BF16);
+      u.out[u.n] = address(t.out, t.flags & KARMA_GRAD_OUT_BF16);
+      u.last[u.n] = (unsigned short)((extent(t) - 1) % GC_SPAN);
       blocks += more;
       u.first[++u.n] = (unsigned)blocks;
     }
