@@ -72,19 +72,22 @@ struct RowVec<float> {
 // rint(2^40 2^(d c)), d <= 0: 2^f on [-1/2, 1/2] as 1 + f q(f), q through the Chebyshev nodes, off by 2^-50 of itself; d = 0 gives 2^40.
 // Rounding to whole numbers is done by adding and subtracting 1.5 2^52 and 2^52, and the power of two goes into the exponent's bits: 64-bit
 // additions and products run at the rate of 32-bit ones.
-__device__ __forceinline__ double weight_of(double d, double c) {
+// The coefficients are kept in scalar registers: from literals each product-and-sum is preceded by a move (OLDNEW).
+struct Exp2 {
+  double q[10];
+  __device__ __forceinline__ Exp2()
+      : q{0x1.62e42fefa39f7p-1, 0x1.ebfbdff82c590p-3, 0x1.c6b08d7044119p-5, 0x1.3b2ab6fba385fp-7, 0x1.5d87fe908f88ap-10, 0x1.4309130378460p-13,
+          0x1.ffcb76789860fp-17, 0x1.62bfe46117445p-20, 0x1.b6571de2f2351p-24, 0x1.e5e9f548e5726p-28} {
+#pragma unroll
+    for (int i = 0; i < 10; ++i) asm volatile("" : "+s"(q[i]));
+  }
+};
+__device__ __forceinline__ double weight_of(const Exp2& k, double d, double c) {
   constexpr double WHOLE = 0x1.8p52, POSITIVE = 0x1p52;
   const double y = fmax(fma(d, c, 40.0), -24.0), t = y + WHOLE, f = y - (t - WHOLE);
-  double q = 0x1.e5e9f548e5726p-28;
-  q = fma(q, f, 0x1.b6571de2f2351p-24);
-  q = fma(q, f, 0x1.62bfe46117445p-20);
-  q = fma(q, f, 0x1.ffcb76789860fp-17);
-  q = fma(q, f, 0x1.4309130378460p-13);
-  q = fma(q, f, 0x1.5d87fe908f88ap-10);
-  q = fma(q, f, 0x1.3b2ab6fba385fp-7);
-  q = fma(q, f, 0x1.c6b08d7044119p-5);
-  q = fma(q, f, 0x1.ebfbdff82c590p-3);
-  q = fma(q, f, 0x1.62e42fefa39f7p-1);
+  double q = k.q[9];
+#pragma unroll
+  for (int i = 8; i >= 0; --i) q = fma(q, f, k.q[i]);
   q = fma(q, f, 1.0);
   const double w = __hiloint2double(__double2hiint(q) + (__double2loint(t) << 20), __double2loint(q));
   return (w + POSITIVE) - POSITIVE;
@@ -156,6 +159,7 @@ struct Sampler {
   int lane, wave;
   float m;                  // the largest logit
   double c;                 // log2 e / temperature
+  Exp2 exp2;
 
   __device__ __forceinline__ Sampler(SampleShared& shared, const SampleArgs& a) : sh(shared) {
     row = (const T*)a.logits + (size_t)blockIdx.x * a.ld;
@@ -214,7 +218,7 @@ struct Sampler {
       for (int e = 0; e < N; ++e) f(z[e]);
     });
   }
-  __device__ __forceinline__ double weight(float z) const { return weight_of((double)z - (double)m, c); }
+  __device__ __forceinline__ double weight(float z) const { return weight_of(exp2, (double)z - (double)m, c); }
 
   // sums over the wavefronts, which are in sh.total: those before this one, and all
   __device__ __forceinline__ u64 totals(u64& all) const {
