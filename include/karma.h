@@ -759,15 +759,15 @@ int karma_k_qk_rotary_bwd_f32(const float* dyq_dev, const float* dyk_dev, const 
  * In the order of falling logits, equal ones by rising index, there stay: the first top_k tokens (0: all); of these the shortest
  * beginning whose weights reach top_p times theirs (at least one; top_p 1 or more: all); of these the tokens with w_j >= min_p 2^40
  * (at least the first), and of these those with w_j > 0.  Their weights, summed up by rising index, first exceed uniform_dev[row] times their sum,
- * rounded down, at the token drawn; uniform fp32 in [0, 1) (less counts as 0, more as the last token).  temperature 0: the first of the largest.
+ * rounded down, at the token drawn; uniform fp32 in [0, 1) (less, and NaN, counts as 0, more as the last token).  temperature 0: the first of the largest.
  * (The products with top_p and uniform are rounded to 64-bit floating point.)
  * Outputs, each NULL where it is not wanted (not all of them): token_dev int32 [rows]; logprob_dev fp32 [rows], the logarithm of the token's share of
  * what stays; kept_dev int32 [rows], how many tokens stay.
  * A logit of -inf has no weight.  A row without answer (NaN or +inf in it, nothing but -inf; a rule with a temperature that is negative, infinite or
  * NaN, or a NaN in top_p or min_p) gives token -1, logprob NaN and kept 0.
- * ws_dev: karma_k_sample_ws_bytes(rows, cols) bytes, 16-byte aligned, for one call at a time (0 bytes: may be NULL).
+ * ws_dev: karma_k_sample_ws_bytes(rows, cols) bytes, 16-byte aligned, for one call at a time (none at present: 0 bytes, may be NULL).
  * cols up to KARMA_SAMPLE_COLS_MAX, rows < 2^20.  Errors: KARMA_E_INVAL (operands off their elements' boundaries among them), KARMA_E_OOM. */
-#define KARMA_SAMPLE_COLS_MAX ((1u << 22) - 1)
+#define KARMA_SAMPLE_COLS_MAX ((1u << 21) - 1)
 typedef struct {
   float temperature, top_p, min_p;
   uint32_t top_k;

@@ -23,7 +23,7 @@ PRODUCT_STAGED_SMALL, PRODUCT_STAGED_LARGE, PRODUCT_SMALL, PRODUCT_LARGE, PRODUC
 PRODUCT_SLICES, PRODUCT_BROAD, PRODUCT_FLAT, PLAN_TILES = 5, 6, 7, 1 << 31
 SCAN_MARK, TOP_MAX = 256, 64
 QK_NORM, QK_PAIRS, QK_D_MAX = 1, 2, 256
-SAMPLE_COLS_MAX = (1 << 22) - 1
+SAMPLE_COLS_MAX = (1 << 21) - 1
 GRAD_BF16, GRAD_OUT_BF16 = 1, 2
 ADAMW_GRAD_BF16, ADAMW_OUT_BF16, ADAMW_STATES_8BIT, ADAMW_BLOCK = 1, 2, 4, 64
 CONV_FWD, CONV_DGRAD, CONV_WGRAD, CONV_KEEP_SUMS = 0, 1, 2, 4

@@ -18,6 +18,8 @@ namespace {
 
 typedef unsigned long long u64;
 constexpr unsigned SP_GRID = 1u << 20;
+// (a thread's sum of weights is a whole number of 64-bit floating point: 2^12 of up to 2^40 each in rows of the largest size)
+static_assert(KARMA_SAMPLE_COLS_MAX / 512 < 1u << 12, "exact sums");
 constexpr int BINS = 2048, LAST = BINS - 1;
 constexpr double ONE = 1099511627776.0;     // 2^40
 // bins reach down to weights of 2^-42 of the largest: what falls into the last one weighs nothing
@@ -69,10 +71,11 @@ struct RowVec<float> {
   static __device__ __forceinline__ float value(unsigned key) { return __uint_as_float((int)key < 0 ? key & 0x7fffffffu : ~key); }
 };
 
-// rint(2^40 2^(d c)), d <= 0: 2^f on [-1/2, 1/2] as 1 + f q(f), q through the Chebyshev nodes, off by 2^-50 of itself; d = 0 gives 2^40.
-// Rounding to whole numbers is done by adding and subtracting 1.5 2^52 and 2^52, and the power of two goes into the exponent's bits: 64-bit
-// additions and products run at the rate of 32-bit ones.
-// The coefficients are kept in scalar registers: from literals each product-and-sum is preceded by a move (OLDNEW).
+// rint(2^40 2^(d c)) as a whole number, d <= 0: 2^f on [-1/2, 1/2] as 1 + f q(f), q through the Chebyshev nodes, off by 2^-50 of itself; d = 0 gives 2^40.
+// Rounding to whole numbers is done by adding 1.5 2^52 and 2^52, which leaves the number in the lower bits, and the power of two goes into the
+// exponent's bits: 64-bit additions and products run at the rate of 32-bit ones, conversions take several operations.
+// The coefficients are kept in scalar registers: from literals each product-and-sum is preceded by a move (4096 x 32000 with
+// top_p 168 -> 157 us).
 struct Exp2 {
   double q[10];
   __device__ __forceinline__ Exp2()
@@ -82,7 +85,7 @@ struct Exp2 {
     for (int i = 0; i < 10; ++i) asm volatile("" : "+s"(q[i]));
   }
 };
-__device__ __forceinline__ double weight_of(const Exp2& k, double d, double c) {
+__device__ __forceinline__ u64 weight_of(const Exp2& k, double d, double c) {
   constexpr double WHOLE = 0x1.8p52, POSITIVE = 0x1p52;
   const double y = fmax(fma(d, c, 40.0), -24.0), t = y + WHOLE, f = y - (t - WHOLE);
   double q = k.q[9];
@@ -90,7 +93,8 @@ __device__ __forceinline__ double weight_of(const Exp2& k, double d, double c) {
   for (int i = 8; i >= 0; --i) q = fma(q, f, k.q[i]);
   q = fma(q, f, 1.0);
   const double w = __hiloint2double(__double2hiint(q) + (__double2loint(t) << 20), __double2loint(q));
-  return (w + POSITIVE) - POSITIVE;
+  const double sum = w + POSITIVE;
+  return (u64)((unsigned)__double2hiint(sum) & 0xfffffu) << 32 | (unsigned)__double2loint(sum);
 }
 
 // 64-bit sums over a wavefront by data-parallel-primitive moves (six reads through the LDS crossbar, twice over, take 700 cycles)
@@ -218,7 +222,7 @@ struct Sampler {
       for (int e = 0; e < N; ++e) f(z[e]);
     });
   }
-  __device__ __forceinline__ double weight(float z) const { return weight_of(exp2, (double)z - (double)m, c); }
+  __device__ __forceinline__ u64 weight(float z) const { return weight_of(exp2, (double)z - (double)m, c); }
 
   // sums over the wavefronts, which are in sh.total: those before this one, and all
   __device__ __forceinline__ u64 totals(u64& all) const {
@@ -412,6 +416,70 @@ struct BinSampler : Sampler<T, THREADS> {
     return this->block_sum(v);
   }
 
+  // The border within a bin: its logits, between `least` and `most`, are put into a list, and a thread adds up what is above one of them.  False if
+  // there are more than the list holds.  (1 x 128000 in fp32 with top_p 121 -> 95 us.)
+  struct Members {
+    static constexpr unsigned MOST = THREADS < 512 ? THREADS : 512;
+    float logit[MOST];
+    u64 weight[MOST], mass[MOST];
+    unsigned above[MOST], equal[MOST], n;
+    Border border;
+    u64 stays;
+  };
+  static_assert(sizeof(Members) <= sizeof(Bins), "room");
+  __device__ __forceinline__ bool among(unsigned b, float least, float most, bool by_mass, bool weigh, u64 need, Border& out, u64& stays) const {
+    Members& l = *(Members*)&fine;
+    const unsigned tid = threadIdx.x;
+    __syncthreads();
+    if (tid == 0) l.n = 0;
+    __syncthreads();
+    this->template each<S::LIGHT>([&](float z) {
+      if (z <= most && z >= least && bin(z) == (int)b) {
+        const unsigned i = atomicAdd(&l.n, 1u);
+        if (i < Members::MOST) l.logit[i] = z;
+      }
+    });
+    __syncthreads();
+    const unsigned n = l.n;
+    if (!n || n > Members::MOST) return false;
+    if (tid < Members::MOST) {
+      l.weight[tid] = tid < n ? this->weight(l.logit[tid]) : 0;
+      l.mass[tid] = 0; l.above[tid] = 0; l.equal[tid] = 0;
+    }
+    __syncthreads();
+    const unsigned group = n <= 64 ? 64 : n <= 128 ? 128 : n <= 256 ? 256 : 512, me = tid % group;
+    const float z = l.logit[min(me, n - 1)];
+    unsigned above = 0, equal = 0;
+    u64 mass = 0;
+#pragma unroll 4
+    for (unsigned j = tid / group; j < n; j += THREADS / group) {
+      const float other = l.logit[j];
+      const u64 w = l.weight[j];
+      above += other > z;
+      mass += other > z ? w : 0;
+      equal += other == z;
+    }
+    if (me < n) {
+      if (above) { atomicAdd(&l.above[me], above); atomicAdd(&l.mass[me], mass); }
+      if (equal) atomicAdd(&l.equal[me], equal);
+    }
+    __syncthreads();
+    if (tid < n) {
+      // (the threads of equal logits write the same)
+      const u64 w = l.weight[tid], before = by_mass ? l.mass[tid] : l.above[tid], own = by_mass ? w * l.equal[tid] : l.equal[tid];
+      if (before < need && before + own >= need) {
+        const unsigned ties = (unsigned)(by_mass ? (need - before + w - 1) / w : need - before);
+        l.border = Border{z, ties, w};
+        l.stays = l.mass[tid] + ties * w;
+      }
+    }
+    __syncthreads();
+    out = l.border;
+    if (weigh) stays += l.stays;
+    __syncthreads();
+    return true;
+  }
+
   // The border behind the token at which count (or mass) reaches `need`, and what stays up to it weighs (0 without `weigh`): false if all that
   // weighs anything stays.
   __device__ __forceinline__ bool border(bool by_mass, bool weigh, u64 need, Border& out, u64& stays) const {
@@ -422,7 +490,9 @@ struct BinSampler : Sampler<T, THREADS> {
     need -= before;
     // the keys of the bin, and some beside them: roundings move a logit by less than `slack`
     const float near = (float)b / s, far = (float)(b + 1) / s, slack = (fabsf(this->m) + far) * 0x1p-20f;
-    unsigned hi = R::key(fminf(this->m - near + slack, this->m)), lo = R::key(fmaxf(this->m - far - slack, -3.4028234e38f));
+    const float most = fminf(this->m - near + slack, this->m), least = fmaxf(this->m - far - slack, -3.4028234e38f);
+    if (among(b, least, most, by_mass, weigh, need, out, stays)) return true;
+    unsigned hi = R::key(most), lo = R::key(least);
     for (;;) {
       const unsigned range = hi - lo, shift = range < BINS ? 0 : 32 - __clz(range) - 11;
       clear(fine);
@@ -431,7 +501,7 @@ struct BinSampler : Sampler<T, THREADS> {
         if (k >= lo && k <= hi && bin(z) == (int)b) {
           const unsigned at = (hi - k) >> shift;
           atomicAdd(&fine.count[at], 1u);
-          if (weigh) atomicAdd(&fine.mass[at], (u64)this->weight(z));
+          if (weigh) atomicAdd(&fine.mass[at], this->weight(z));
         }
       });
       unsigned at;
@@ -442,7 +512,7 @@ struct BinSampler : Sampler<T, THREADS> {
       if (!shift) {
         // `need` of the bin's tokens, which weigh the same
         out.logit = R::value(top);
-        out.weight = (u64)this->weight(out.logit);
+        out.weight = this->weight(out.logit);
         out.ties = (unsigned)(by_mass ? (need + out.weight - 1) / out.weight : need);
         stays += out.ties * out.weight;
         __syncthreads();
@@ -455,7 +525,7 @@ struct BinSampler : Sampler<T, THREADS> {
 };
 
 template <typename T, int THREADS>
-__device__ __forceinline__ void sample_by_bins(const SampleArgs& a, const karma_sample_rule& rule, float uniform, double least, const Sampler<T, THREADS>& base,
+__device__ __forceinline__ void sample_by_bins(const SampleArgs& a, const karma_sample_rule& rule, float uniform, u64 least, const Sampler<T, THREADS>& base,
                                                Bins* bins) {
   BinSampler<T, THREADS> p(base, bins);
   float own;
@@ -465,51 +535,51 @@ __device__ __forceinline__ void sample_by_bins(const SampleArgs& a, const karma_
   Border border{-INFINITY, 0, 0};
   if (by_count || by_mass) {
     p.clear(p.coarse);
-    double mine = 0.0;
+    u64 mine = 0;
     p.each([&](float z) {
       const int b = p.bin(z);
       if (b < LAST) {
         if (by_count) atomicAdd(&p.coarse.count[b], 1u);
         if (by_mass) {
-          const double w = p.weight(z);
+          const u64 w = p.weight(z);
           mine += w;
-          atomicAdd(&p.coarse.mass[b], (u64)w);
+          atomicAdd(&p.coarse.mass[b], w);
         }
       }
     });
-    u64 all = by_mass ? p.block_sum((u64)mine) : 0, stays;
+    u64 all = by_mass ? p.block_sum(mine) : 0, stays;
     if (by_count && p.border(false, by_mass, rule.top_k, border, stays)) all = stays;
     if (by_mass) p.border(true, true, top_p_need(rule.top_p, all), border, stays);
   }
   // (the border's weight may be below min-p's: then none of its tokens stays)
-  if ((double)border.weight < least) border.ties = 0;
+  if (border.weight < least) border.ties = 0;
   auto drawn = [&](float z, u64& w) {
     if (z == border.logit) return true;
     if (z > border.logit) {
-      const double v = p.weight(z);
-      w = v >= least ? (u64)v : 0;
+      const u64 v = p.weight(z);
+      w = v >= least ? v : 0;
     }
     return false;
   };
-  double mine = 0.0;
+  u64 mine = 0;
   unsigned count = 0, ties = 0;
-  if (border.logit == -INFINITY && least <= 0.0) {      // all stays
+  if (border.logit == -INFINITY && !least) {      // all stays
     p.each([&](float z) {
-      const double w = p.weight(z);
+      const u64 w = p.weight(z);
       mine += w;
-      count += w > 0.0;
+      count += w != 0;
     });
   } else {
     p.each([&](float z) {
       if (z > border.logit) {
-        const double w = p.weight(z);
-        if (w >= least) { mine += w; count += w > 0.0; }
+        const u64 w = p.weight(z);
+        if (w >= least) { mine += w; count += w != 0; }
       }
       ties += z == border.logit;
     });
   }
   unsigned kept = (unsigned)p.block_sum(count) + (border.weight ? border.ties : 0);
-  p.leave((u64)mine, ties);
+  p.leave(mine, ties);
   u64 all;
   p.totals(all);
   all += border.ties * border.weight;
@@ -530,7 +600,7 @@ struct List {
 };
 // false: the row has to go another way
 template <typename T, int THREADS>
-__device__ __forceinline__ bool sample_by_list(const SampleArgs& a, const karma_sample_rule& rule, float uniform, double least, Sampler<T, THREADS>& p, List& l) {
+__device__ __forceinline__ bool sample_by_list(const SampleArgs& a, const karma_sample_rule& rule, float uniform, u64 least, Sampler<T, THREADS>& p, List& l) {
   constexpr int N = RowVec<T>::N, WAVES = THREADS / 64;
   const int tid = threadIdx.x;
   for (int i = tid; i < BINS; i += THREADS) l.count[i] = 0;
@@ -585,7 +655,7 @@ __device__ __forceinline__ bool sample_by_list(const SampleArgs& a, const karma_
   const unsigned n = l.n;
   if (n > LIST_MOST) return false;
   const bool mine = tid < (int)n;
-  const u64 weight = mine ? (u64)p.weight(l.logit[tid]) : 0;
+  const u64 weight = mine ? p.weight(l.logit[tid]) : 0;
   if (tid < (int)LIST_MOST) { l.weight[tid] = weight; l.rank[tid] = 0; l.before[tid] = 0; l.drawn_before[tid] = 0; }
   __syncthreads();
   // pairs: a token of the list for every thread of a group, and the groups share the others
@@ -613,7 +683,7 @@ __device__ __forceinline__ bool sample_by_list(const SampleArgs& a, const karma_
     const u64 need = top_p_need(rule.top_p, p.block_sum(stays ? weight : 0));
     stays = stays && before < need;
   }
-  stays = stays && weight && (double)weight >= least;
+  stays = stays && weight && weight >= least;
   // 256 tokens weigh 2^48 at most: their number above that, in the same sum
   const u64 sums = p.block_sum(stays ? weight + (1ull << 52) : 0), total = sums & ((1ull << 52) - 1), target = draw_target(uniform, total);
   if (tid < (int)LIST_MOST) l.weight[tid] = stays ? weight : 0;
@@ -681,7 +751,7 @@ constexpr unsigned CT_TABLE = SAMPLE_ROOM / sizeof(double);
 
 // false: the row has to go by bins
 template <int THREADS>
-__device__ __forceinline__ bool sample_by_counters(const SampleArgs& a, const karma_sample_rule& rule, float uniform, double least, Sampler<bf16_t, THREADS>& p,
+__device__ __forceinline__ bool sample_by_counters(const SampleArgs& a, const karma_sample_rule& rule, float uniform, u64 least, Sampler<bf16_t, THREADS>& p,
                                                    Counted& ct) {
   typedef Sampler<bf16_t, THREADS> S;
   constexpr int WAVES = S::WAVES, AHEAD = THREADS == 1024 ? 8 : 4;
@@ -796,13 +866,13 @@ __device__ __forceinline__ bool sample_by_counters(const SampleArgs& a, const ka
     }
   };
   // (ranks before the first one have no tokens)
-  auto rank_weight = [&](unsigned rank) { return (u64)p.weight(fminf(rank_value(rank), p.m)); };
+  auto rank_weight = [&](unsigned rank) { return p.weight(fminf(rank_value(rank), p.m)); };
   sweep([&](unsigned g, const unsigned* r, const unsigned* n) {
     u64 w = 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) w += n[j] * rank_weight(r[j]);
     if (g == ZERO_GROUP)
-      for (unsigned i = lane % 16; i < tiny; i += 16) w += (u64)p.weight(bf2f(ct.tiny_bits[i]));
+      for (unsigned i = lane % 16; i < tiny; i += 16) w += p.weight(bf2f(ct.tiny_bits[i]));
     w += dpp_u64<0xB1, 0xf>(w);
     w += dpp_u64<0x4E, 0xf>(w);
     w += dpp_u64<0x141, 0xf>(w);
@@ -849,7 +919,7 @@ __device__ __forceinline__ bool sample_by_counters(const SampleArgs& a, const ka
   __syncthreads();
   const unsigned border = ct.border;
   unsigned ties = ct.ties, kept = ct.count_stays;
-  if (ct.border_weight && least <= 0.0) all = ct.stays;
+  if (ct.border_weight && !least) all = ct.stays;
   else {
     u64 sum = 0;
     unsigned number = 0;
@@ -858,26 +928,25 @@ __device__ __forceinline__ bool sample_by_counters(const SampleArgs& a, const ka
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const unsigned some = r[j] < border ? n[j] : r[j] == border ? min(n[j], ties) : 0;
-        const double w = p.weight(fminf(rank_value(r[j]), p.m));
-        if (w >= least && w > 0.0) { sum += some * (u64)w; number += some; }
+        const u64 w = p.weight(fminf(rank_value(r[j]), p.m));
+        if (w >= least && w) { sum += some * w; number += some; }
       }
       if (g == ZERO_GROUP)
         for (unsigned i = lane % 16; i < tiny; i += 16) {
-          const double w = p.weight(bf2f(ct.tiny_bits[i]));
-          if (w >= least && w > 0.0) { sum += (u64)w; ++number; }
+          const u64 w = p.weight(bf2f(ct.tiny_bits[i]));
+          if (w >= least && w) { sum += w; ++number; }
         }
     });
     kept = (unsigned)p.block_sum(number);
     all = p.block_sum(sum);
   }
   const Search s{draw_target(uniform, all), ties};
-  const double limit = p.weight(rank_value(border));
-  const u64 tie_weight = limit >= least ? (u64)limit : 0;
+  const u64 limit = p.weight(rank_value(border)), tie_weight = limit >= least ? limit : 0;
   const unsigned span = border - first;
   const float z_border = rank_value(border);
   auto weigh = [&](float z) {
-    const double w = p.weight(z);
-    return w >= least ? w : 0.0;
+    const u64 w = p.weight(z);
+    return w >= least ? w : 0;
   };
   if (span + 2 <= CT_TABLE) {
     // The weights of the ranks that stay, where the counters were; a mark for the border's; and a 0 behind them that all others read: a read
@@ -885,7 +954,7 @@ __device__ __forceinline__ bool sample_by_counters(const SampleArgs& a, const ka
     constexpr double MARK = 0x1p47;
     double* table = (double*)&ct;
     __syncthreads();
-    for (unsigned i = tid; i <= span + 1; i += THREADS) table[i] = i < span ? weigh(rank_value(first + i)) : i == span ? MARK : 0.0;
+    for (unsigned i = tid; i <= span + 1; i += THREADS) table[i] = i < span ? (double)weigh(rank_value(first + i)) : i == span ? MARK : 0.0;
     __syncthreads();
     u64 sum = 0;
     unsigned number = 0;
@@ -923,26 +992,26 @@ __device__ __forceinline__ bool sample_by_counters(const SampleArgs& a, const ka
       auto of = [&](unsigned u) { return table[min(rank_of(u) - first, span + 1)]; };
       auto stays = [&](unsigned u) { return next_to_zero(u) && __uint_as_float(u << 16) > z_border; };
       pass([&](const u32x4& v) {
-             if (tiny) for_some(v, stays, [&](unsigned u) { sum += (u64)weigh(__uint_as_float(u << 16)); });
+             if (tiny) for_some(v, stays, [&](unsigned u) { sum += weigh(__uint_as_float(u << 16)); });
              return false;
            }, of);
       p.leave(sum, number);
       p.search(s, tie_weight, [&](float z, u64& w) {
         const unsigned u = __float_as_uint(z) >> 16;
-        w = (u64)(tiny && stays(u) ? weigh(z) : of(u));
+        w = tiny && stays(u) ? weigh(z) : (u64)of(u);
         return z == z_border;
       });
     }
   } else {
-    double mine = 0.0;
+    u64 mine = 0;
     unsigned number = 0;
     p.each([&](float z) {
       if (z > z_border) mine += weigh(z);
       number += z == z_border;
     });
-    p.leave((u64)mine, number);
+    p.leave(mine, number);
     p.search(s, tie_weight, [&](float z, u64& w) {
-      w = z > z_border ? (u64)weigh(z) : 0;
+      w = z > z_border ? weigh(z) : 0;
       return z == z_border;
     });
   }
@@ -970,7 +1039,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 ? 6 : THREADS == 256 ? 3 : 
     return answer(a, (int)sh.token, 0.f, 1);
   }
   p.c = 1.4426950408889634074 / (double)rule.temperature;
-  const double least = rule.min_p > 0.f ? fmin((double)rule.min_p, 1.0) * ONE : 0.0;
+  const u64 least = rule.min_p > 0.f ? (u64)ceil(fmin((double)rule.min_p, 1.0) * ONE) : 0;
   static_assert(sizeof(List) <= SAMPLE_ROOM, "room");
   if (rule.top_k && rule.top_k <= LIST_TOP_K && rule.top_k < a.cols) {
     if (sample_by_list<T, THREADS>(a, rule, uniform, least, p, *(List*)room)) return;
