@@ -18,8 +18,7 @@ namespace {
 
 typedef unsigned long long u64;
 constexpr unsigned SP_GRID = 1u << 20;
-// (a thread's sum of weights is a whole number of 64-bit floating point: 2^12 of up to 2^40 each in rows of the largest size)
-static_assert(KARMA_SAMPLE_COLS_MAX / 512 < 1u << 12, "exact sums");
+static_assert(KARMA_SAMPLE_COLS_MAX < 1u << 23, "a row's weights of up to 2^40 add up to less than 2^63");
 constexpr int BINS = 2048, LAST = BINS - 1;
 constexpr double ONE = 1099511627776.0;     // 2^40
 // bins reach down to weights of 2^-42 of the largest: what falls into the last one weighs nothing
@@ -419,7 +418,7 @@ struct BinSampler : Sampler<T, THREADS> {
   // The border within a bin: its logits, between `least` and `most`, are put into a list, and a thread adds up what is above one of them.  False if
   // there are more than the list holds.  (1 x 128000 in fp32 with top_p 121 -> 95 us.)
   struct Members {
-    static constexpr unsigned MOST = THREADS < 512 ? THREADS : 512;
+    static constexpr unsigned MOST = 512;      // (a thread for each)
     float logit[MOST];
     u64 weight[MOST], mass[MOST];
     unsigned above[MOST], equal[MOST], n;
@@ -797,10 +796,21 @@ __device__ __forceinline__ bool sample_by_counters(const SampleArgs& a, const ka
       others |= at >= CT_SIDE;
     }
     if (!others) return;
-    for_some(v, [&](unsigned u) { return !has_rank(u); },
+    // most of them are masked, -inf or far below
+    constexpr unsigned FAR = 0x8000 + CT_LOW + CT_SIDE, FARS = 0xff80 - FAR;
+    bool left_out = false;
+    others = false;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const unsigned u = i % 2 ? v[i / 2] >> 16 : v[i / 2] & 0xffff;
+      left_out |= u - FAR < FARS;
+      others |= !has_rank(u) && u - FAR > FARS;
+    }
+    if (left_out) ct.left_out = 1;
+    if (!others) return;
+    for_some(v, [&](unsigned u) { return !has_rank(u) && u - FAR > FARS; },
              [&](unsigned u) {
                if (!(u & 0x7fff)) atomicAdd(&ct.zeros, 1u);
-               else if (u >= 0x8000 + CT_LOW + CT_SIDE && u <= 0xff80) { if (u != 0xff80) ct.left_out = 1; }
                else if (next_to_zero(u)) {
                  const unsigned i = atomicAdd(&ct.tiny, 1u);
                  if (i < CT_TINY) ct.tiny_bits[i] = (unsigned short)u;
@@ -1020,7 +1030,7 @@ __device__ __forceinline__ bool sample_by_counters(const SampleArgs& a, const ka
 }
 
 template <typename T, int THREADS>
-__global__ __launch_bounds__(THREADS, THREADS == 512 ? 6 : THREADS == 256 ? 3 : 4) void sample_kernel(SampleArgs a) {
+__global__ __launch_bounds__(THREADS, THREADS == 512 ? 6 : 4) void sample_kernel(SampleArgs a) {
   constexpr bool COUNTED = sizeof(T) == 2;
   __shared__ SampleShared sh;
   __shared__ __attribute__((aligned(16))) unsigned char room[SAMPLE_ROOM];
@@ -1059,13 +1069,10 @@ bool aligned_to(const void* p, size_t n) { return (uintptr_t)p % n == 0; }
 }  // namespace
 
 size_t sample_ws_bytes(uint32_t, uint32_t) { return 0; }
-// Threads of a row.  More of them shorten a row's way (1 x 51200 in bf16 with top_p: 256 / 512 / 1024 threads 58 / 38 / 29 us), fewer leave
-// room for more rows on a compute unit: three of 512 threads, one of 1024 (4096 x 8000: 98 / 102 / 224; 1024 x 16000: 49 / 44 / 70), and wait less
-// for each other where rows are short (64 x 1000 12.3 / 12.5 / 14.5).
-static int sample_threads(uint32_t rows, uint32_t cols) {
-  if (rows <= 256) return cols <= 4096 ? 256 : cols <= 12288 ? 512 : 1024;
-  return cols <= 12288 ? 256 : 512;
-}
+// Threads of a row: more of them shorten a long row's way, where every row has a compute unit to itself (1 x 128000 with top_p in bf16, 512 / 1024
+// threads: 36 / 27 us, in fp32 153 / 95; 256 x 51200 39 / 32 and 86 / 59); otherwise three rows of 512 threads on a compute unit are better than one of 1024
+// (1024 x 16000 38 / 67 and 70 / 87, 4096 x 2000 73 / 187), and than rows of 256 threads, which the LDS allows as many of (57.5, 77 and 70).
+static int sample_threads(uint32_t rows, uint32_t cols) { return rows <= 256 && cols > 12288 ? 1024 : 512; }
 
 int sample_rows(SampleArgs a, bool bf16, hipStream_t s) {
   if (!a.ld) a.ld = a.cols;
@@ -1078,8 +1085,8 @@ int sample_rows(SampleArgs a, bool bf16, hipStream_t s) {
   if (!a.logits || !a.rules || !a.uniform || !aligned_to(a.logits, bf16 ? 2 : 4)) return KARMA_E_INVAL;
 #define KARMA_SAMPLE_LAUNCH(T, THREADS) hipLaunchKernelGGL((sample_kernel<T, THREADS>), dim3(a.rows), dim3(THREADS), 0, s, a)
   const int threads = sample_threads(a.rows, a.cols);
-  if (bf16) { if (threads == 256) KARMA_SAMPLE_LAUNCH(bf16_t, 256); else if (threads == 512) KARMA_SAMPLE_LAUNCH(bf16_t, 512); else KARMA_SAMPLE_LAUNCH(bf16_t, 1024); }
-  else { if (threads == 256) KARMA_SAMPLE_LAUNCH(float, 256); else if (threads == 512) KARMA_SAMPLE_LAUNCH(float, 512); else KARMA_SAMPLE_LAUNCH(float, 1024); }
+  if (bf16) { if (threads == 512) KARMA_SAMPLE_LAUNCH(bf16_t, 512); else KARMA_SAMPLE_LAUNCH(bf16_t, 1024); }
+  else { if (threads == 512) KARMA_SAMPLE_LAUNCH(float, 512); else KARMA_SAMPLE_LAUNCH(float, 1024); }
 #undef KARMA_SAMPLE_LAUNCH
   return hipGetLastError() == hipSuccess ? KARMA_OK : KARMA_E_HIP;
 }
