@@ -744,7 +744,7 @@ __device__ __forceinline__ unsigned rank_of(unsigned u) {
   return u & 0x7fff ? CT_RANKS : RANK_ZERO;
 }
 __device__ __forceinline__ bool next_to_zero(unsigned u) { return (u & 0x7fff) - 1 < CT_LOW - 1; }
-// the room of both ways, which later holds the weights by rank
+// the room of all ways, which later holds the weights by rank; with 49 KB three rows have room on a compute unit
 constexpr size_t SAMPLE_ROOM = sizeof(Counted) > 2 * sizeof(Bins) ? sizeof(Counted) : 2 * sizeof(Bins);
 constexpr unsigned CT_TABLE = SAMPLE_ROOM / sizeof(double);
 
@@ -1029,6 +1029,10 @@ __device__ __forceinline__ bool sample_by_counters(const SampleArgs& a, const ka
   return true;
 }
 
+// A row's way by its rule.  What bounds it: vector operations, of which a compute unit does one of 64 lanes a cycle, and the steps between barriers, some
+// 500 to 2000 cycles each.  8 x 51200 in bf16 with top_k 50 and top_p 0.9: 13 us in the kernel, of which the two passes over the row take 6; 4096 x 32000 with
+// top_p 0.95: 153 us, 25 operations and one LDS atomic a logit, at 1.7 TB/s of logits; 301 x 50021 in fp32 without limits: 47 us, two passes of which
+// the second takes 20 operations of 64 bits a logit.
 template <typename T, int THREADS>
 __global__ __launch_bounds__(THREADS, THREADS == 512 ? 6 : 4) void sample_kernel(SampleArgs a) {
   constexpr bool COUNTED = sizeof(T) == 2;

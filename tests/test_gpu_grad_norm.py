@@ -238,3 +238,41 @@ def test_on_another_stream_and_in_two_graphs():
             gr.replay()
         torch.cuda.synchronize()
         assert all(same(b) for b in lists)
+
+
+def test_a_tensor_beyond_32_bits():
+    import torch
+    n = (1 << 31) + 1001
+    g = torch.ones(n, dtype=torch.bfloat16, device="cuda")
+    g[-1], g[1 << 31] = 300.0, -200.0
+    out = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    a = List([g], [out])
+    assert a.run(1.0) == 0 and a.clip() == 0
+    torch.cuda.synchronize()
+    want = math.sqrt(n - 2 + 300.0 ** 2 + 200.0 ** 2)
+    assert abs(a.norm.item() - want) <= (U + 1e-12) * want and a.each[0].item() == a.norm.item()
+    f = a.factor
+    for i in (0, 1 << 20, (1 << 31) - 1, 1 << 31, (1 << 31) + 1, n - 2, n - 1):
+        assert torch.equal(out[i], (g[i].float() * f[0]).to(torch.bfloat16)), i
+    assert int((out == (f[0]).to(torch.bfloat16)).sum()) == n - 2
+
+
+def test_two_calls_at_once():
+    import torch
+    lists = [List(g, [torch.zeros_like(t) for t in g]) for g in (make([70001, 5000, 33], 11), make([123456, 77], 12, ("f32",)))]
+    want = []
+    for a in lists:
+        assert a.run(2.0) == 0 and a.clip() == 0
+        torch.cuda.synchronize()
+        want.append([t.clone() for t in (a.norm, a.factor, a.each, *a.out)])
+        for t in (a.norm, a.factor, *a.out):
+            t.zero_()
+    streams = [torch.cuda.Stream() for _ in lists]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for a, s in zip(lists, streams):
+            with torch.cuda.stream(s):
+                assert a.run(2.0) == 0 and a.clip() == 0
+    torch.cuda.synchronize()
+    for a, w in zip(lists, want):
+        assert all(torch.equal(x, y) for x, y in zip((a.norm, a.factor, a.each, *a.out), w))

@@ -296,3 +296,28 @@ def test_on_another_stream_and_in_two_graphs():
             gr.replay()
         torch.cuda.synchronize()
         assert all(equal(s) for s in sets)
+
+
+def test_offsets_beyond_32_bits():
+    import torch
+    tokens, d = 3, 64
+    ld = (1 << 31) + 8
+    rng = np.random.default_rng(21)
+    freq = torch.from_numpy(freqs(d)).cuda()
+    room = lambda: torch.empty(2 * ld + d + 64, dtype=torch.bfloat16, device="cuda").as_strided((tokens, d), (ld, 1))
+    x, y, dy, dx = (room() for _ in range(4))
+    for t in (x, dy):
+        t.copy_(torch.from_numpy(rng.standard_normal((tokens, d)).astype(np.float32)).to(torch.bfloat16))
+    import gpu_util as g
+    shape = K.QkShape(tokens=tokens, heads_q=1, d=d, rot=d, flags=K.QK_NORM, eps=EPS, ld_q=ld, ld_yq=ld, ld_dq=ld)
+    lib = K.lib()
+    assert lib.karma_k_qk_rotary_fwd_bf16(g.ptr(x), None, None, None, None, None, g.ptr(freq), g.ptr(y), None, None, C.byref(shape), g.stream_ptr()) == 0
+    assert lib.karma_k_qk_rotary_bwd_bf16(g.ptr(dy), None, None, g.ptr(x), None, None, None, None, g.ptr(freq), g.ptr(dx), None, None, None, None,
+                                          C.byref(shape), None, C.c_uint64(0), g.stream_ptr()) == 0
+    torch.cuda.synchronize()
+    angle = np.arange(tokens)[:, None] * freqs(d)
+    h = lambda t: t.double().cpu().numpy().reshape(tokens, 1, d)
+    want, bound = D.qk_forward(h(x), None, angle, d, False, EPS)
+    assert (np.abs(h(y) - want) <= bound + half(torch.bfloat16) * (np.abs(want) + bound)).all()
+    want, _, bound, _ = D.qk_backward(h(dy), h(x), None, angle, d, False, EPS)
+    assert (np.abs(h(dx) - want) <= bound + half(torch.bfloat16) * (np.abs(want) + bound)).all()

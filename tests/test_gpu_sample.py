@@ -290,3 +290,32 @@ def test_on_another_stream_and_in_two_graphs():
             gr.replay()
         torch.cuda.synchronize()
         assert all(same(s, want) for s in sets)
+
+
+def test_offsets_beyond_32_bits():
+    import torch
+    rng = np.random.default_rng(15)
+    ld = (1 << 31) + 9
+    room = torch.empty(2 * ld + 3000, dtype=torch.bfloat16, device="cuda")
+    z = room.as_strided((3, 2000), (ld, 1))
+    z.copy_(torch.from_numpy((2 * rng.standard_normal((3, 2000))).astype(np.float32)).to(torch.bfloat16))
+    for rules in ([(1.0, 0.9, 0.0, 0)], [(1.0, 1.0, 0.0, 0), (0.8, 0.9, 0.0, 30), (0.0, 1.0, 0.0, 0)]):
+        check(z, rules, rng.random(3).astype(np.float32))
+
+
+def test_two_calls_at_once():
+    import torch
+    rng = np.random.default_rng(16)
+    zs = [torch.from_numpy((2 * rng.standard_normal((300, 9000))).astype(np.float32)).to(t).cuda() for t in (torch.bfloat16, torch.float32)]
+    rules, u = rules_of([RULES[r % len(RULES)] for r in range(300)]), torch.from_numpy(rng.random(300).astype(np.float32)).cuda()
+    want = [draw(z, rules, u) for z in zs]
+    import gpu_util as g
+    streams = [torch.cuda.Stream() for _ in zs]
+    outs = [(torch.zeros(300, dtype=torch.int32, device="cuda"), torch.zeros(300, device="cuda"), torch.zeros(300, dtype=torch.int32, device="cuda")) for _ in zs]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for z, s, o, fn in zip(zs, streams, outs, (K.lib().karma_k_sample_bf16, K.lib().karma_k_sample_f32)):
+            assert fn(g.ptr(z), C.c_uint64(0), g.ptr(rules), 300, g.ptr(u), *map(g.ptr, o), 300, 9000, None, C.c_uint64(0), C.c_void_p(s.cuda_stream)) == 0
+    torch.cuda.synchronize()
+    for o, w in zip(outs, want):
+        assert all(np.array_equal(a.cpu().numpy(), b, equal_nan=a.dtype.is_floating_point) for a, b in zip(o, w))
