@@ -589,7 +589,11 @@ __device__ __forceinline__ void sample_by_bins(const SampleArgs& a, const karma_
 // ------------------------------------------------------------------------------------- by a list of the likeliest tokens
 // With a small top_k: there are at least top_k logits from the threads' top_k-th largest maximum on.  Those, few more than top_k, are put
 // into a list, and all else is sums over pairs of its tokens.  (1 x 128000 in fp32 with top_k 50 and top_p 0.9: 17 us, by bins 106.)
-constexpr unsigned LIST_MOST = 256, LIST_TOP_K = 128;
+// Up to a top_k where the other way is as fast (us by the list / the other way: bf16 512 x 8000 at top_k 96 15.3 / 17.5, at 128 23.4 / 17.3, 2048 x 16000
+// at 96 51 / 54, at 128 78 / 54; fp32 at 128 24.5 / 25.1 and 89 / 122).
+constexpr unsigned LIST_MOST = 256;
+template <typename T>
+constexpr unsigned LIST_TOP_K = sizeof(T) == 2 ? 96 : 128;
 struct List {
   float logit[LIST_MOST];
   unsigned column[LIST_MOST], rank[LIST_MOST];
@@ -1055,7 +1059,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 ? 6 : 4) void sample_kernel
   p.c = 1.4426950408889634074 / (double)rule.temperature;
   const u64 least = rule.min_p > 0.f ? (u64)ceil(fmin((double)rule.min_p, 1.0) * ONE) : 0;
   static_assert(sizeof(List) <= SAMPLE_ROOM, "room");
-  if (rule.top_k && rule.top_k <= LIST_TOP_K && rule.top_k < a.cols) {
+  if (rule.top_k && rule.top_k <= LIST_TOP_K<T> && rule.top_k < a.cols) {
     if (sample_by_list<T, THREADS>(a, rule, uniform, least, p, *(List*)room)) return;
     __syncthreads();
   }

@@ -163,7 +163,7 @@ def test_rows_for_every_number_of_threads(t):
         for u in (rng.random(rows), np.full(rows, 0.999)):
             check(z, rules, u.astype(np.float32))
     z = torch.from_numpy((2 * rng.standard_normal((8, 140001))).astype(np.float32)).to(types()[t]).cuda()
-    check(z, [(1.0, 0.9, 0.0, 0), (0.7, 0.95, 0.0, 40), (1.0, 1.0, 0.0, 0), (1.3, 0.97, 0.02, 0), (1.0, 0.9, 0.0, 128), (1.0, 0.9, 0.0, 129), (1.5, 1.0, 0.0, 5000),
+    check(z, [(1.0, 0.9, 0.0, 0), (0.7, 0.95, 0.0, 40), (1.0, 1.0, 0.0, 0), (1.3, 0.97, 0.02, 0), (1.0, 0.9, 0.0, 96), (1.0, 0.9, 0.0, 129), (1.5, 1.0, 0.0, 5000),
               (0.8, 1.0, 0.1, 0)], rng.random(8).astype(np.float32))
 
 
@@ -175,7 +175,7 @@ def test_many_equal_logits_at_a_small_top_k(t):
     z = torch.from_numpy((0.3 * rng.standard_normal((4, 6000))).astype(np.float32)).to(types()[t]).cuda()
     for some in (100, 300, 5000):
         z[:, rng.permutation(6000)[:some]] = 2.0
-        for k in (2, 50, 128):
+        for k in (2, 50, 96, 97, 128, 129):
             check(z, [(1.0, 0.9, 0.0, k)], np.array([0.0, 0.3, 0.6, 0.99], np.float32))
 
 
