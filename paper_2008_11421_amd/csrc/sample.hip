@@ -178,8 +178,7 @@ struct Sampler {
   template <int B>
   __device__ __forceinline__ void read(u32x4 (&v)[B], unsigned t, unsigned end) const {
     const unsigned past = min(t + B, end);
-    // (with 80 registers the second way serves both: 4096 x 32000 in 167 us instead of 184)
-    if (THREADS != 512 && (t || !skip) && past * TILE <= cols + skip) {
+    if ((t || !skip) && past * TILE <= cols + skip) {
       const T* from = row + (size_t)t * TILE - skip;
 #pragma unroll
       for (int b = 0; b < B; ++b)
@@ -727,7 +726,8 @@ struct Counted {
   unsigned short tiny_bits[CT_TINY];
   u64 mass[CT_GROUPS];
   unsigned count[CT_GROUPS];
-  unsigned short list[CT_GROUPS];     // groups that have any
+  unsigned short list[CT_SIDE / 2];   // vectors of four counters of which one is not 0
+  unsigned vectors;
   // the group that a border falls into and what lies before it; the border found, what stays up to it, and the weight of its rank
   u64 mass_before, stays, border_weight;
   unsigned group, count_before, border, ties, count_stays, first;
@@ -756,8 +756,7 @@ constexpr unsigned CT_TABLE = SAMPLE_ROOM / sizeof(double);
 template <int THREADS>
 __device__ __forceinline__ bool sample_by_counters(const SampleArgs& a, const karma_sample_rule& rule, float uniform, u64 least, Sampler<bf16_t, THREADS>& p,
                                                    Counted& ct) {
-  typedef Sampler<bf16_t, THREADS> S;
-  constexpr int WAVES = S::WAVES, AHEAD = THREADS == 1024 ? 8 : 4;
+  constexpr int AHEAD = THREADS == 1024 ? 8 : 4;
   const int lane = p.lane, wave = p.wave, tid = threadIdx.x;
   // ---- count the row; its first vectors are under way while the counters are cleared
   u32x4 ahead[AHEAD];
@@ -766,7 +765,7 @@ __device__ __forceinline__ bool sample_by_counters(const SampleArgs& a, const ka
   for (int i = tid; i < (int)CT_SIDE / 2; i += THREADS) ((u32x4*)ct.counter)[i] = u32x4{0, 0, 0, 0};
   for (int i = tid; i < (int)CT_GROUPS; i += THREADS) { ct.count[i] = 0; ct.mass[i] = 0; }
   if (tid == 0) {
-    ct.zeros = 0; ct.tiny = 0; ct.other = 0; ct.left_out = 0; ct.first = CT_GROUPS; ct.group = CT_GROUPS; ct.border = CT_RANKS - 1; ct.ties = 0xffffffffu;
+    ct.zeros = 0; ct.tiny = 0; ct.vectors = 0; ct.other = 0; ct.left_out = 0; ct.first = CT_GROUPS; ct.group = CT_GROUPS; ct.border = CT_RANKS - 1; ct.ties = 0xffffffffu;
     ct.border_weight = 0;
   }
   __syncthreads();
@@ -822,20 +821,6 @@ __device__ __forceinline__ bool sample_by_counters(const SampleArgs& a, const ka
                } else ct.other = 1;
              });
   };
-  // 64 counters are 16 lanes' vectors
-  auto count_groups = [&]() {
-    for (int at = tid; at < (int)CT_SIDE / 2; at += THREADS) {
-      const u32x4 v = ((const u32x4*)ct.counter)[at];
-      int n = (int)((v[0] + v[1]) + (v[2] + v[3]));
-      if (!__ballot(n != 0)) continue;
-      n += __builtin_amdgcn_update_dpp(0, n, 0xB1, 0xf, 0xf, false);     // quad_perm [1,0,3,2]
-      n += __builtin_amdgcn_update_dpp(0, n, 0x4E, 0xf, 0xf, false);     // quad_perm [2,3,0,1]
-      n += __builtin_amdgcn_update_dpp(0, n, 0x141, 0xf, 0xf, false);    // row_half_mirror
-      n += __builtin_amdgcn_update_dpp(0, n, 0x140, 0xf, 0xf, false);    // row_mirror
-      const int group = at / 16;
-      if (tid % 16 == 0) ct.count[group < (int)ZERO_GROUP ? ZERO_GROUP - 1 - group : group + 1] = n;
-    }
-  };
   auto largest_of = [](const u32x4& v) {
     // as whole numbers of 16 bits positive logits are ordered and negative ones lie below them
     const short2_t x = max2(max2(as_short2(v[0]), as_short2(v[1])), max2(as_short2(v[2]), as_short2(v[3])));
@@ -844,39 +829,47 @@ __device__ __forceinline__ bool sample_by_counters(const SampleArgs& a, const ka
   for_vectors(count);
   __syncthreads();
   if (ct.other) return false;
-  count_groups();
+  // ---- the counters that are not 0 are put into a list by fours; 64 of them are a group
+  for (int at = tid; at < (int)CT_SIDE / 2; at += THREADS) {
+    const u32x4 v = ((const u32x4*)ct.counter)[at];
+    const unsigned n = (v[0] + v[1]) + (v[2] + v[3]);
+    const u64 some = __ballot(n != 0);
+    if (!some) continue;
+    unsigned place = 0;
+    if (lane == 0) place = atomicAdd(&ct.vectors, (unsigned)__popcll(some));
+    place = __builtin_amdgcn_readfirstlane(place) + __popcll(some & ((1ull << lane) - 1));
+    if (n) {
+      ct.list[place] = (unsigned short)at;
+      atomicAdd(&ct.count[at < (int)CT_SIDE / 4 ? ZERO_GROUP - 1 - at / 16 : at / 16 + 1], n);
+    }
+  }
   if (tid == 0) ct.count[ZERO_GROUP] = ct.zeros + ct.tiny;
   __syncthreads();
-  // ---- the groups that have any, one behind the other, and the largest logit
-  const unsigned own_count = tid < (int)CT_GROUPS ? ct.count[tid] : 0;
+  // ---- the largest logit
+  const unsigned own_count = tid < (int)CT_GROUPS ? ct.count[tid] : 0, tiny = ct.tiny, vectors = ct.vectors;
   u64 row_count;
-  // (counts and groups side by side in one sum)
-  const u64 before = p.block_before((u64)own_count << 32 | (own_count != 0), row_count);
-  const unsigned count_before = (unsigned)(before >> 32), lists = (unsigned)row_count;
-  const unsigned tiny = ct.tiny;
-  if (!lists) return false;
-  if (own_count) {
-    ct.list[(unsigned)before] = (unsigned short)tid;
-    if (!count_before) ct.first = tid;
-  }
+  const unsigned count_before = (unsigned)p.block_before(own_count, row_count);
+  if (!row_count) return false;
+  if (own_count && !count_before) ct.first = tid;
   __syncthreads();
   if (tiny && ct.first == ZERO_GROUP) return false;
   const unsigned first = ct.first * 64 + __ffsll((unsigned long long)__ballot(ct.of(ct.first * 64 + lane) != 0)) - 1;
   p.m = rank_value(first);
   if (ct.left_out && !(p.m + CT_FAR > REACH * rule.temperature)) return false;
 
-  // f(group, its ranks, their counts) with four ranks a lane and four groups a wavefront
+  // f(group, four ranks of it, their counts); 0 and the numbers next to it are another matter
   auto sweep = [&](auto f) {
-    for (unsigned i = wave * 4 + lane / 16; i < lists; i += WAVES * 4) {
-      const unsigned g = ct.list[i], zero = ZERO_GROUP;
-      const u32x4 v = *(const u32x4*)&ct.counter[(g < zero ? zero - 1 - g : g == zero ? 0 : g - 1) * 64 + lane % 16 * 4];
+    for (unsigned i = tid; i < vectors; i += THREADS) {
+      const unsigned at = ct.list[i];
+      const u32x4 v = ((const u32x4*)ct.counter)[at];
+      const bool high = at < CT_SIDE / 4;
       unsigned n[4], r[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        n[j] = g == zero ? (lane % 16 || j ? 0 : ct.zeros) : v[j];
-        r[j] = g < zero ? g * 64 + 63 - (lane % 16 * 4 + j) : g * 64 + lane % 16 * 4 + j;
+        n[j] = v[j];
+        r[j] = high ? CT_SIDE - 1 - (at * 4 + j) : RANK_NEGATIVE - CT_SIDE + at * 4 + j;
       }
-      f(g, r, n);
+      f(high ? ZERO_GROUP - 1 - at / 16 : at / 16 + 1, r, n);
     }
   };
   // (ranks before the first one have no tokens)
@@ -885,14 +878,14 @@ __device__ __forceinline__ bool sample_by_counters(const SampleArgs& a, const ka
     u64 w = 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) w += n[j] * rank_weight(r[j]);
-    if (g == ZERO_GROUP)
-      for (unsigned i = lane % 16; i < tiny; i += 16) w += p.weight(bf2f(ct.tiny_bits[i]));
-    w += dpp_u64<0xB1, 0xf>(w);
-    w += dpp_u64<0x4E, 0xf>(w);
-    w += dpp_u64<0x141, 0xf>(w);
-    w += dpp_u64<0x140, 0xf>(w);
-    if (lane % 16 == 0) ct.mass[g] = w;
+    atomicAdd(&ct.mass[g], w);
   });
+  if (ct.count[ZERO_GROUP] && wave == 0) {
+    u64 w = lane == 0 ? ct.zeros * rank_weight(RANK_ZERO) : 0;
+    if (lane < (int)tiny) w += p.weight(bf2f(ct.tiny_bits[lane]));
+    w = wave_sum_u64(w);
+    if (lane == 0) ct.mass[ZERO_GROUP] = w;
+  }
   __syncthreads();
   const u64 own_mass = tid < (int)CT_GROUPS ? ct.mass[tid] : 0;
   u64 all;
@@ -915,7 +908,7 @@ __device__ __forceinline__ bool sample_by_counters(const SampleArgs& a, const ka
     ct.count_stays = (unsigned)number - (n - some);
   };
   auto from_here = [&]() { ct.group = tid; ct.mass_before = mass_before; ct.count_before = count_before; };
-  if (rule.top_k && rule.top_k < (row_count >> 32)) {
+  if (rule.top_k && rule.top_k < row_count) {
     if (count_before < rule.top_k && count_before + own_count >= rule.top_k) from_here();
     __syncthreads();
     if (tiny && ct.group == ZERO_GROUP) return false;
@@ -937,20 +930,18 @@ __device__ __forceinline__ bool sample_by_counters(const SampleArgs& a, const ka
   else {
     u64 sum = 0;
     unsigned number = 0;
+    auto add = [&](unsigned some, u64 w) {
+      if (w >= least && w) { sum += some * w; number += some; }
+    };
     sweep([&](unsigned g, const unsigned* r, const unsigned* n) {
       if (g > border / 64) return;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const unsigned some = r[j] < border ? n[j] : r[j] == border ? min(n[j], ties) : 0;
-        const u64 w = p.weight(fminf(rank_value(r[j]), p.m));
-        if (w >= least && w) { sum += some * w; number += some; }
-      }
-      if (g == ZERO_GROUP)
-        for (unsigned i = lane % 16; i < tiny; i += 16) {
-          const u64 w = p.weight(bf2f(ct.tiny_bits[i]));
-          if (w >= least && w) { sum += w; ++number; }
-        }
+      for (int j = 0; j < 4; ++j) add(r[j] < border ? n[j] : r[j] == border ? min(n[j], ties) : 0, rank_weight(r[j]));
     });
+    if (border >= RANK_ZERO) {
+      if (tid == 0) add(border > RANK_ZERO ? ct.zeros : min(ct.zeros, ties), rank_weight(RANK_ZERO));
+      if (tid < (int)tiny) add(1, p.weight(bf2f(ct.tiny_bits[tid])));
+    }
     kept = (unsigned)p.block_sum(number);
     all = p.block_sum(sum);
   }
@@ -1035,8 +1026,8 @@ __device__ __forceinline__ bool sample_by_counters(const SampleArgs& a, const ka
 
 // A row's way by its rule.  What bounds it: vector operations, of which a compute unit does one of 64 lanes a cycle, and the steps between barriers, some
 // 500 to 2000 cycles each.  8 x 51200 in bf16 with top_k 50 and top_p 0.9: 13 us in the kernel, of which the two passes over the row take 6; 4096 x 32000 with
-// top_p 0.95: 153 us, 25 operations and one LDS atomic a logit, at 1.7 TB/s of logits; 301 x 50021 in fp32 without limits: 47 us, two passes of which
-// the second takes 20 operations of 64 bits a logit.
+// top_p 0.95: 148 us, 33 vector operations and an LDS atomic a logit, which alone take 115, at 1.8 TB/s of logits; 301 x 50021 in fp32 without limits: 40 us, two
+// passes of which the second takes 20 operations of 64 bits a logit.
 template <typename T, int THREADS>
 __global__ __launch_bounds__(THREADS, THREADS == 512 ? 6 : 4) void sample_kernel(SampleArgs a) {
   constexpr bool COUNTED = sizeof(T) == 2;
