@@ -415,7 +415,7 @@ struct BinSampler : Sampler<T, THREADS> {
   }
 
   // The border within a bin: its logits, between `least` and `most`, are put into a list, and a thread adds up what is above one of them.  False if
-  // there are more than the list holds.  (1 x 128000 in fp32 with top_p 121 -> 95 us.)
+  // there are more than the list holds.  (1 x 128000 in fp32 with top_p 121 -> 96 us.)
   struct Members {
     static constexpr unsigned MOST = 512;      // (a thread for each)
     float logit[MOST];
@@ -587,7 +587,8 @@ __device__ __forceinline__ void sample_by_bins(const SampleArgs& a, const karma_
 
 // ------------------------------------------------------------------------------------- by a list of the likeliest tokens
 // With a small top_k: there are at least top_k logits from the threads' top_k-th largest maximum on.  Those, few more than top_k, are put
-// into a list, and all else is sums over pairs of its tokens.  (1 x 128000 in fp32 with top_k 50 and top_p 0.9: 17 us, by bins 106.)
+// into a list, and all else is sums over pairs of its tokens.  (64 x 51200 in fp32 with top_p 0.95: 20.6 us at top_k 128, 39 by bins
+// at 129.)
 // Up to a top_k where the other way is as fast (us by the list / the other way: bf16 512 x 8000 at top_k 96 15.3 / 17.5, at 128 23.4 / 17.3, 2048 x 16000
 // at 96 51 / 54, at 128 78 / 54; fp32 at 128 24.5 / 25.1 and 89 / 122).
 constexpr unsigned LIST_MOST = 256;
@@ -715,7 +716,8 @@ __device__ __forceinline__ short2_t max2(short2_t a, short2_t b) { return __buil
 // From 2^-14 to 2^18 there are 4096 bf16 numbers, and as many negative ones: the row is counted by its bits, and everything but the draw itself
 // follows from the counters, with one weight for every value that occurs.  Ranks rise as logits fall: the positive ones, a group of 64 for 0
 // alone, the negative ones.  The few numbers next to 0 are kept one by one; what lies below -2^18 is left out (masked logits) where it weighs
-// nothing.  A row that has other numbers, many next to 0, or its border among those goes by bins.
+// nothing.  A row that has other numbers, many next to 0, or its border among those goes by bins.  (1024 x 16000 with top_p 0.95: 39 us; fp32 rows, by
+// bins, 60.)
 constexpr unsigned CT_LOW = 0x3880, CT_SIDE = 4096;
 constexpr unsigned ZERO_GROUP = CT_SIDE / 64, CT_GROUPS = 2 * ZERO_GROUP + 1, RANK_ZERO = CT_SIDE, RANK_NEGATIVE = CT_SIDE + 64, CT_RANKS = RANK_NEGATIVE + CT_SIDE;
 constexpr unsigned CT_TINY = 64;
@@ -1026,7 +1028,7 @@ __device__ __forceinline__ bool sample_by_counters(const SampleArgs& a, const ka
 
 // A row's way by its rule.  What bounds it: vector operations, of which a compute unit does one of 64 lanes a cycle, and the steps between barriers, some
 // 500 to 2000 cycles each.  8 x 51200 in bf16 with top_k 50 and top_p 0.9: 13 us in the kernel, of which the two passes over the row take 6; 4096 x 32000 with
-// top_p 0.95: 148 us, 33 vector operations and an LDS atomic a logit, which alone take 115, at 1.8 TB/s of logits; 301 x 50021 in fp32 without limits: 40 us, two
+// top_p 0.95: 148 us, 33 vector operations and an LDS atomic a logit, which alone take 111, at 1.8 TB/s of logits; 301 x 50021 in fp32 without limits: 40 us, two
 // passes of which the second takes 20 operations of 64 bits a logit.
 template <typename T, int THREADS>
 __global__ __launch_bounds__(THREADS, THREADS == 512 ? 6 : 4) void sample_kernel(SampleArgs a) {
@@ -1068,9 +1070,9 @@ bool aligned_to(const void* p, size_t n) { return (uintptr_t)p % n == 0; }
 }  // namespace
 
 size_t sample_ws_bytes(uint32_t, uint32_t) { return 0; }
-// Threads of a row: more of them shorten a long row's way, where every row has a compute unit to itself (1 x 128000 with top_p in bf16, 512 / 1024
-// threads: 36 / 27 us, in fp32 153 / 95; 256 x 51200 39 / 32 and 86 / 59); otherwise three rows of 512 threads on a compute unit are better than one of 1024
-// (1024 x 16000 38 / 67 and 70 / 87, 4096 x 2000 73 / 187), and than rows of 256 threads, which the LDS allows as many of (57.5, 77 and 70).
+// Threads of a row: more of them shorten a long row's way, where every row has a compute unit to itself (with top_p 0.95, us at 512 / 1024 threads: 1 x 128000 in
+// bf16 34 / 27, in fp32 119 / 96; 256 x 51200 38 / 31 and 64 / 58; 256 x 12000 19.5 / 19.5 and 20.8 / 20.9, 64 x 8000 14.5 / 16.4 and 17.5 / 18.5); otherwise three rows of
+// 512 threads on a compute unit are better than one of 1024 (300 x 51200 44 / 47 and 84 / 99, 1024 x 16000 39 / 67 and 60 / 87, 4096 x 2000 70 / 186 and 74 / 197).
 static int sample_threads(uint32_t rows, uint32_t cols) { return rows <= 256 && cols > 12288 ? 1024 : 512; }
 
 int sample_rows(SampleArgs a, bool bf16, hipStream_t s) {
