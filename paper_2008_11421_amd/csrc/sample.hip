@@ -568,8 +568,10 @@ __device__ __forceinline__ void sample_by_bins(const SampleArgs& a, const karma_
       count += w != 0;
     });
   } else {
+    // what min-p leaves out needs no weight: by logits first, with room for what the cut's roundings move it by
+    const float cut = least > 1 ? p.m + (float)((double)(log2f((float)(least - 1)) - 40.02f) / p.c) - fabsf(p.m) * 0x1p-20f : -INFINITY;
     p.each([&](float z) {
-      if (z > border.logit) {
+      if (z > border.logit && z >= cut) {
         const u64 w = p.weight(z);
         if (w >= least) { mine += w; count += w != 0; }
       }

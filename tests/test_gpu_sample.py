@@ -168,6 +168,19 @@ def test_rows_for_every_number_of_threads(t):
 
 
 @pytest.mark.parametrize("t", ["bf16", "f32"])
+def test_min_p_alone(t):
+    """From next to nothing to the largest, at temperatures and places where few bits are left of the logits' differences."""
+    import torch
+    rng = np.random.default_rng(17)
+    min_p = [1e-12, 2e-12, 3e-12, 1e-9, 1e-3, 0.05, 0.5, 0.999, 1.0]
+    for T in (1e-3, 0.7, 1.0, 50.0, 1e30):
+        for at in (0.0, 40.0, -3000.0, 2.0 ** 20):
+            z = (at + 4 * max(T, 1e-2) * rng.standard_normal((len(min_p), 3000))).astype(np.float32)
+            z = torch.from_numpy(z).clamp(-1e38, 1e38).to(types()[t]).cuda()
+            check(z, [(T, 1.0, m, 0) for m in min_p], rng.random(len(min_p)).astype(np.float32))
+
+
+@pytest.mark.parametrize("t", ["bf16", "f32"])
 def test_many_equal_logits_at_a_small_top_k(t):
     """More tokens than a list of candidates holds, all of them equal."""
     import torch
