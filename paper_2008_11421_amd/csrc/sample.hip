@@ -23,6 +23,8 @@ constexpr int BINS = 2048, LAST = BINS - 1;
 constexpr double ONE = 1099511627776.0;     // 2^40
 // bins reach down to weights of 2^-42 of the largest: what falls into the last one weighs nothing
 constexpr float REACH = 42.f * 0.69314718f;
+// (a small temperature divides into infinity; a large one leaves more than 2e-37)
+__device__ __forceinline__ float bins_per_logit(float temperature) { return fminf((float)LAST / REACH / temperature, 1e30f); }
 
 // A row in 16-byte vectors on 16-byte boundaries: vector v has the columns v N - skip .. + N.
 template <typename T>
@@ -374,9 +376,16 @@ struct BinSampler : Sampler<T, THREADS> {
   typedef Sampler<T, THREADS> S;
   typedef RowVec<T> R;
   Bins &coarse, &fine;
-  float s;                  // bins per logit
+  // bins per logit, of differences that are taken `h` times, and h m.  A difference that 32 bits do not hold weighs nothing up to a temperature of
+  // 1.1e37 (it is more than 29 of those); beyond, halves of the logits are subtracted, whose difference is held.
+  float s, h, hm;
   __device__ __forceinline__ BinSampler(const S& base, Bins* b) : S(base), coarse(b[0]), fine(b[1]) {}
-  __device__ __forceinline__ int bin(float z) const { return (int)fminf((this->m - z) * s, (float)LAST); }
+  __device__ __forceinline__ void scale(float temperature) {
+    h = temperature > 1e37f ? 0.5f : 1.f;
+    hm = h * this->m;
+    s = bins_per_logit(temperature) / h;
+  }
+  __device__ __forceinline__ int bin(float z) const { return (int)fminf(fmaf(-z, h, hm) * s, (float)LAST); }
 
   __device__ __forceinline__ void clear(Bins& b) const {
     __syncthreads();
@@ -487,8 +496,9 @@ struct BinSampler : Sampler<T, THREADS> {
     stays = weigh ? (by_mass ? before : mass_before(coarse, b)) : 0;
     need -= before;
     // the keys of the bin, and some beside them: roundings move a logit by less than `slack`
-    const float near = (float)b / s, far = (float)(b + 1) / s, slack = (fabsf(this->m) + far) * 0x1p-20f;
-    const float most = fminf(this->m - near + slack, this->m), least = fmaxf(this->m - far - slack, -3.4028234e38f);
+    // (infinite where the bin reaches beyond the largest number)
+    const float near = (float)b / (s * h), far = (float)(b + 1) / (s * h), slack = (fabsf(this->m) + far) * 0x1p-20f;
+    const float most = fminf(fmaxf(this->m - near, -3.4028234e38f) + slack, this->m), least = fmaxf(this->m - far - slack, -3.4028234e38f);
     if (among(b, least, most, by_mass, weigh, need, out, stays)) return true;
     unsigned hi = R::key(most), lo = R::key(least);
     for (;;) {
@@ -528,7 +538,7 @@ __device__ __forceinline__ void sample_by_bins(const SampleArgs& a, const karma_
   BinSampler<T, THREADS> p(base, bins);
   float own;
   if (!p.largest(own)) return no_answer(a);
-  p.s = fminf((float)LAST / (REACH * rule.temperature), 1e30f);
+  p.scale(rule.temperature);
   const bool by_count = rule.top_k && rule.top_k < a.cols, by_mass = rule.top_p < 1.f;
   Border border{-INFINITY, 0, 0};
   if (by_count || by_mass) {
@@ -616,7 +626,7 @@ __device__ __forceinline__ bool sample_by_list(const SampleArgs& a, const karma_
     return true;
   }
   // the bin of the top_k-th largest of the threads' maxima, and the smallest maximum that is not behind it
-  const float s = fminf((float)LAST / (REACH * rule.temperature), 1e30f);
+  const float s = bins_per_logit(rule.temperature);
   const int bin = (int)fminf((p.m - own) * s, (float)LAST);
   if (bin < LAST) atomicAdd(&l.count[bin], 1u);
   __syncthreads();

@@ -332,3 +332,24 @@ def test_two_calls_at_once():
     torch.cuda.synchronize()
     for o, w in zip(outs, want):
         assert all(np.array_equal(a.cpu().numpy(), b, equal_nan=a.dtype.is_floating_point) for a, b in zip(o, w))
+
+
+@pytest.mark.parametrize("t", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [1e36, 1.1e37, 1.2e37, 5e37, 1e38, 3e38, 3.4e38])
+def test_temperatures_and_logits_up_to_the_largest_number(t, T):
+    """Differences of logits that 32 bits do not hold, and that weigh something all the same."""
+    import torch
+    top = float(torch.finfo(types()[t]).max)
+    rules = [(T, 0.95, 0.0, 0), (T, 0.5, 0.0, 0), (T, 1.0, 0.0, 0), (T, 1.0, 0.2, 0), (T, 1.0, 0.0, 3), (T, 0.9, 1e-5, 700), (T, 0.999, 0.0, 700), (T, 1.0, 0.0, 2000)]
+    for cols in (2, 5, 900, 4000):
+        rng = np.random.default_rng(cols)
+        h = rng.uniform(-1, 1, (len(rules), cols)) * top
+        h[:, 0], h[:, -1] = top, -top
+        few = np.where(h > 0, 3e38, -3e38)      # two values, many of each
+        mid = 1e-3 * h
+        mid[:, 1::3] = -np.inf
+        mid[:, 1] = -top
+        for z in (h, few, mid, h / 4 - 0.75 * top):
+            z = torch.from_numpy(z).to(types()[t]).cuda()
+            for u in (rng.random(len(rules)), np.full(len(rules), 0.9999)):
+                check(z, rules, u.astype(np.float32))
