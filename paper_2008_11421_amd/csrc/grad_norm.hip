@@ -308,6 +308,7 @@ int grad_norm(const karma_grad_tensor* tensors, uint32_t n, float max_norm, floa
   NormOut o{norm, factor, each, max_norm, scale};
   uint64_t before = 0;
   bool first = norm || factor;
+  bool launched = total > 0;
   uint32_t k = 0;
   do {
     EachSet u;
@@ -320,10 +321,11 @@ int grad_norm(const karma_grad_tensor* tensors, uint32_t n, float max_norm, floa
       }
     const unsigned grid = (first ? 1 : 0) + (u.n + FIN_THREADS / 64 - 1) / (FIN_THREADS / 64);
     if (grid) hipLaunchKernelGGL(grad_finish_kernel, dim3(grid), dim3(FIN_THREADS), 0, s, u, partial, (unsigned)total, o, first ? 1 : 0);
+    launched |= grid > 0;
     o.each = each ? o.each + u.n : nullptr;
     first = false;
   } while (each && k < n);
-  return hipGetLastError() == hipSuccess ? KARMA_OK : KARMA_E_HIP;
+  return !launched || hipGetLastError() == hipSuccess ? KARMA_OK : KARMA_E_HIP;
 }
 
 int grad_clip(const karma_grad_tensor* tensors, uint32_t n, const float* factor, hipStream_t s) {

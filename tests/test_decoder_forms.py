@@ -182,3 +182,8 @@ def test_structures_are_laid_out_as_in_the_header(tmp_path):
     out = subprocess.run([str(tmp_path / "l")], check=True, capture_output=True, text=True).stdout.split("\n")
     for line, (name, s) in zip(out, structures.items()):
         assert [int(v) for v in line.split()] == [C.sizeof(s)] + [getattr(s, f[0]).offset for f in s._fields_], name
+
+
+def test_a_norm_that_launches_nothing_reports_no_error_of_others():
+    """No tensors and only norms of each wanted: there is nothing to do, whatever became of the calls before."""
+    assert K.lib().karma_k_grad_norm(None, 0, C.c_float(1), C.c_float(1), None, P, None, P, u64(8), None) == K.OK
