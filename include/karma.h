@@ -803,7 +803,7 @@ uint64_t karma_k_grad_norm_ws_bytes(const karma_grad_tensor* tensors, uint32_t n
 int karma_k_grad_norm(const karma_grad_tensor* tensors, uint32_t n, float max_norm, float grad_scale, float* norm_dev,
                       float* tensor_norms_dev, float* factor_dev, void* ws_dev, uint64_t ws_bytes, void* stream);
 /* out = factor_dev[0] * grad for every tensor (out may be grad where both have one type: a factor of 1 then touches nothing; no other overlap,
- * other tensors of the list included).  Errors: KARMA_E_INVAL. */
+ * other tensors of the list included).  Errors: KARMA_E_INVAL (out at grad's place with another type among them). */
 int karma_k_grad_clip(const karma_grad_tensor* tensors, uint32_t n, const float* factor_dev, void* stream);
 
 /* ---- convolutional workload (Sec. III-C: convolution, batch normalisation, ReLU and

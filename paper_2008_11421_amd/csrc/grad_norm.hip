@@ -330,8 +330,13 @@ int grad_norm(const karma_grad_tensor* tensors, uint32_t n, float max_norm, floa
 
 int grad_clip(const karma_grad_tensor* tensors, uint32_t n, const float* factor, hipStream_t s) {
   if (!good_grads(tensors, n) || !factor || !aligned_to(factor, 4)) return KARMA_E_INVAL;
-  for (uint32_t k = 0; k < n; ++k)
-    if (tensors[k].n && (!tensors[k].out || (uintptr_t)tensors[k].out > ADDRESS || !aligned_to(tensors[k].out, tensors[k].flags & KARMA_GRAD_OUT_BF16 ? 2 : 4))) return KARMA_E_INVAL;
+  for (uint32_t k = 0; k < n; ++k) {
+    const karma_grad_tensor& t = tensors[k];
+    const size_t out_size = t.flags & KARMA_GRAD_OUT_BF16 ? 2 : 4;
+    if (t.n && (!t.out || (uintptr_t)t.out > ADDRESS || !aligned_to(t.out, out_size))) return KARMA_E_INVAL;
+    // in place: a lane reads what it writes, and no other one does, if both have one size
+    if (t.n && t.out == t.grad && out_size != grad_size(t)) return KARMA_E_INVAL;
+  }
   bool launched = false;
   for (uint32_t k = 0; k < n;) {
     ClipSet u;

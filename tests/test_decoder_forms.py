@@ -187,3 +187,14 @@ def test_structures_are_laid_out_as_in_the_header(tmp_path):
 def test_a_norm_that_launches_nothing_reports_no_error_of_others():
     """No tensors and only norms of each wanted: there is nothing to do, whatever became of the calls before."""
     assert K.lib().karma_k_grad_norm(None, 0, C.c_float(1), C.c_float(1), None, P, None, P, u64(8), None) == K.OK
+
+
+def test_clipping_in_place_needs_one_type():
+    """A gradient that becomes a value of another size at the same place would be written over before it is read."""
+    one = lambda flags, **change: K.lib().karma_k_grad_clip((K.GradTensor * 2)(K.GradTensor(grad=8192, out=12288, n=4, flags=0),
+                                                                                 K.GradTensor(**{**dict(grad=4096, out=4096, n=10, flags=flags), **change})), 2, P, None)
+    assert one(K.GRAD_OUT_BF16) == K.E_INVAL and one(K.GRAD_BF16) == K.E_INVAL
+    # (the norm does not look at the outputs, nor clipping at those of no values)
+    empty = (K.GradTensor * 1)(K.GradTensor(grad=4096, out=4096, n=0, flags=K.GRAD_OUT_BF16))
+    assert K.lib().karma_k_grad_clip(empty, 1, P, None) == K.OK
+    assert K.grad_norm_ws_bytes((K.GradTensor * 1)(K.GradTensor(grad=4096, out=4096, n=10, flags=K.GRAD_OUT_BF16))) > 0
