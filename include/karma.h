@@ -710,7 +710,8 @@ int karma_k_adamw_states(const karma_adamw_tensor* tensors, uint32_t n, float* c
  * q_dev [tokens][heads_q * d] and k_dev [tokens][heads_k * d] (rows ld_q and ld_k elements apart; 0: one behind the other) become
  * yq_dev and yk_dev (ld_yq, ld_yk); all may be parts of one buffer, such as a projection's thirds, and an output may be its input
  * where their strides are equal; no other overlap.  For every head's x of d columns (even, up to KARMA_QK_D_MAX):
- *   KARMA_QK_NORM: n = x gamma / sqrt(mean(x^2) + eps), gamma [d] of the operands' type (NULL: ones); else n = x, and gamma is NULL;
+ *   KARMA_QK_NORM: n = x gamma / sqrt(mean(x^2) + eps), gamma [d] of the operands' type (NULL: ones; not read where
+ *   there are no heads); else n = x, and gamma is NULL;
  *   the first `rot` columns (even; 0: none, which needs the norm) are turned in pairs: (a, b) -> (a cos - b sin, b cos + a sin) by the
  *   angle position * freq_dev[i], pair i being columns i and i + rot / 2, or with KARMA_QK_PAIRS columns 2 i and 2 i + 1.
  * freq_dev fp64 [rot / 2], radians from one position to the next; positions_dev int32 [tokens], or NULL: token % seq (seq 0: tokens).

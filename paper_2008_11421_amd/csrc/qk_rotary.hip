@@ -529,8 +529,10 @@ static int qk_args(QkArgs& a, const karma_qk_shape& s, bool bf16, bool backward)
     if (reads_x && a.out[k] == a.x[k] && a.ld_out[k] != a.ld_x[k]) return KARMA_E_INVAL;
     if (k < 2 && backward && a.out[k] == a.dy[k] && a.ld_out[k] != a.ld_dy[k]) return KARMA_E_INVAL;
   }
-  for (int k = 0; k < 2; ++k)
+  for (int k = 0; k < 2; ++k) {
     if (a.gamma[k] && (!a.norm || !aligned_to(a.gamma[k], e))) return KARMA_E_INVAL;
+    if (!a.heads[k]) a.gamma[k] = nullptr;      // (the kernels read what is given, in pieces whose size the kinds with heads allow)
+  }
   if (s.rot && s.tokens && (!a.freq || !aligned_to(a.freq, 8))) return KARMA_E_INVAL;
   if (!aligned_to(a.positions, 4)) return KARMA_E_INVAL;
   // values that are in their place stay there

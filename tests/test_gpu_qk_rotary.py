@@ -321,3 +321,23 @@ def test_offsets_beyond_32_bits():
     assert (np.abs(h(y) - want) <= bound + half(torch.bfloat16) * (np.abs(want) + bound)).all()
     want, _, bound, _ = D.qk_backward(h(dy), h(x), None, angle, d, False, EPS)
     assert (np.abs(h(dx) - want) <= bound + half(torch.bfloat16) * (np.abs(want) + bound)).all()
+
+
+@pytest.mark.parametrize("t", ["bf16", "f32"])
+def test_gamma_of_no_heads_is_not_read(t):
+    """Also where it lies on its elements' boundaries alone, while all else allows wide accesses."""
+    import torch
+    for heads in ((3, 0), (0, 3)):
+        c = Case(types()[t], 70, *heads, 0, 128, 64, seed=22)
+        other = 0 if heads[0] == 0 else 1
+        outs = []
+        for gamma in (None, torch.full((136,), float("nan"), dtype=c.t, device="cuda")[1:129]):
+            c.gammas[other] = gamma
+            y, dx, dg = c.buffer(), c.buffer(), [torch.full((128,), 9.0, device="cuda") for _ in range(2)]
+            assert c.fwd(c.x, y) == 0 and c.bwd(c.dy, c.x, dx, dg, c.workspace()) == 0
+            torch.cuda.synchronize()
+            outs.append((y, dx, *dg))
+        assert all(torch.equal(a, b) for a, b in zip(*outs)) and (outs[0][2 + other] == 0).all()
+        c.gammas[other] = None
+        c.check_forward(c.x, outs[1][0])
+        c.check_backward(c.dy, c.x, outs[1][1], outs[1][2:])
