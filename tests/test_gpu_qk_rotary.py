@@ -341,3 +341,44 @@ def test_gamma_of_no_heads_is_not_read(t):
         c.gammas[other] = None
         c.check_forward(c.x, outs[1][0])
         c.check_backward(c.dy, c.x, outs[1][1], outs[1][2:])
+
+
+# Many tokens of many heads: a wavefront has all of a token's heads, or every second group of them, and goes around several times.
+LONG = [
+    # tokens, query, key and value heads, d, rot, pairs, norm, gap, off
+    (8195, 9, 5, 3, 64, 32, False, True, 0, 0),
+    (8195, 9, 5, 3, 152, 152, False, True, 0, 0),
+    (8195, 9, 5, 3, 256, 128, True, True, 0, 0),
+    (8195, 37, 5, 0, 64, 64, False, False, 0, 0),
+    (8195, 9, 5, 0, 96, 0, False, True, 4, 4),
+    (5501, 9, 5, 3, 128, 64, False, True, 1, 1),
+    (5501, 9, 5, 0, 250, 126, True, True, 0, 0),
+]
+
+
+@pytest.mark.parametrize("t", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", LONG, ids=lambda s: "x".join(str(int(v)) for v in s))
+def test_many_tokens_of_many_heads(t, shape):
+    import torch
+    tokens, hq, hk, hv, d, rot, pairs, norm, gap, off = shape
+    c = Case(types()[t], tokens, hq, hk, hv, d, rot, pairs, norm, gap, off, seq=777, seed=tokens + d)
+    x0, dy0 = c.x.clone(), c.dy.clone()
+    y, dx = c.buffer(), c.buffer()
+    dg, dg2, dg3 = ([torch.full((d,), 9.0, device="cuda") if norm else None for _ in range(2)] for _ in range(3))
+    ws = c.workspace() if norm else None
+    assert c.fwd(c.x, y) == 0 and c.bwd(c.dy, c.x, dx, dg, ws) == 0
+    torch.cuda.synchronize()
+    assert torch.equal(c.x, x0) and torch.equal(c.dy, dy0) and c.untouched(y) and c.untouched(dx)
+    c.check_forward(c.x, y)
+    c.check_backward(c.dy, c.x, dx, dg)
+    # in place: y over x, dx over dy, dx over x
+    x2, d2, x3 = c.x.clone(), c.dy.clone(), c.x.clone()
+    assert c.fwd(x2, x2) == 0 and c.bwd(d2, c.x, d2, dg2, ws) == 0
+    same = lambda a, b: torch.equal(c.inside(a), c.inside(b))
+    assert same(x2, y) and same(d2, dx) and c.untouched(x2) and c.untouched(d2)
+    c.heads = (hq, hk, 0)       # (dv over v would be another matter)
+    assert c.bwd(c.dy, x3, x3, dg3, ws) == 0
+    torch.cuda.synchronize()
+    n = (hq + hk) * d
+    assert torch.equal(c.inside(x3)[:, :n], c.inside(dx)[:, :n]) and torch.equal(c.inside(x3)[:, n:], c.inside(x0)[:, n:])
+    assert all(torch.equal(a, b) and torch.equal(a, e) for a, b, e in zip(dg, dg2, dg3) if norm)
