@@ -715,7 +715,8 @@ int karma_k_adamw_states(const karma_adamw_tensor* tensors, uint32_t n, float* c
  *   the first `rot` columns (even; 0: none, which needs the norm) are turned in pairs: (a, b) -> (a cos - b sin, b cos + a sin) by the
  *   angle position * freq_dev[i], pair i being columns i and i + rot / 2, or with KARMA_QK_PAIRS columns 2 i and 2 i + 1.
  * freq_dev fp64 [rot / 2], radians from one position to the next; positions_dev int32 [tokens], or NULL: token % seq (seq 0: tokens).
- * Angles are computed in 64 bits, everything else in 32, rounded once.  |x| up to 1e18: its square has to fit 32 bits.
+ * Angles are computed in 64 bits and, once whole turns are taken off, rounded to 32; everything else is computed in 32 and rounded once.  |x| up
+ * to 1e18: its square has to fit 32 bits.
  * v_dev [tokens][heads_v * d] goes to yv_dev unchanged (heads_v 0, or yv_dev == v_dev: nothing is moved), so that the three parts
  * of a projection's output become those that attention reads.
  * tokens up to KARMA_QK_TOKENS_MAX, heads of a kind up to KARMA_QK_HEADS_MAX.  Errors: KARMA_E_INVAL (operands off their elements'
@@ -739,7 +740,8 @@ int karma_k_qk_rotary_fwd_f32(const float* q_dev, const float* k_dev, const floa
                               const int32_t* positions_dev, const double* freq_dev, float* yq_dev, float* yk_dev, float* yv_dev,
                               const karma_qk_shape* shape, void* stream);
 /* Its backward: dq_dev and dk_dev from the gradients dyq_dev and dyk_dev of its results and from its inputs (q_dev and k_dev are not
- * looked at without the norm); dgamma_q_dev and dgamma_k_dev fp32 [d] (each may be NULL; with the norm only), summed in a fixed order.  dyv_dev goes to
+ * looked at without the norm); dgamma_q_dev and dgamma_k_dev fp32 [d] (each may be NULL; with the norm only), summed in a fixed order, within a
+ * wavefront in 32 bits and beyond in 64.  dyv_dev goes to
  * dv_dev as v_dev does.  An output may be dy or the input of its part where the strides are equal; no other overlap.
  * ws_dev: karma_k_qk_rotary_ws_bytes(shape) bytes (0 for a wrong shape and without the norm), 16-byte aligned, for one call at a
  * time; not looked at where no dgamma is asked for.  Errors: KARMA_E_INVAL, KARMA_E_OOM. */

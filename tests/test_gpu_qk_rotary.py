@@ -382,3 +382,25 @@ def test_many_tokens_of_many_heads(t, shape):
     n = (hq + hk) * d
     assert torch.equal(c.inside(x3)[:, :n], c.inside(dx)[:, :n]) and torch.equal(c.inside(x3)[:, n:], c.inside(x0)[:, n:])
     assert all(torch.equal(a, b) and torch.equal(a, e) for a, b, e in zip(dg, dg2, dg3) if norm)
+
+
+@pytest.mark.parametrize("t", ["bf16", "f32"])
+def test_sums_for_gamma_of_large_terms_that_cancel(t):
+    """With r = 1 and no rotation the terms are whole numbers, one for a token.  Wavefronts and workgroups are added up in 64 bits, each workgroup's sum is rounded to
+    32 and the result is: half a step of all the terms together.  (A partial sum of 2^30 in 32 bits leaves nothing of any 1.)"""
+    bound = U * (2.0 ** 31 + 998) + U * 998
+    import torch
+    for hq, hk in ((1, 1), (1, 0), (0, 1)):
+        c = Case(types()[t], 1000, hq, hk, 0, 64, 0, gamma=False, seed=1)
+        c.inside(c.x).fill_(1.0)
+        c.inside(c.dy).fill_(1.0)
+        c.inside(c.dy)[3] = 2.0 ** 30
+        c.inside(c.dy)[996] = -2.0 ** 30
+        shape = c.shape()
+        shape.eps = 1e-12       # 1 / sqrt(1 + eps) is 1
+        c.shape = lambda: shape
+        dg = [torch.zeros(64, device="cuda") for _ in range(2)]
+        assert c.bwd(c.dy, c.x, c.buffer(), dg, c.workspace()) == 0
+        torch.cuda.synchronize()
+        for got, h in zip(dg, (hq, hk)):
+            assert ((got.double() - 998.0 * h).abs() <= bound * h).all(), (hq, hk)
