@@ -788,7 +788,8 @@ int karma_k_sample_f32(const float* logits_dev, uint64_t ld, const karma_sample_
  * gradients multiplies them by.  norm_dev, factor_dev fp32 [1] and tensor_norms_dev fp32 [n] (s times the norm of each) may be NULL, not
  * all of them; factor_dev may be the grad_scale of a karma_adamw_live, whose update then clips without another pass.  max_norm above 0,
  * INFINITY: no bound.  Sums are taken in 64 bits in a fixed order.  An infinite gradient makes the norm infinite and the factor 0 (with no bound: s), NaN
- * makes both NaN.  Tensors hold n values, bf16 with KARMA_GRAD_BF16, else fp32, on boundaries of their elements; n may be 0 (grad NULL);
+ * makes both NaN.  0 times an infinite value is NaN, clipped and in an update's states and weight: a program looks at the norm before it takes such a
+ * step.  Tensors hold n values, bf16 with KARMA_GRAD_BF16, else fp32, on boundaries of their elements; n may be 0 (grad NULL);
  * all together up to KARMA_GRAD_VALUES_MAX, at most KARMA_GRAD_TENSORS_MAX tensors.  `out` is not looked at.
  * tensors is a host array, read during the call.  ws_dev: karma_k_grad_norm_ws_bytes(tensors, n) bytes (0 for a wrong list), 16-byte aligned, for
  * one call at a time.  Errors: KARMA_E_INVAL, KARMA_E_OOM. */

@@ -276,3 +276,38 @@ def test_two_calls_at_once():
     torch.cuda.synchronize()
     for a, w in zip(lists, want):
         assert all(torch.equal(x, y) for x, y in zip((a.norm, a.factor, a.each, *a.out), w))
+
+
+@pytest.mark.parametrize("t", ["bf16", "f32"])
+@pytest.mark.parametrize("off", [0, 1])
+def test_clipping_and_updates_of_values_that_are_no_numbers(t, off):
+    """What an infinite norm leaves: a factor of 0, under which infinite values become NaN and all others 0; NaN spoils all."""
+    import torch
+    import gpu_util as gu
+    for out in (torch.bfloat16, torch.float32):
+        g = make([1000, 4099], 13, (t,), (off,))
+        g[0][7], g[0][999], g[1][4098], g[1][64] = math.inf, -math.inf, math.inf, -math.inf
+        a = List(g, [torch.full_like(x, 5.0, dtype=out) for x in g])
+        assert a.run(1.0) == 0 and a.clip() == 0
+        torch.cuda.synchronize()
+        assert a.norm.item() == math.inf and a.factor.item() == 0
+        for x, o in zip(g, a.out):
+            assert torch.isnan(o[torch.isinf(x)]).all() and (o[torch.isfinite(x)] == 0).all()
+        # the update that takes the factor: the same values' weights and states
+        live = torch.zeros(4, device="cuda")
+        live[0], live[1] = 1e-3, a.factor[0]
+        live.view(torch.int32)[2] = 1
+        now = K.AdamwStep(lr=9.0, beta1=0.9, beta2=0.95, eps=1e-8, grad_scale=9.0, seed=0, step=9)
+        w, m, v = [torch.ones(x.numel(), device="cuda") for x in g], [torch.zeros(x.numel(), device="cuda") for x in g], [torch.zeros(x.numel(), device="cuda") for x in g]
+        ts = (K.AdamwTensor * 2)(*[K.AdamwTensor(w=w[k].data_ptr(), m=m[k].data_ptr(), v=v[k].data_ptr(), grad=g[k].data_ptr(), n=g[k].numel(),
+                                                 flags=K.ADAMW_GRAD_BF16 if t == "bf16" else 0) for k in range(2)])
+        assert K.lib().karma_k_adamw(ts, 2, C.byref(now), gu.ptr(live), gu.stream_ptr()) == 0
+        torch.cuda.synchronize()
+        for k, x in enumerate(g):
+            bad = torch.isinf(x)
+            for s in (w[k], m[k], v[k]):
+                assert torch.isnan(s[bad]).all() and torch.isfinite(s[~bad]).all()
+        g[0][500] = math.nan
+        assert a.run(1.0) == 0 and a.clip() == 0
+        torch.cuda.synchronize()
+        assert math.isnan(a.norm.item()) and math.isnan(a.factor.item()) and all(torch.isnan(o).all() for o in a.out)
