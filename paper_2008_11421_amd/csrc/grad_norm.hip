@@ -17,7 +17,6 @@ namespace {
 constexpr int GN_THREADS = 256;
 constexpr unsigned GN_GRID = (1u << 24) - 1;        // workgroups of 256 lanes in a launch, which has less than 2^32
 constexpr unsigned GC_SPAN = 4096;                  // elements of a workgroup (clipping)
-static_assert(KARMA_GRAD_VALUES_MAX / GC_SPAN + 1 <= GN_GRID, "a tensor fits a launch");
 
 // The tensors of one launch travel as kernel arguments, 4 KB in all: addresses of 48 bits with what is known of them above, the elements of a
 // tensor's last workgroup, and the workgroups before it.
@@ -41,6 +40,8 @@ struct EachSet {        // tensor k has the partial sums [first[k], first[k + 1]
   unsigned first[MOST + 1];
   int n;
 };
+// (a tensor has up to two spans more than its values fill; the norm's spans are as long or longer)
+static_assert(KARMA_GRAD_VALUES_MAX / GC_SPAN + 2 * NormSet::MOST <= GN_GRID && ClipSet::MOST <= NormSet::MOST, "the tensors of a launch fit it");
 static_assert(sizeof(NormSet) + 16 <= 4096 && sizeof(ClipSet) + 16 <= 4096 && sizeof(EachSet) + 64 <= 4096, "kernel arguments");
 
 template <typename Set>
@@ -295,7 +296,6 @@ int grad_norm(const karma_grad_tensor* tensors, uint32_t n, float max_norm, floa
     for (; k < n && u.n < NormSet::MOST; ++k) {
       const uint64_t more = spans(tensors[k], span);
       if (!more) continue;
-      if (blocks + more > GN_GRID) break;
       u.grad[u.n] = address(tensors[k].grad, tensors[k].flags & KARMA_GRAD_BF16);
       u.last[u.n] = (unsigned short)((extent(tensors[k]) - 1) % span);
       blocks += more;
@@ -347,7 +347,6 @@ int grad_clip(const karma_grad_tensor* tensors, uint32_t n, const float* factor,
       const karma_grad_tensor& t = tensors[k];
       const uint64_t more = spans(t, GC_SPAN);
       if (!more) continue;
-      if (blocks + more > GN_GRID) break;
       u.grad[u.n] = address(t.grad, t.flags & KARMA_GRAD_BF16);
       u.out[u.n] = address(t.out, t.flags & KARMA_GRAD_OUT_BF16);
       u.last[u.n] = (unsigned short)((extent(t) - 1) % GC_SPAN);
