@@ -768,8 +768,8 @@ int karma_k_qk_rotary_bwd_f32(const float* dyq_dev, const float* dyk_dev, const 
  * what stays; kept_dev int32 [rows], how many tokens stay.
  * A logit of -inf has no weight.  A row without answer (NaN or +inf in it, nothing but -inf; a rule with a temperature that is negative, infinite or
  * NaN, or a NaN in top_p or min_p) gives token -1, logprob NaN and kept 0.
- * ws_dev: karma_k_sample_ws_bytes(rows, cols) bytes, 16-byte aligned, for one call at a time (none at present: 0 bytes, may be NULL).
- * cols up to KARMA_SAMPLE_COLS_MAX, rows < 2^20.  Errors: KARMA_E_INVAL (operands off their elements' boundaries among them), KARMA_E_OOM. */
+ * ws_dev: karma_k_sample_ws_bytes(rows, cols) bytes, 16-byte aligned, for one call at a time.  At present that is 0 bytes: it may be NULL and is not
+ * looked at.  cols up to KARMA_SAMPLE_COLS_MAX, rows < 2^20.  Errors: KARMA_E_INVAL (operands off their elements' boundaries among them). */
 #define KARMA_SAMPLE_COLS_MAX ((1u << 21) - 1)
 typedef struct {
   float temperature, top_p, min_p;

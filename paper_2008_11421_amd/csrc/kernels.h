@@ -222,9 +222,7 @@ struct SampleArgs {
   const float* uniform;
   int* token; float* logprob; int* kept;
   uint32_t rows, cols;
-  void* ws; size_t ws_bytes;
 };
-size_t sample_ws_bytes(uint32_t rows, uint32_t cols);
 int sample_rows(SampleArgs a, bool bf16, hipStream_t s);
 
 // ---- the global norm of gradients, clipping (grad_norm.hip)

@@ -4,7 +4,8 @@
 // Tokens are ordered by falling logit, equal ones by rising index; what top-k, top-p and min-p leave is a beginning of that order: all tokens
 // above a logit, the border, and the first `ties` of those that equal it.  The border is found by counting and weighing the row, without sorting,
 // and the draw by sums over runs of columns: of the wavefronts, of tiles, of lanes.
-// A workgroup has a row and goes over it a few times: the first time from memory, then from the L2.
+// A workgroup has a row and goes over it a few times: the first time from memory, then from the L2 where the rows under way fit it (4096 x 32000 in
+// bf16, three rows of 64 KB on a compute unit, reads 464 MB for 250 MB of logits; 301 x 50021 in fp32 117 MB for 57).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -1040,7 +1041,9 @@ __device__ __forceinline__ bool sample_by_counters(const SampleArgs& a, const ka
 
 // A row's way by its rule.  What bounds it: vector operations, of which a compute unit does one of 64 lanes a cycle, and the steps between barriers, some
 // 500 to 2000 cycles each.  8 x 51200 in bf16 with top_k 50 and top_p 0.9: 13 us in the kernel, of which the two passes over the row take 6; 4096 x 32000 with
-// top_p 0.95: 148 us, 33 vector operations and an LDS atomic a logit, which alone take 111, at 1.8 TB/s of logits; 301 x 50021 in fp32 without limits: 40 us, two
+// top_p 0.95: 147 us, at 1.8 TB/s of logits.  Some 64 of them do not depend on the columns (4096 x 500 takes 73, x 2000 69, x 8000 87): clearing and
+// walking the counters, weights of the values that occur, a table of them, some twenty barriers, 6600 vector operations a row by counter; the rest is 20 vector
+// operations, an LDS atomic and an LDS read a logit, of which the operations alone take 67.  301 x 50021 in fp32 without limits: 40 us, two
 // passes of which the second takes 20 operations of 64 bits a logit.
 template <typename T, int THREADS>
 __global__ __launch_bounds__(THREADS, THREADS == 512 ? 6 : 4) void sample_kernel(SampleArgs a) {
@@ -1081,7 +1084,6 @@ bool aligned_to(const void* p, size_t n) { return (uintptr_t)p % n == 0; }
 
 }  // namespace
 
-size_t sample_ws_bytes(uint32_t, uint32_t) { return 0; }
 // Threads of a row: more of them shorten a long row's way, where every row has a compute unit to itself (with top_p 0.95, us at 512 / 1024 threads: 1 x 128000 in
 // bf16 34 / 27, in fp32 119 / 96; 256 x 51200 38 / 31 and 64 / 58; 256 x 12000 19.5 / 19.5 and 20.8 / 20.9, 64 x 8000 14.5 / 16.4 and 17.5 / 18.5); otherwise three rows of
 // 512 threads on a compute unit are better than one of 1024 (300 x 51200 44 / 47 and 84 / 99, 1024 x 16000 39 / 67 and 60 / 87, 4096 x 2000 70 / 186 and 74 / 197).
@@ -1108,14 +1110,14 @@ int sample_rows(SampleArgs a, bool bf16, hipStream_t s) {
 
 using namespace karma;
 
-extern "C" uint64_t karma_k_sample_ws_bytes(uint32_t rows, uint32_t cols) { return sample_ws_bytes(rows, cols); }
+// (none is needed: a row is one workgroup's)
+extern "C" uint64_t karma_k_sample_ws_bytes(uint32_t, uint32_t) { return 0; }
 
 #define KARMA_SAMPLE_ENTRY(SUFFIX, T, BF16)                                                                                                  \
   extern "C" int karma_k_sample_##SUFFIX(const T* logits, uint64_t ld, const karma_sample_rule* rules, uint32_t n_rules, const float* uniform, \
-                                         int32_t* token, float* logprob, int32_t* kept, uint32_t rows, uint32_t cols, void* ws,              \
-                                         uint64_t ws_bytes, void* stream) {                                                                  \
-    return sample_rows(SampleArgs{logits, ld, rules, n_rules, uniform, token, logprob, kept, rows, cols, ws, ws ? ws_bytes : 0}, BF16,       \
-                       (hipStream_t)stream);                                                                                                 \
+                                         int32_t* token, float* logprob, int32_t* kept, uint32_t rows, uint32_t cols, void*, uint64_t,       \
+                                         void* stream) {                                                                                     \
+    return sample_rows(SampleArgs{logits, ld, rules, n_rules, uniform, token, logprob, kept, rows, cols}, BF16, (hipStream_t)stream);        \
   }
 KARMA_SAMPLE_ENTRY(bf16, void, true)
 KARMA_SAMPLE_ENTRY(f32, float, false)
