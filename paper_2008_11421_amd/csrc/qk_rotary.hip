@@ -499,7 +499,7 @@ void deal(QkArgs& a, QkCut c) {
   a.lanes = 1;
   while (a.lanes * c.nu < units) a.lanes *= 2;
   const int per = 64 / a.lanes;
-  // (values do not count: whether they are moved changes no order of sums)
+  // (values do not count: whether they are moved changes the order of sums only where they allow narrower accesses than queries and keys do)
   const int rounds = (a.heads[0] + per - 1) / per + (a.heads[1] + per - 1) / per;
   a.parts = (int)std::min<uint64_t>(rounds, std::max<uint64_t>(1, QK_PLACES / std::max(a.tokens, 1u)));
 }
